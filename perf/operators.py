@@ -158,7 +158,8 @@ def _run_own(s):
 
 def _quantise(x):
     top = x.abs().amax(1, keepdim=True)
-    return torch.round(x * (127.0 / top)), top / 127.0
+    most = torch.full_like(top, 127.0)      # (a division by or of a number is not rounded as one of two tensors is)
+    return torch.round(x * (most / top)), top / most
 
 
 def _norm(x, gamma, beta):
