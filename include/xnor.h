@@ -436,6 +436,118 @@ int xnor_conv2d_fwd_static(const uint32_t *Ipk, const uint32_t *Wpk, const float
 int xnor_conv2d_pick_algo(const xnor_shape *s, size_t workspace_bytes);
 
 /*
+ * Dense layers: what stands beside the binary convolutions in a network of layers with few bits -- the 8-bit linear
+ * layer, layer norm, and the gated feed-forward block, which is trained in 16 bits and served in 8.  The 8-bit product is rescaled
+ * as a binary convolution is: one factor per token (there K, per position) and one per output channel (there alpha).
+ *
+ * Conventions beside those above
+ *   - Matrices are [rows][columns] with consecutive columns and a stride between rows, in values.  Input strides
+ *     are >= 0 (0: one row for all); strides of outputs are >= the number of columns.  Rows may start at any multiple of
+ *     a value's size; those of 8-bit operands that start at multiples of 16 bytes (xnor_int8_quantize with such a
+ *     q_stride) and of 16-bit ones that do are read faster.
+ *   - Types of real values are given as an xnor_type; others than those named at a call: XNOR_E_UNSUPPORTED.
+ *   - The number of tokens (M, rows) may be 0: then nothing is launched for them, their pointers may be NULL, and gradients of
+ *     weights are written as zeros.  Other sizes are >= 1, at most 2^30.
+ *   - Sums, statistics and scales are fp32 or (8-bit products) exact 32-bit integers; each output is rounded once from fp32, to
+ *     nearest, ties to even.
+ */
+typedef enum { XNOR_TYPE_FP32 = 0, XNOR_TYPE_F16 = 1, XNOR_TYPE_BF16 = 2 } xnor_type;
+
+/* silu(g) = g / (1 + exp(-g)); gelu(g) = g (1 + erf(g / sqrt 2)) / 2; relu(g) = max(g, 0), slope 0 at 0 */
+typedef enum { XNOR_ACT_SILU = 0, XNOR_ACT_GELU = 1, XNOR_ACT_RELU = 2 } xnor_act;
+
+/*
+ * Rows to 8 bits: scale[r] = top / 127 with top = max_c |x[r][c]|, q[r][c] = x[r][c] * (127 / top) rounded to nearest, ties to
+ * even (both factors and the product in fp32).  For tokens before xnor_int8_matmul, and for weights (rows = output channels).
+ * A row whose largest magnitude is below 2^-100 is quantised to zeros with scale 0; one that holds a NaN or an infinity to
+ * zeros with scale NaN, so that what is computed from it is NaN.
+ *   x      in   [rows][cols], x_type any
+ *   q      out  int8 [rows][cols]
+ *   scale  out  fp32 [rows]
+ */
+int xnor_int8_quantize(const void *x, int x_type, long long rows, int cols, long long x_stride, int8_t *q,
+                       long long q_stride, float *scale, void *stream);
+
+/*
+ * 8-bit product: out[m][n] = float(sum_k a[m][k] b[n][k]) * (a_scale[m] * b_scale[n]) + bias[n].
+ *   a       in   int8 [M][K], a_scale fp32 [M]      b  in  int8 [N][K], b_scale fp32 [N]
+ *   bias    in   fp32 [N] or NULL
+ *   out     out  [M][N], out_type any
+ * The integer sum is exact: K < 2^17, else XNOR_E_SHAPE.
+ */
+int xnor_int8_matmul(const int8_t *a, long long a_stride, const float *a_scale, const int8_t *b, long long b_stride,
+                     const float *b_scale, const float *bias, long long M, int N, int K, void *out, int out_type,
+                     long long out_stride, void *stream);
+
+/*
+ * A linear layer with 8-bit weights on real tokens: xnor_int8_quantize of x and xnor_int8_matmul with w, the same values.
+ *   workspace   16-byte aligned, xnor_int8_linear_workspace_bytes bytes (host only); its contents mean nothing afterwards
+ */
+int xnor_int8_linear_workspace_bytes(long long M, int K, size_t *bytes);
+int xnor_int8_linear(const void *x, int x_type, long long x_stride, const int8_t *w, long long w_stride, const float *w_scale,
+                     const float *bias, long long M, int N, int K, void *out, int out_type, long long out_stride,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Layer norm over the columns: xh = (x - mean) * rstd, rstd = 1 / sqrt(var + eps) with the mean of squares about the mean,
+ * y = xh * gamma + beta.
+ *   x            in   [rows][cols], x_type any
+ *   gamma, beta  in   [cols], p_type (XNOR_TYPE_FP32 or x's type), or NULL: 1 and 0
+ *   y            out  [rows][cols], x's type
+ *   mean, rstd   out  fp32 [rows], each may be NULL
+ * _int8: y quantised as by xnor_int8_quantize, from fp32, without its ever being written in x's type.
+ * eps >= 0, else XNOR_E_SHAPE.
+ */
+int xnor_layer_norm_fwd(const void *x, int x_type, long long rows, int cols, long long x_stride, const void *gamma,
+                        const void *beta, int p_type, float eps, void *y, long long y_stride, float *mean, float *rstd,
+                        void *stream);
+int xnor_layer_norm_fwd_int8(const void *x, int x_type, long long rows, int cols, long long x_stride, const void *gamma,
+                             const void *beta, int p_type, float eps, int8_t *q, long long q_stride, float *scale,
+                             float *mean, float *rstd, void *stream);
+
+/*
+ * Its gradients: with p = dy * gamma, dx = rstd * (p - mean_c(p) - xh * mean_c(p * xh)); dgamma = sum over rows of dy * xh,
+ * dbeta = sum over rows of dy, added in an order that depends on the sizes alone (the same inputs give the same bits).
+ *   dy, x, mean, rstd, gamma   in   as above (gamma may be NULL)
+ *   dx             out  [rows][cols], x's type
+ *   dgamma, dbeta  out  [cols], p_type; or both NULL (parameters that are not trained)
+ *   workspace      16-byte aligned, xnor_layer_norm_bwd_workspace_bytes bytes (host only); may be NULL without dgamma
+ */
+int xnor_layer_norm_bwd_workspace_bytes(int x_type, long long rows, int cols, size_t *bytes);
+int xnor_layer_norm_bwd(const void *dy, long long dy_stride, const void *x, int x_type, long long rows, int cols,
+                        long long x_stride, const void *gamma, int p_type, const float *mean, const float *rstd, void *dx,
+                        long long dx_stride, void *dgamma, void *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gated feed-forward block, both products, the activation and the product of the two in one kernel:
+ *     g = x wg^T, u = x wu^T, h = act(g) * u          (act: an xnor_act, else XNOR_E_UNSUPPORTED)
+ *   x        in   [M][K], type XNOR_TYPE_F16 or _BF16, like all that follow
+ *   wg, wu   in   [F][K] (one stride)
+ *   h        out  [M][F]
+ *   g, u     out  [M][F] (one stride), rounded, for the backward pass; or both NULL.  h is formed from g and u before they are rounded.
+ * Gradients, from those of h and the g and u that the forward pass left:
+ *     dg = dh * u * act'(g), du = dh * act(g);  dx = dg wg + du wu, dwg = dg^T x, dwu = du^T x
+ * dg and du are rounded to the block's type before the products, as the matrix instructions take them.
+ *   workspace  16-byte aligned, xnor_gated_bwd_workspace_bytes bytes (host only); its contents mean nothing afterwards
+ */
+int xnor_gated_fwd(const void *x, int type, long long x_stride, const void *wg, const void *wu, long long w_stride, int act,
+                   long long M, int F, int K, void *h, long long h_stride, void *g, void *u, long long gu_stride, void *stream);
+int xnor_gated_bwd_workspace_bytes(long long M, int F, int K, size_t *bytes);
+int xnor_gated_bwd(const void *dh, long long dh_stride, const void *x, int type, long long x_stride, const void *wg,
+                   const void *wu, long long w_stride, const void *g, const void *u, long long gu_stride, int act, long long M,
+                   int F, int K, void *dx, long long dx_stride, void *dwg, void *dwu, long long dw_stride, void *workspace,
+                   size_t workspace_bytes, void *stream);
+
+/*
+ * The gated block on 8-bit tokens and weights: g and u as by xnor_int8_matmul (without a bias, in fp32), h = act(g) * u.
+ *   a   in  int8 [M][K], a_scale fp32 [M]     wg, wu  in  int8 [F][K] (one stride), their scales fp32 [F]
+ *   h   out [M][F], h_type any                K < 2^17
+ */
+int xnor_int8_gated(const int8_t *a, long long a_stride, const float *a_scale, const int8_t *wg, const float *wg_scale,
+                    const int8_t *wu, const float *wu_scale, long long w_stride, int act, long long M, int F, int K, void *h,
+                    int h_type, long long h_stride, void *stream);
+
+/*
  * Measurement probes (no part of the forward pass): what the GPU at hand sustains on the resources
  * the kernels above are priced against, for reading a roofline fraction against a measured
  * ceiling beside the published one.  Each enqueues one kernel on `stream` and returns; the caller

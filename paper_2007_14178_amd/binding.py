@@ -131,7 +131,23 @@ def _load() -> ctypes.CDLL:
     L.xnor_bwn_split_plan.argtypes = [sp, ci, ctypes.POINTER(ci), ctypes.POINTER(ci), ctypes.POINTER(sz),
                                       ctypes.POINTER(ctypes.c_longlong)]
     L.xnor_conv2d_workspace_bytes.argtypes = [sp, ctypes.POINTER(sz)]
-    for name in ("xnor_out_dim", "xnor_packed_words", "xnor_binarize_pack", "xnor_scale_K",
+    ll = ctypes.c_longlong
+    L.xnor_int8_quantize.argtypes = [vp, ci, ll, ci, ll, vp, ll, vp, vp]
+    L.xnor_int8_matmul.argtypes = [vp, ll, vp, vp, ll, vp, vp, ll, ci, ci, vp, ci, ll, vp]
+    L.xnor_int8_linear_workspace_bytes.argtypes = [ll, ci, ctypes.POINTER(sz)]
+    L.xnor_int8_linear.argtypes = [vp, ci, ll, vp, ll, vp, vp, ll, ci, ci, vp, ci, ll, vp, sz, vp]
+    L.xnor_int8_gated.argtypes = [vp, ll, vp, vp, vp, vp, vp, ll, ci, ll, ci, ci, vp, ci, ll, vp]
+    L.xnor_layer_norm_fwd.argtypes = [vp, ci, ll, ci, ll, vp, vp, ci, ctypes.c_float, vp, ll, vp, vp, vp]
+    L.xnor_layer_norm_fwd_int8.argtypes = [vp, ci, ll, ci, ll, vp, vp, ci, ctypes.c_float, vp, ll, vp, vp, vp, vp]
+    L.xnor_layer_norm_bwd_workspace_bytes.argtypes = [ci, ll, ci, ctypes.POINTER(sz)]
+    L.xnor_layer_norm_bwd.argtypes = [vp, ll, vp, ci, ll, ci, ll, vp, ci, vp, vp, vp, ll, vp, vp, vp, sz, vp]
+    L.xnor_gated_fwd.argtypes = [vp, ci, ll, vp, vp, ll, ci, ll, ci, ci, vp, ll, vp, vp, ll, vp]
+    L.xnor_gated_bwd_workspace_bytes.argtypes = [ll, ci, ci, ctypes.POINTER(sz)]
+    L.xnor_gated_bwd.argtypes = [vp, ll, vp, ci, ll, vp, vp, ll, vp, vp, ll, ci, ll, ci, ci, vp, ll, vp, vp, ll, vp, sz, vp]
+    for name in ("xnor_int8_quantize", "xnor_int8_matmul", "xnor_int8_linear_workspace_bytes", "xnor_int8_linear", "xnor_int8_gated",
+                 "xnor_layer_norm_fwd", "xnor_layer_norm_fwd_int8", "xnor_layer_norm_bwd_workspace_bytes", "xnor_layer_norm_bwd",
+                 "xnor_gated_fwd", "xnor_gated_bwd_workspace_bytes", "xnor_gated_bwd",
+                 "xnor_out_dim", "xnor_packed_words", "xnor_binarize_pack", "xnor_scale_K",
                  "xnor_alpha", "xnor_conv2d_fwd", "xnor_conv2d_fwd_algo", "xnor_conv2d_pick_algo",
                  "xnor_conv2d_workspace_bytes", "xnor_input_prepare", "xnor_filter_prepare",
                  "xnor_filter_expand", "xnor_conv2d_fwd_expanded", "xnor_box_filter_K",
@@ -635,3 +651,250 @@ def xnor_conv2d_fwd_chain(Ipk: torch.Tensor, Wpk: torch.Tensor | None, K: torch.
         _dev(Opk, torch.int32, (s.N, OH, OW, Cwn), "Opk"), _dev(A_next, torch.float32, (s.N, OH, OW), "A_next"),
         _dev(workspace, torch.uint8, name="workspace"), workspace.numel(), algo, _stream()), "xnor_conv2d_fwd_chain")
     return Opk, A_next
+
+
+# ---- dense layers: 8-bit products, layer norm, the gated feed-forward block -------------------------------------------
+
+TYPE_FP32, TYPE_F16, TYPE_BF16 = 0, 1, 2
+ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
+_TYPES = {torch.float32: TYPE_FP32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}
+
+
+def _real(dtype: torch.dtype, name: str) -> int:
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        raise TypeError(f"{name}: need torch.float32, float16 or bfloat16, got {dtype}")
+    return kind
+
+
+def _rows(t: torch.Tensor, dtype, shape, name: str) -> tuple[int, int]:
+    """Pointer and row stride of a matrix whose columns are consecutive (or that has only one)."""
+    if not t.is_cuda or t.dtype is not dtype or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] != 1):
+        raise TypeError(f"{name}: need a GPU matrix of {dtype} with consecutive columns, got {t.dtype} on {t.device}, strides {t.stride()}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} != expected {tuple(shape)}")
+    return t.data_ptr(), t.stride(0)
+
+
+def _matrix(t: torch.Tensor, name: str) -> tuple[int, int]:
+    if t.dim() != 2:
+        raise ValueError(f"{name}: need a matrix, got shape {tuple(t.shape)}")
+    return t.shape
+
+
+def _out_rows(t: torch.Tensor | None, like: torch.Tensor, dtype, shape, name: str) -> tuple[torch.Tensor, int, int]:
+    """An output matrix, its pointer and its row stride: the caller's after the checks, or a new one."""
+    if t is None:
+        t = like.new_empty(shape, dtype=dtype)
+        return t, t.data_ptr(), shape[1]
+    ptr, stride = _rows(t, dtype, shape, name)
+    return t, ptr, stride if shape[0] > 1 else max(stride, shape[1])      # (one row's stride means nothing)
+
+
+def _params(gamma: torch.Tensor | None, beta: torch.Tensor | None, cols: int) -> tuple[int | None, int | None, int]:
+    """Pointers of the norm's parameters and their type."""
+    one = gamma if gamma is not None else beta
+    if one is None:
+        return None, None, TYPE_FP32
+    kind = _real(one.dtype, "gamma")
+    return (_dev(gamma, one.dtype, (cols,), "gamma") if gamma is not None else None,
+            _dev(beta, one.dtype, (cols,), "beta") if beta is not None else None, kind)
+
+
+def _new_int8(like: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
+    """8-bit rows that start at multiples of 16 bytes, which the products read fastest."""
+    return like.new_empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8)[:, :cols]
+
+
+def _workspace(given: torch.Tensor | None, like: torch.Tensor, nbytes: int) -> tuple[torch.Tensor, int, int]:
+    if given is None:
+        given = like.new_empty((nbytes,), dtype=torch.uint8)
+        return given, given.data_ptr(), nbytes
+    return given, _dev(given, torch.uint8, name="workspace"), given.numel()
+
+
+def xnor_int8_quantize(x: torch.Tensor, q: torch.Tensor | None = None, scale: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Rows of x (fp32, f16, bf16) to 8 bits: returns (q int8 [rows][cols], scale fp32 [rows]).  For tokens and for weights."""
+    rows, cols = _matrix(x, "x")
+    kind = _real(x.dtype, "x")
+    ptr, stride = _rows(x, x.dtype, x.shape, "x")
+    q, q_ptr, q_stride = _out_rows(_new_int8(x, rows, cols) if q is None else q, x, torch.int8, (rows, cols), "q")
+    scale, s_ptr = _own(scale, x, torch.float32, (rows,), "scale")
+    _ok(lib.xnor_int8_quantize(ptr, kind, rows, cols, stride, q_ptr, q_stride, s_ptr, _stream()), "xnor_int8_quantize")
+    return q, scale
+
+
+def xnor_int8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_scale: torch.Tensor, bias: torch.Tensor | None = None,
+                     out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """out[m][n] = (a b^T)[m][n] * (a_scale[m] * b_scale[n]) + bias[n] for int8 a [M][K], b [N][K].  ``out_dtype``: of a new out."""
+    (M, K), (N, _) = _matrix(a, "a"), _matrix(b, "b")
+    a_ptr, a_stride = _rows(a, torch.int8, (M, K), "a")
+    b_ptr, b_stride = _rows(b, torch.int8, (N, K), "b")
+    dtype = out.dtype if out is not None else out_dtype
+    kind = _real(dtype, "out")
+    out, o_ptr, o_stride = _out_rows(out, a, dtype, (M, N), "out")
+    _ok(lib.xnor_int8_matmul(a_ptr, a_stride, _dev(a_scale, torch.float32, (M,), "a_scale"), b_ptr, b_stride,
+                             _dev(b_scale, torch.float32, (N,), "b_scale"), _dev(bias, torch.float32, (N,), "bias") if bias is not None else None,
+                             M, N, K, o_ptr, kind, o_stride, _stream()), "xnor_int8_matmul")
+    return out
+
+
+def xnor_int8_linear_workspace_bytes(M: int, K: int) -> int:
+    n = ctypes.c_size_t()
+    _ok(lib.xnor_int8_linear_workspace_bytes(M, K, ctypes.byref(n)), "xnor_int8_linear_workspace_bytes")
+    return n.value
+
+
+def xnor_int8_linear(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                     out_dtype: torch.dtype | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Linear layer with 8-bit weights w [N][K] on real tokens x [M][K], quantised on the way.  ``out_dtype`` (of a new
+    out): x's by default; ``workspace``: uint8, xnor_int8_linear_workspace_bytes, a new one by default."""
+    (M, K), (N, _) = _matrix(x, "x"), _matrix(w, "w")
+    x_kind = _real(x.dtype, "x")
+    x_ptr, x_stride = _rows(x, x.dtype, x.shape, "x")
+    w_ptr, w_stride = _rows(w, torch.int8, (N, K), "w")
+    dtype = out.dtype if out is not None else out_dtype or x.dtype
+    kind = _real(dtype, "out")
+    out, o_ptr, o_stride = _out_rows(out, x, dtype, (M, N), "out")
+    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int8_linear_workspace_bytes(M, K) if workspace is None else 0)
+    _ok(lib.xnor_int8_linear(x_ptr, x_kind, x_stride, w_ptr, w_stride, _dev(w_scale, torch.float32, (N,), "w_scale"),
+                             _dev(bias, torch.float32, (N,), "bias") if bias is not None else None, M, N, K, o_ptr, kind, o_stride,
+                             ws, ws_bytes, _stream()), "xnor_int8_linear")
+    return out
+
+
+def xnor_int8_gated(a: torch.Tensor, a_scale: torch.Tensor, wg: torch.Tensor, wg_scale: torch.Tensor, wu: torch.Tensor, wu_scale: torch.Tensor,
+                    act: int = ACT_SILU, h: torch.Tensor | None = None, out_dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """h = act(g) * u with g, u the 8-bit products of tokens a [M][K] with wg, wu [F][K].  ``out_dtype``: of a new h."""
+    (M, K), (F, _) = _matrix(a, "a"), _matrix(wg, "wg")
+    a_ptr, a_stride = _rows(a, torch.int8, (M, K), "a")
+    g_ptr, w_stride = _rows(wg, torch.int8, (F, K), "wg")
+    u_ptr, u_stride = _rows(wu, torch.int8, (F, K), "wu")
+    if u_stride != w_stride and F > 1:
+        raise ValueError("xnor_int8_gated: wg and wu need the same row stride")
+    dtype = h.dtype if h is not None else out_dtype
+    kind = _real(dtype, "h")
+    h, h_ptr, h_stride = _out_rows(h, a, dtype, (M, F), "h")
+    f32 = torch.float32
+    _ok(lib.xnor_int8_gated(a_ptr, a_stride, _dev(a_scale, f32, (M,), "a_scale"), g_ptr, _dev(wg_scale, f32, (F,), "wg_scale"), u_ptr,
+                            _dev(wu_scale, f32, (F,), "wu_scale"), w_stride, act, M, F, K, h_ptr, kind, h_stride, _stream()), "xnor_int8_gated")
+    return h
+
+
+def xnor_layer_norm_fwd(x: torch.Tensor, gamma: torch.Tensor | None, beta: torch.Tensor | None, eps: float = 1e-5, y: torch.Tensor | None = None,
+                        mean: torch.Tensor | None = None, rstd: torch.Tensor | None = None, want_stats: bool = True):
+    """Layer norm over the columns of x: returns (y, mean, rstd), the last two (for the backward pass) None without want_stats."""
+    rows, cols = _matrix(x, "x")
+    kind = _real(x.dtype, "x")
+    ptr, stride = _rows(x, x.dtype, x.shape, "x")
+    g, b, p_kind = _params(gamma, beta, cols)
+    y, y_ptr, y_stride = _out_rows(y, x, x.dtype, (rows, cols), "y")
+    m = r = None
+    if want_stats:
+        mean, m = _own(mean, x, torch.float32, (rows,), "mean")
+        rstd, r = _own(rstd, x, torch.float32, (rows,), "rstd")
+    _ok(lib.xnor_layer_norm_fwd(ptr, kind, rows, cols, stride, g, b, p_kind, eps, y_ptr, y_stride, m, r, _stream()), "xnor_layer_norm_fwd")
+    return y, (mean if want_stats else None), (rstd if want_stats else None)
+
+
+def xnor_layer_norm_fwd_int8(x: torch.Tensor, gamma: torch.Tensor | None, beta: torch.Tensor | None, eps: float = 1e-5,
+                             q: torch.Tensor | None = None, scale: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Layer norm with its output quantised by row, for the 8-bit products: returns (q, scale)."""
+    rows, cols = _matrix(x, "x")
+    kind = _real(x.dtype, "x")
+    ptr, stride = _rows(x, x.dtype, x.shape, "x")
+    g, b, p_kind = _params(gamma, beta, cols)
+    q, q_ptr, q_stride = _out_rows(_new_int8(x, rows, cols) if q is None else q, x, torch.int8, (rows, cols), "q")
+    scale, s_ptr = _own(scale, x, torch.float32, (rows,), "scale")
+    _ok(lib.xnor_layer_norm_fwd_int8(ptr, kind, rows, cols, stride, g, b, p_kind, eps, q_ptr, q_stride, s_ptr, None, None, _stream()),
+        "xnor_layer_norm_fwd_int8")
+    return q, scale
+
+
+def xnor_layer_norm_bwd_workspace_bytes(dtype: torch.dtype, rows: int, cols: int) -> int:
+    n = ctypes.c_size_t()
+    _ok(lib.xnor_layer_norm_bwd_workspace_bytes(_real(dtype, "x"), rows, cols, ctypes.byref(n)), "xnor_layer_norm_bwd_workspace_bytes")
+    return n.value
+
+
+def xnor_layer_norm_bwd(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor | None, mean: torch.Tensor, rstd: torch.Tensor,
+                        dx: torch.Tensor | None = None, dgamma: torch.Tensor | None = None, dbeta: torch.Tensor | None = None,
+                        workspace: torch.Tensor | None = None, want_params: bool = True):
+    """Gradients of xnor_layer_norm_fwd: returns (dx, dgamma, dbeta), the last two in gamma's type (fp32 without one), or
+    None without want_params."""
+    rows, cols = _matrix(x, "x")
+    kind = _real(x.dtype, "x")
+    x_ptr, x_stride = _rows(x, x.dtype, x.shape, "x")
+    d_ptr, d_stride = _rows(dy, x.dtype, x.shape, "dy")
+    g, _, p_kind = _params(gamma, None, cols)
+    dx, dx_ptr, dx_stride = _out_rows(dx, x, x.dtype, (rows, cols), "dx")
+    dg = db = ws = None
+    ws_bytes = 0
+    if want_params:
+        dtype = gamma.dtype if gamma is not None else torch.float32
+        dgamma, dg = _own(dgamma, x, dtype, (cols,), "dgamma")
+        dbeta, db = _own(dbeta, x, dtype, (cols,), "dbeta")
+        workspace, ws, ws_bytes = _workspace(workspace, x, xnor_layer_norm_bwd_workspace_bytes(x.dtype, rows, cols) if workspace is None else 0)
+    _ok(lib.xnor_layer_norm_bwd(d_ptr, d_stride, x_ptr, kind, rows, cols, x_stride, g, p_kind, _dev(mean, torch.float32, (rows,), "mean"),
+                                _dev(rstd, torch.float32, (rows,), "rstd"), dx_ptr, dx_stride, dg, db, ws, ws_bytes, _stream()),
+        "xnor_layer_norm_bwd")
+    return dx, (dgamma if want_params else None), (dbeta if want_params else None)
+
+
+def _gate_weights(wg: torch.Tensor, wu: torch.Tensor, x: torch.Tensor, where: str) -> tuple[int, int, int, int]:
+    F, K = _matrix(wg, "wg")
+    g_ptr, stride = _rows(wg, x.dtype, (F, x.shape[1]), "wg")
+    u_ptr, u_stride = _rows(wu, x.dtype, (F, x.shape[1]), "wu")
+    if u_stride != stride and F > 1:
+        raise ValueError(f"{where}: wg and wu need the same row stride")
+    return F, g_ptr, u_ptr, stride
+
+
+def xnor_gated_fwd(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: int = ACT_SILU, h: torch.Tensor | None = None,
+                   g: torch.Tensor | None = None, u: torch.Tensor | None = None, want_pre: bool = False):
+    """Gated block h = act(x wg^T) * (x wu^T) in f16 or bf16: returns h, or with want_pre (h, g, u), g and u the two products
+    for the backward pass."""
+    M, K = _matrix(x, "x")
+    kind = _real(x.dtype, "x")
+    x_ptr, x_stride = _rows(x, x.dtype, x.shape, "x")
+    F, g_w, u_w, w_stride = _gate_weights(wg, wu, x, "xnor_gated_fwd")
+    h, h_ptr, h_stride = _out_rows(h, x, x.dtype, (M, F), "h")
+    gp = up = None
+    gu_stride = F
+    if want_pre:
+        g, gp, gu_stride = _out_rows(g, x, x.dtype, (M, F), "g")
+        u, up, u_stride = _out_rows(u, x, x.dtype, (M, F), "u")
+        if u_stride != gu_stride:
+            raise ValueError("xnor_gated_fwd: g and u need the same row stride")
+    _ok(lib.xnor_gated_fwd(x_ptr, kind, x_stride, g_w, u_w, w_stride, act, M, F, K, h_ptr, h_stride, gp, up, gu_stride, _stream()), "xnor_gated_fwd")
+    return (h, g, u) if want_pre else h
+
+
+def xnor_gated_bwd_workspace_bytes(M: int, F: int, K: int) -> int:
+    n = ctypes.c_size_t()
+    _ok(lib.xnor_gated_bwd_workspace_bytes(M, F, K, ctypes.byref(n)), "xnor_gated_bwd_workspace_bytes")
+    return n.value
+
+
+def xnor_gated_bwd(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, g: torch.Tensor, u: torch.Tensor, act: int = ACT_SILU,
+                   dx: torch.Tensor | None = None, dwg: torch.Tensor | None = None, dwu: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None):
+    """Gradients of xnor_gated_fwd from dh and the g and u that it left: returns (dx, dwg, dwu)."""
+    M, K = _matrix(x, "x")
+    kind = _real(x.dtype, "x")
+    x_ptr, x_stride = _rows(x, x.dtype, x.shape, "x")
+    F, g_w, u_w, w_stride = _gate_weights(wg, wu, x, "xnor_gated_bwd")
+    d_ptr, d_stride = _rows(dh, x.dtype, (M, F), "dh")
+    g_ptr, gu_stride = _rows(g, x.dtype, (M, F), "g")
+    u_ptr, u_stride = _rows(u, x.dtype, (M, F), "u")
+    if u_stride != gu_stride and M > 1:
+        raise ValueError("xnor_gated_bwd: g and u need the same row stride")
+    dx, dx_ptr, dx_stride = _out_rows(dx, x, x.dtype, (M, K), "dx")
+    dwg, dg_ptr, dw_stride = _out_rows(dwg, x, x.dtype, (F, K), "dwg")
+    dwu, du_ptr, du_stride = _out_rows(dwu, x, x.dtype, (F, K), "dwu")
+    if du_stride != dw_stride:
+        raise ValueError("xnor_gated_bwd: dwg and dwu need the same row stride")
+    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_gated_bwd_workspace_bytes(M, F, K) if workspace is None else 0)
+    _ok(lib.xnor_gated_bwd(d_ptr, d_stride, x_ptr, kind, x_stride, g_w, u_w, w_stride, g_ptr, u_ptr, gu_stride, act, M, F, K, dx_ptr, dx_stride,
+                           dg_ptr, du_ptr, dw_stride, ws, ws_bytes, _stream()), "xnor_gated_bwd")
+    return dx, dwg, dwu

@@ -1,0 +1,174 @@
+// What the dense operators (8-bit and 16-bit products, layer norm, the gated block) share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <type_traits>
+
+#include "xnor_internal.hpp"
+
+namespace xnor {
+
+typedef _Float16 f16_t;
+typedef __bf16 bf16_t;
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kWave = 64;
+
+// 16 bytes of values as one load or store.  Any byte address will do: global accesses need no alignment on this target.
+template <class T>
+struct Chunk {
+    static constexpr int kCount = 16 / (int)sizeof(T);
+    T v[kCount];
+};
+
+// The chunk that starts `at` values into a row of `n`; values behind the row's end are zero.
+template <class T>
+__device__ inline Chunk<T> load_chunk(const T *row, int at, int n)
+{
+    Chunk<T> c;
+    if (at + Chunk<T>::kCount <= n) {
+        __builtin_memcpy(&c, row + at, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < Chunk<T>::kCount; ++i) c.v[i] = at + i < n ? row[at + i] : T(0);
+    }
+    return c;
+}
+
+// COUNT values to row[at ..], as far as the row goes.
+template <class T, int COUNT>
+__device__ inline void store_values(T *row, int at, int n, const T (&v)[COUNT])
+{
+    if (at + COUNT <= n) {
+        __builtin_memcpy(row + at, v, sizeof v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i)
+            if (at + i < n) row[at + i] = v[i];
+    }
+}
+
+__device__ inline float wave_sum(float v)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+// fmaxf drops a NaN; a row's largest magnitude keeps it.
+__device__ inline float max_nan(float a, float b) { return a > b || a != a ? a : b; }
+
+__device__ inline float wave_max_nan(float v)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v = max_nan(v, __shfl_xor(v, d));
+    return v;
+}
+
+// Rows whose largest magnitude is below this are quantised to zeros: 127 / max and max / 127 stay normal numbers.
+constexpr float kQuantFloor = 0x1p-100f;
+
+// The factor that takes a row to its levels, and the size of a level.  A row that holds a NaN or an infinity has neither: its
+// levels are 0 and its scale is NaN, so that whatever is computed from it is NaN.
+struct RowLevels {
+    float to, scale;
+};
+__device__ inline RowLevels row_levels(float top)
+{
+    if (top < kQuantFloor) return {0.f, 0.f};
+    if (!(top <= 3.402823466e38f)) return {0.f, __uint_as_float(0x7fc00000u)};
+    return {127.f / top, top / 127.f};
+}
+__device__ inline int8_t level_of(float x, const RowLevels &r)
+{
+    // (r.to 0: whatever x is, NaN and infinity among them, its level is 0)
+    return r.to == 0.f ? (int8_t)0 : (int8_t)(int)rintf(x * r.to);
+}
+
+// Activations of the gated block and their derivatives, in fp32.  kind: an xnor_act.
+template <int ACT>
+__device__ inline float act_value(float g)
+{
+    if constexpr (ACT == XNOR_ACT_SILU) return g / (1.f + expf(-g));
+    if constexpr (ACT == XNOR_ACT_GELU) return 0.5f * g * erfcf(g * -0.70710678118654752f);
+    return g > 0.f ? g : (g != g ? g : 0.f);
+}
+template <int ACT>
+__device__ inline float act_slope(float g)
+{
+    if constexpr (ACT == XNOR_ACT_SILU) {
+        const float s = 1.f / (1.f + expf(-g));
+        return s * (1.f + g * (1.f - s));
+    }
+    if constexpr (ACT == XNOR_ACT_GELU)
+        return 0.5f * erfcf(g * -0.70710678118654752f) + g * expf(-0.5f * g * g) * 0.39894228040143268f;
+    return g > 0.f ? 1.f : (g != g ? g : 0.f);
+}
+
+// One product of the dense operators: out[m][n] = sum_k a[m][k] b[n][k], both operands with the contraction along their rows.
+// Strides of a and b are in bytes, of outputs in values.
+struct DenseArgs {
+    const void *a;              // [M][K]
+    const void *b, *b2;         // [N][K]; b2: the gated block's second matrix
+    long long lda, ldb;
+    long long M;
+    int N, K;                   // K in values
+    void *out, *out2, *out3;    // gated: h, and g and u or NULL.  Plain: rows from `split` on go to out2
+    long long ldo, ldo2;
+    long long split, valid;     // plain: of the rows of either output the first `valid` are written
+    const float *a_scale, *b_scale, *b2_scale, *bias;
+    int act;
+    long long first;            // (set by the launchers: the launch's first token)
+};
+
+constexpr long long kMaxBlocks = 1 << 22;      // of a launch, for up to 1024 threads each: fewer than 2^32 threads
+
+hipError_t launch_dense(const DenseArgs &p, int type, hipStream_t st);                       // 16-bit: out = a b^T
+hipError_t launch_dense_gated(const DenseArgs &p, int type, hipStream_t st);                 // 16-bit
+hipError_t launch_dense_int8(const DenseArgs &p, int out_type, hipStream_t st);
+hipError_t launch_dense_int8_gated(const DenseArgs &p, int out_type, hipStream_t st);
+
+struct RowArgs {
+    const void *x;
+    long long rows;
+    int cols;
+    long long x_stride;
+    const void *gamma, *beta;
+    float eps;
+    void *y;
+    int8_t *q;
+    long long y_stride;          // of y or q
+    float *scale, *mean, *rstd;
+    long long first;             // (set by the launchers: the launch's first row)
+};
+hipError_t launch_quantize(const RowArgs &p, int x_type, hipStream_t st);
+hipError_t launch_layer_norm(const RowArgs &p, int x_type, int p_type, hipStream_t st);      // y or q
+struct NormBackArgs {
+    const void *dy, *x, *gamma;
+    long long rows;
+    int cols;
+    long long dy_stride, x_stride, dx_stride;
+    const float *mean, *rstd;
+    void *dx, *dgamma, *dbeta;
+    float *partial;              // workspace
+};
+size_t layer_norm_bwd_workspace(int x_type, long long rows, int cols);
+hipError_t launch_layer_norm_bwd(const NormBackArgs &p, int x_type, int p_type, hipStream_t st);
+
+struct GatedBackArgs {
+    const void *dh, *x, *wg, *wu, *g, *u;
+    long long dh_stride, x_stride, w_stride, gu_stride, dx_stride, dw_stride;
+    int act;
+    long long M;
+    int F, K;
+    void *dx, *dwg, *dwu;
+    void *workspace;
+};
+size_t gated_bwd_workspace(long long M, int F, int K);
+hipError_t launch_gated_bwd(const GatedBackArgs &p, int type, hipStream_t st);
+
+}  // namespace xnor

@@ -1,0 +1,388 @@
+// Operators on the rows of a matrix: layer norm forward (real or quantised output) and backward, and the quantisation of rows
+// to 8 bits.  All are bound by memory: a row is read once into registers, where its sums are formed, and written once.
+#include <algorithm>
+
+#include "dense_common.hpp"
+
+namespace xnor {
+namespace {
+
+enum RowOutput { kReal, kLevels, kQuantize };       // layer norm; layer norm, quantised; quantisation alone
+
+constexpr int kBlock = 256;
+
+template <class P>
+__device__ inline float param(const P *p, int at, float none) { return p ? (float)p[at] : none; }
+
+// Sum or largest value over the THREADS threads of a row (a wave, or the whole workgroup).  `slots` is not reused before
+// another barrier has passed: callers alternate between two.
+template <int THREADS, class Op>
+__device__ inline float row_reduce(float v, float *slots, Op op)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v = op(v, __shfl_xor(v, d));
+    if constexpr (THREADS == kWave) return v;
+    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = slots[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / kWave; ++i) v = op(v, slots[i]);
+    return v;
+}
+
+// A row by THREADS threads, NV chunks of 16 bytes each in registers (NV = 0: read again for every sum, rows of any length).
+template <class T, class P, int OUT, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < kBlock ? kBlock : THREADS) void row_kernel(const RowArgs p)
+{
+    constexpr int V = Chunk<T>::kCount, ROWS = THREADS < kBlock ? kBlock / THREADS : 1;
+    __shared__ float slots[3][16];
+    const int t = threadIdx.x % THREADS;
+    const long long row = p.first + (long long)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    if (row >= p.rows) return;                  // (rows share no barrier where a workgroup has several)
+    const T *x = (const T *)p.x + row * p.x_stride;
+
+    Chunk<T> held[NV ? NV : 1];
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) held[i] = load_chunk(x, (t + i * THREADS) * V, p.cols);
+    }
+    auto each = [&](auto f) __attribute__((always_inline)) {        // f(column of the chunk's first value, chunk)
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if ((t + i * THREADS) * V < p.cols) f((t + i * THREADS) * V, held[i]);
+        } else {
+            for (int at = t * V; at < p.cols; at += THREADS * V) f(at, load_chunk(x, at, p.cols));
+        }
+    };
+    auto sum = [](float a, float b) { return a + b; };
+
+    float mean = 0.f, rstd = 1.f;
+    if constexpr (OUT != kQuantize) {
+        float s = 0.f;
+        each([&](int, const Chunk<T> &c) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) s += (float)c.v[k];
+        });
+        mean = row_reduce<THREADS>(s, slots[0], sum) / (float)p.cols;
+        float d2 = 0.f;         // about the mean: no difference of large squares
+        each([&](int at, const Chunk<T> &c) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float d = (float)c.v[k] - mean;
+                d2 += at + k < p.cols ? d * d : 0.f;
+            }
+        });
+        rstd = 1.f / sqrtf(row_reduce<THREADS>(d2, slots[1], sum) / (float)p.cols + p.eps);
+        if (t == 0) {
+            if (p.mean) p.mean[row] = mean;
+            if (p.rstd) p.rstd[row] = rstd;
+        }
+    }
+    auto value = [&](int at, const Chunk<T> &c, int k) __attribute__((always_inline)) -> float {
+        if constexpr (OUT == kQuantize) return (float)c.v[k];
+        if (at + k >= p.cols) return 0.f;
+        return ((float)c.v[k] - mean) * rstd * param((const P *)p.gamma, at + k, 1.f) + param((const P *)p.beta, at + k, 0.f);
+    };
+    if constexpr (OUT == kReal) {
+        T *y = (T *)p.y + row * p.y_stride;
+        each([&](int at, const Chunk<T> &c) {
+            T out[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) out[k] = (T)value(at, c, k);
+            store_values(y, at, p.cols, out);
+        });
+    } else {
+        float top = 0.f;
+        each([&](int at, const Chunk<T> &c) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) top = max_nan(top, fabsf(value(at, c, k)));
+        });
+        top = row_reduce<THREADS>(top, slots[2], max_nan);
+        const RowLevels levels = row_levels(top);
+        if (t == 0) p.scale[row] = levels.scale;
+        int8_t *q = p.q + row * p.y_stride;
+        each([&](int at, const Chunk<T> &c) {
+            int8_t out[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) out[k] = level_of(value(at, c, k), levels);
+            store_values(q, at, p.cols, out);
+        });
+    }
+}
+
+template <class T, class P, int OUT>
+hipError_t launch_rows(const RowArgs &p, hipStream_t st)
+{
+    constexpr int V = Chunk<T>::kCount;
+    if (p.rows == 0) return hipSuccess;
+    const int chunks = ceil_div(p.cols, V);
+    auto go = [&](auto threads, auto nv) {
+        constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
+        constexpr int ROWS = THREADS < kBlock ? kBlock / THREADS : 1;
+        for (long long row = 0; row < p.rows; row += kMaxBlocks * ROWS) {
+            RowArgs q = p;
+            q.first = row;
+            q.rows = std::min(p.rows, row + kMaxBlocks * ROWS);
+            row_kernel<T, P, OUT, THREADS, NV><<<dim3((unsigned)((q.rows - row + ROWS - 1) / ROWS)), dim3(THREADS < kBlock ? kBlock : THREADS), 0, st>>>(q);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    };
+    using std::integral_constant;
+    if (chunks <= 64) return go(integral_constant<int, 64>(), integral_constant<int, 1>());
+    if (chunks <= 128) return go(integral_constant<int, 64>(), integral_constant<int, 2>());
+    if (chunks <= 256) return go(integral_constant<int, 256>(), integral_constant<int, 1>());
+    if (chunks <= 512) return go(integral_constant<int, 256>(), integral_constant<int, 2>());
+    if (chunks <= 1024) return go(integral_constant<int, 256>(), integral_constant<int, 4>());
+    if (chunks <= 4096) return go(integral_constant<int, 1024>(), integral_constant<int, 4>());
+    return go(integral_constant<int, 1024>(), integral_constant<int, 0>());
+}
+
+// ------------------------------------------------------------------------------------------------
+// Backward.  p = dy gamma, xh = (x - mean) rstd: dx = rstd (p - mean(p) - xh mean(p xh)), dgamma = sum over rows of dy xh,
+// dbeta = sum over rows of dy.  A workgroup takes every gridDim.x-th row and keeps its columns' part of the two sums in
+// registers; a second launch adds the parts in a fixed order.
+// ------------------------------------------------------------------------------------------------
+template <class T, class P, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS < kBlock ? kBlock : THREADS) void norm_back_kernel(const NormBackArgs p)
+{
+    constexpr int V = Chunk<T>::kCount, ROWS = THREADS < kBlock ? kBlock / THREADS : 1;
+    __shared__ float slots[2][2][16];
+    const int t = threadIdx.x % THREADS;
+    const long long first = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS, step = (long long)gridDim.x * ROWS;
+    float sg[NV][V] = {}, sb[NV][V] = {};
+    int turn = 0;
+    for (long long row = first; row < p.rows; row += step, turn ^= 1) {
+        const T *x = (const T *)p.x + row * p.x_stride, *dy = (const T *)p.dy + row * p.dy_stride;
+        Chunk<T> cx[NV], cd[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            cx[i] = load_chunk(x, (t + i * THREADS) * V, p.cols);
+            cd[i] = load_chunk(dy, (t + i * THREADS) * V, p.cols);
+        }
+        const float mean = p.mean[row], rstd = p.rstd[row];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const int at = (t + i * THREADS) * V + k;
+                if (at < p.cols) {
+                    const float xh = ((float)cx[i].v[k] - mean) * rstd, d = (float)cd[i].v[k];
+                    const float pv = d * param((const P *)p.gamma, at, 1.f);
+                    s1 += pv;
+                    s2 += pv * xh;
+                    sg[i][k] += d * xh;
+                    sb[i][k] += d;
+                }
+            }
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        if constexpr (THREADS > kWave) {
+            if ((threadIdx.x & 63) == 0) {
+                slots[turn][0][threadIdx.x >> 6] = s1;
+                slots[turn][1][threadIdx.x >> 6] = s2;
+            }
+            __syncthreads();
+            s1 = s2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < THREADS / kWave; ++i) {
+                s1 += slots[turn][0][i];
+                s2 += slots[turn][1][i];
+            }
+        }
+        s1 /= (float)p.cols;
+        s2 /= (float)p.cols;
+        T *dx = (T *)p.dx + row * p.dx_stride;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = (t + i * THREADS) * V;
+            if (at >= p.cols) continue;
+            T out[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float xh = ((float)cx[i].v[k] - mean) * rstd;
+                const float pv = (float)cd[i].v[k] * (at + k < p.cols ? param((const P *)p.gamma, at + k, 1.f) : 0.f);
+                out[k] = (T)(rstd * (pv - s1 - xh * s2));
+            }
+            store_values(dx, at, p.cols, out);
+        }
+    }
+    if (!p.partial) return;
+    float *to = p.partial + ((long long)blockIdx.x * ROWS + threadIdx.x / THREADS) * 2 * p.cols;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int at = (t + i * THREADS) * V;
+        if (at >= p.cols) continue;
+        store_values(to, at, p.cols, sg[i]);
+        store_values(to + p.cols, at, p.cols, sb[i]);
+    }
+}
+
+// Rows that no workgroup holds in registers: dx from two readings, the parameters' sums by column.
+template <class T, class P>
+__global__ __launch_bounds__(1024) void norm_back_long_kernel(const NormBackArgs p)
+{
+    constexpr int V = Chunk<T>::kCount, THREADS = 1024;
+    __shared__ float slots[2][16];
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    __syncthreads();        // (slots: the last row's sums have been read)
+    const T *x = (const T *)p.x + row * p.x_stride, *dy = (const T *)p.dy + row * p.dy_stride;
+    const float mean = p.mean[row], rstd = p.rstd[row];
+    auto sum = [](float a, float b) { return a + b; };
+    float s1 = 0.f, s2 = 0.f;
+    for (int at = threadIdx.x * V; at < p.cols; at += THREADS * V) {
+        const Chunk<T> cx = load_chunk(x, at, p.cols), cd = load_chunk(dy, at, p.cols);
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (at + k < p.cols) {
+                const float pv = (float)cd.v[k] * param((const P *)p.gamma, at + k, 1.f);
+                s1 += pv;
+                s2 += pv * (((float)cx.v[k] - mean) * rstd);
+            }
+    }
+    s1 = row_reduce<THREADS>(s1, slots[0], sum) / (float)p.cols;
+    s2 = row_reduce<THREADS>(s2, slots[1], sum) / (float)p.cols;
+    T *dx = (T *)p.dx + row * p.dx_stride;
+    for (int at = threadIdx.x * V; at < p.cols; at += THREADS * V) {
+        const Chunk<T> cx = load_chunk(x, at, p.cols), cd = load_chunk(dy, at, p.cols);
+        T out[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float pv = at + k < p.cols ? (float)cd.v[k] * param((const P *)p.gamma, at + k, 1.f) : 0.f;
+            out[k] = (T)(rstd * (pv - s1 - ((float)cx.v[k] - mean) * rstd * s2));
+        }
+        store_values(dx, at, p.cols, out);
+    }
+    }
+}
+
+// Part b of the sums over rows b, b + parts, ...: one column a thread.
+template <class T>
+__global__ __launch_bounds__(kBlock) void norm_back_columns_kernel(const NormBackArgs p, int parts)
+{
+    const int col = blockIdx.x * kBlock + threadIdx.x;
+    if (col >= p.cols) return;
+    float g = 0.f, b = 0.f;
+    for (long long row = blockIdx.y; row < p.rows; row += parts) {
+        const float d = (float)((const T *)p.dy)[row * p.dy_stride + col];
+        g += d * (((float)((const T *)p.x)[row * p.x_stride + col] - p.mean[row]) * p.rstd[row]);
+        b += d;
+    }
+    float *to = p.partial + (long long)blockIdx.y * 2 * p.cols + col;
+    to[0] = g;
+    to[p.cols] = b;
+}
+
+// dgamma and dbeta from `parts` parts [part][gamma, beta][cols]: 16 columns a workgroup, 16 threads a column.
+template <class P>
+__global__ __launch_bounds__(kBlock) void norm_back_parts_kernel(const float *partial, int parts, int cols, P *dgamma, P *dbeta)
+{
+    __shared__ float lds[16][17];
+    const int c = threadIdx.x & 15, s = threadIdx.x >> 4;
+    const long long col = (long long)blockIdx.x * 16 + c;          // over both vectors
+    float v = 0.f;
+    if (col < 2LL * cols)
+        for (int i = s; i < parts; i += 16) v += partial[(long long)i * 2 * cols + col];
+    lds[s][c] = v;
+    __syncthreads();
+    if (s == 0 && col < 2LL * cols) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) v += lds[i][c];
+        if (col < cols) dgamma[col] = (P)v;
+        else dbeta[col - cols] = (P)v;
+    }
+}
+
+struct BackPlan {
+    int threads, nv;            // nv 0: the long rows' kernels
+    int blocks, parts;
+};
+
+BackPlan back_plan(int x_type, long long rows, int cols)
+{
+    const int chunks = ceil_div(cols, x_type == XNOR_TYPE_FP32 ? 4 : 8);
+    BackPlan b{};
+    if (chunks <= 128) b.threads = 64, b.nv = chunks <= 64 ? 1 : 2;
+    else if (chunks <= 1024) b.threads = 256, b.nv = chunks <= 256 ? 1 : chunks <= 512 ? 2 : 4;
+    else if (chunks <= 4096) b.threads = 1024, b.nv = 4;
+    if (b.nv == 0) {
+        b.blocks = (int)std::min(rows, kMaxBlocks);
+        b.parts = (int)std::min<long long>(rows, 64);
+        return b;
+    }
+    const int rows_a_block = b.threads < kBlock ? kBlock / b.threads : 1;
+    const long long want = std::max<long long>(1, std::min<long long>(2 * kPlanUnits, (rows + rows_a_block * 4 - 1) / (rows_a_block * 4)));
+    b.blocks = (int)want;
+    b.parts = b.blocks * rows_a_block;
+    return b;
+}
+
+template <class T, class P>
+hipError_t back(const NormBackArgs &p, int x_type, hipStream_t st)
+{
+    const BackPlan b = back_plan(x_type, p.rows, p.cols);
+    int parts = p.rows ? b.parts : 0;
+    if (p.rows > 0) {
+        using std::integral_constant;
+        auto go = [&](auto threads, auto nv) {
+            constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
+            norm_back_kernel<T, P, THREADS, NV><<<dim3((unsigned)b.blocks), dim3(THREADS < kBlock ? kBlock : THREADS), 0, st>>>(p);
+        };
+        if (b.nv == 0) {
+            norm_back_long_kernel<T, P><<<dim3((unsigned)b.blocks), dim3(1024), 0, st>>>(p);
+            if (p.partial) norm_back_columns_kernel<T><<<dim3(ceil_div(p.cols, kBlock), parts), dim3(kBlock), 0, st>>>(p, parts);
+        } else if (b.threads == 64) {
+            b.nv == 1 ? go(integral_constant<int, 64>(), integral_constant<int, 1>()) : go(integral_constant<int, 64>(), integral_constant<int, 2>());
+        } else if (b.threads == 256) {
+            b.nv == 1   ? go(integral_constant<int, 256>(), integral_constant<int, 1>())
+            : b.nv == 2 ? go(integral_constant<int, 256>(), integral_constant<int, 2>()) : go(integral_constant<int, 256>(), integral_constant<int, 4>());
+        } else {
+            go(integral_constant<int, 1024>(), integral_constant<int, 4>());
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (p.partial) {
+        norm_back_parts_kernel<P><<<dim3(ceil_div(2LL * p.cols, 16)), dim3(kBlock), 0, st>>>(p.partial, parts, p.cols, (P *)p.dgamma, (P *)p.dbeta);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const RowArgs &p, int x_type, hipStream_t st)
+{
+    return x_type == XNOR_TYPE_FP32  ? launch_rows<float, float, kQuantize>(p, st)
+           : x_type == XNOR_TYPE_F16 ? launch_rows<f16_t, float, kQuantize>(p, st) : launch_rows<bf16_t, float, kQuantize>(p, st);
+}
+
+template <int OUT>
+static hipError_t norm_forward(const RowArgs &p, int x_type, int p_type, hipStream_t st)
+{
+    if (x_type == XNOR_TYPE_FP32) return launch_rows<float, float, OUT>(p, st);
+    if (x_type == XNOR_TYPE_F16) return p_type == XNOR_TYPE_FP32 ? launch_rows<f16_t, float, OUT>(p, st) : launch_rows<f16_t, f16_t, OUT>(p, st);
+    return p_type == XNOR_TYPE_FP32 ? launch_rows<bf16_t, float, OUT>(p, st) : launch_rows<bf16_t, bf16_t, OUT>(p, st);
+}
+
+hipError_t launch_layer_norm(const RowArgs &p, int x_type, int p_type, hipStream_t st)
+{
+    return p.q ? norm_forward<kLevels>(p, x_type, p_type, st) : norm_forward<kReal>(p, x_type, p_type, st);
+}
+
+size_t layer_norm_bwd_workspace(int x_type, long long rows, int cols)
+{
+    return (size_t)back_plan(x_type, rows, cols).parts * 2 * (size_t)cols * sizeof(float);
+}
+
+hipError_t launch_layer_norm_bwd(const NormBackArgs &p, int x_type, int p_type, hipStream_t st)
+{
+    if (x_type == XNOR_TYPE_FP32) return back<float, float>(p, x_type, st);
+    if (x_type == XNOR_TYPE_F16) return p_type == XNOR_TYPE_FP32 ? back<f16_t, float>(p, x_type, st) : back<f16_t, f16_t>(p, x_type, st);
+    return p_type == XNOR_TYPE_FP32 ? back<bf16_t, float>(p, x_type, st) : back<bf16_t, bf16_t>(p, x_type, st);
+}
+
+}  // namespace xnor

@@ -7,16 +7,18 @@
 
 #include "xnor_internal.hpp"
 
-namespace {
+static thread_local char g_hip_err[256] = "";
 
-thread_local char g_hip_err[256] = "";
-
-int hip_status(hipError_t e)
+int xnor::hip_status(hipError_t e)
 {
     if (e == hipSuccess) return XNOR_OK;
     snprintf(g_hip_err, sizeof g_hip_err, "%s: %s", hipGetErrorName(e), hipGetErrorString(e));
     return XNOR_E_HIP;
 }
+
+namespace {
+
+using xnor::hip_status;
 
 constexpr long long kMaxIndex = 0x7fffffffLL;
 

@@ -80,6 +80,9 @@ inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 inline uint32_t reciprocal(unsigned long long d) { return d == 1 ? 0u : (uint32_t)(((1ULL << 32) + d - 1) / d); }
 __device__ inline uint32_t quot(uint32_t n, uint32_t inv) { return inv == 0 ? n : __umulhi(n, inv); }
 
+// A call's status for what the runtime said; the text of a failure stays with the thread.
+int hip_status(hipError_t e);
+
 // Launchers: enqueue on `st`, return the launch status.  Arguments are already validated.
 hipError_t launch_binarize_pack(const float *x, int N, int C, int H, int W, uint32_t *packed,
                                 hipStream_t st);
