@@ -124,6 +124,12 @@ int xnor_int8_linear(const void *x, int x_type, long long x_stride, const int8_t
     size_t need;
     if (const int rc = xnor_int8_linear_workspace_bytes(M, K, &need)) return rc;
     if (workspace_bytes < need) return XNOR_E_WORKSPACE;
+    if (M > 0 && dense_few_real_supports(M, K)) {
+        DenseArgs d{};
+        d.a = x, d.lda = x_stride * xs, d.b = w, d.ldb = w_stride, d.b_scale = w_scale, d.bias = bias;
+        d.M = M, d.N = N, d.K = K, d.out = out, d.ldo = out_stride;
+        return hip_status(launch_dense_few_real(d, x_type, out_type, (hipStream_t)stream));
+    }
     int8_t *q = (int8_t *)workspace;
     const long long q_stride = (long long)q_stride_of(K);
     float *scale = (float *)(q + M * q_stride);

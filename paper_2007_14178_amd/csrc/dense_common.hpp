@@ -52,22 +52,48 @@ __device__ inline void store_values(T *row, int at, int n, const T (&v)[COUNT])
     }
 }
 
-__device__ inline float wave_sum(float v)
+// V parameters from `at` on as fp32; `none` where there are no parameters, and anything behind the end.
+template <int V, class P>
+__device__ inline void load_params(const P *p, int at, int n, float none, float (&to)[V])
 {
+    P raw[V];
+    if (p && at + V <= n) {
+        __builtin_memcpy(raw, p + at, sizeof raw);
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+        for (int k = 0; k < V; ++k) to[k] = (float)raw[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) to[k] = p && at + k < n ? (float)p[at + k] : none;
+    }
 }
+
+// v of the lane that CTRL names, within 16 lanes.
+template <int CTRL>
+__device__ inline float dpp(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// Over a wave, to all lanes: the other of each pair, pair of pairs, half and whole row of 16 lanes by DPP, then two exchanges.
+template <class Op>
+__device__ inline float wave_reduce(float v, Op op)
+{
+    v = op(v, dpp<0xb1>(v));
+    v = op(v, dpp<0x4e>(v));
+    v = op(v, dpp<0x141>(v));
+    v = op(v, dpp<0x140>(v));
+    v = op(v, __shfl_xor(v, 16));
+    return op(v, __shfl_xor(v, 32));
+}
+
+struct Sum {
+    __device__ float operator()(float a, float b) const { return a + b; }
+};
 
 // fmaxf drops a NaN; a row's largest magnitude keeps it.
-__device__ inline float max_nan(float a, float b) { return a > b || a != a ? a : b; }
-
-__device__ inline float wave_max_nan(float v)
-{
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v = max_nan(v, __shfl_xor(v, d));
-    return v;
-}
+struct MaxNan {
+    __device__ float operator()(float a, float b) const { return a > b || a != a ? a : b; }
+};
 
 // Rows whose largest magnitude is below this are quantised to zeros: 127 / max and max / 127 stay normal numbers.
 constexpr float kQuantFloor = 0x1p-100f;
@@ -131,6 +157,9 @@ hipError_t launch_dense(const DenseArgs &p, int type, hipStream_t st);          
 hipError_t launch_dense_gated(const DenseArgs &p, int type, hipStream_t st);                 // 16-bit
 hipError_t launch_dense_int8(const DenseArgs &p, int out_type, hipStream_t st);
 hipError_t launch_dense_int8_gated(const DenseArgs &p, int out_type, hipStream_t st);
+// The 8-bit product of real tokens, a and lda theirs, quantised in the kernel; where it takes them.
+bool dense_few_real_supports(long long M, int K);
+hipError_t launch_dense_few_real(const DenseArgs &p, int x_type, int out_type, hipStream_t st);
 
 struct RowArgs {
     const void *x;
@@ -143,7 +172,6 @@ struct RowArgs {
     int8_t *q;
     long long y_stride;          // of y or q
     float *scale, *mean, *rstd;
-    long long first;             // (set by the launchers: the launch's first row)
 };
 hipError_t launch_quantize(const RowArgs &p, int x_type, hipStream_t st);
 hipError_t launch_layer_norm(const RowArgs &p, int x_type, int p_type, hipStream_t st);      // y or q

@@ -1,0 +1,194 @@
+// Products for few tokens (a decoding step): b is read once, by as many waves as there are, and that is what they take.
+//
+// A workgroup has 16 rows of b (of each matrix in the gated block), its eight waves an eighth of the contraction each, whose sums are
+// added in LDS.  The tokens are columns of the matrix instruction: up to 16 cost what one costs.
+#include <type_traits>
+
+#include "dense_tile.hpp"
+
+namespace xnor {
+namespace {
+
+constexpr int kWaves = 8, kThreads = kWaves * kWave;
+constexpr int kRealTokens = 2, kRealCols = 8192;        // real tokens that are quantised here: how many, and how long
+
+// X: the type of real tokens, quantised by every workgroup for itself; void: a holds T.
+template <class T, class O, int EPI, int TT, class X>
+__global__ __launch_bounds__(kThreads) void few_kernel(const DenseArgs p)
+{
+    constexpr bool GATED = EPI == kGated || EPI == kInt8Gated, REAL = !std::is_void<X>::value;
+    constexpr int MATS = GATED ? 2 : 1, U = 4;
+    typedef Mat<T> Mul;
+    typedef typename Mul::acc Acc;
+    __shared__ Acc sums[kWaves][MATS][TT][kWave];
+    __shared__ float tops[REAL ? kRealTokens : 1][kWaves];
+    extern __shared__ __align__(16) int8_t levels[];        // real tokens: [M][whole steps]
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16;
+    const int steps = (int)(((long long)p.K * (int)sizeof(T) + kStep - 1) / kStep), share = (steps + kWaves - 1) / kWaves;
+    const int from = wave * share, to = min(steps, from + share);
+    const int held_bytes = steps * kStep;
+
+    const long long row = min(n0 + r, p.N - 1);
+    const T *b[MATS];
+    b[0] = (const T *)((const char *)p.b + row * p.ldb);
+    if constexpr (GATED) b[1] = (const T *)((const char *)p.b2 + row * p.ldb);
+    const T *a[TT];
+#pragma unroll
+    for (int j = 0; j < TT; ++j) {
+        const long long m = min((long long)j * 16 + r, p.M - 1);
+        a[j] = (const T *)((const char *)p.a + m * p.lda);
+    }
+
+    i32x4 vb[MATS][U][2];
+    auto load_b = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < MATS; ++k)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int at = ((s + u) * kStep + g * 32 + i * 16) / (int)sizeof(T);
+                    vb[k][u][i] = i32x4{};
+                    if (s + u < to) vb[k][u][i] = __builtin_bit_cast(i32x4, load_chunk(b[k], at, p.K));
+                }
+    };
+
+    float scale[TT] = {};
+    if constexpr (REAL) {
+        // the tokens first, b's first rows on their way while the tokens are quantised
+        constexpr int XV = 16 / (int)sizeof(X), kRealChunks = kRealCols / (kThreads * XV);
+        Chunk<X> held[kRealTokens][kRealChunks];
+#pragma unroll
+        for (int m = 0; m < kRealTokens; ++m)
+            if (m < p.M)
+#pragma unroll
+                for (int c = 0; c < kRealChunks; ++c)
+                    held[m][c] = load_chunk((const X *)((const char *)p.a + m * p.lda), (t + c * kThreads) * XV, p.K);
+        load_b(from);
+#pragma unroll
+        for (int m = 0; m < kRealTokens; ++m)
+            if (m < p.M) {
+                float top = 0.f;
+#pragma unroll
+                for (int c = 0; c < kRealChunks; ++c)
+#pragma unroll
+                    for (int k = 0; k < XV; ++k) top = MaxNan()(fabsf((float)held[m][c].v[k]), top);
+                top = wave_reduce(top, MaxNan());
+                if (lane == 0) tops[m][wave] = top;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < kRealTokens; ++m)
+            if (m < p.M) {
+                float top = tops[m][0];
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) top = MaxNan()(tops[m][w], top);
+                const RowLevels l = row_levels(top);
+                if (r == m) scale[0] = l.scale;
+#pragma unroll
+                for (int c = 0; c < kRealChunks; ++c) {
+                    const int at = (t + c * kThreads) * XV;
+                    int8_t q[XV];
+#pragma unroll
+                    for (int k = 0; k < XV; ++k) q[k] = level_of((float)held[m][c].v[k], l);
+                    if (at < held_bytes) __builtin_memcpy(levels + m * held_bytes + at, q, XV);        // (zeros behind the token's end)
+                }
+            }
+        __syncthreads();
+    } else {
+        load_b(from);
+#pragma unroll
+        for (int j = 0; j < TT; ++j) {
+            const long long m = j * 16 + r;
+            scale[j] = p.a_scale && m < p.M ? p.a_scale[m] : 1.f;
+        }
+    }
+
+    Acc acc[MATS][TT] = {};
+    for (int s = from; s < to; s += U) {
+        if (s > from) load_b(s);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s + u >= to) break;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int at = (s + u) * kStep + g * 32 + i * 16;
+#pragma unroll
+                for (int j = 0; j < TT; ++j) {
+                    i32x4 va;
+                    if constexpr (REAL) va = *(const i32x4 *)(levels + min(r, (int)p.M - 1) * held_bytes + at);
+                    else va = __builtin_bit_cast(i32x4, load_chunk(a[j], at / (int)sizeof(T), p.K));
+#pragma unroll
+                    for (int k = 0; k < MATS; ++k) acc[k][j] = Mul::mul(vb[k][u][i], va, acc[k][j]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < MATS; ++k)
+#pragma unroll
+        for (int j = 0; j < TT; ++j) sums[wave][k][j][lane] = acc[k][j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TT; ++j) {
+        const long long m = j * 16 + r;
+        const int n = n0 + g * 4;
+        if (wave != j % kWaves || m >= p.M || n >= p.N) continue;       // (a wave a tile of tokens)
+        Acc v[MATS];
+#pragma unroll
+        for (int k = 0; k < MATS; ++k) {
+            v[k] = sums[0][k][j][lane];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v[k] += sums[w][k][j][lane];
+        }
+        finish<T, O, EPI>(p, m, scale[j], n, v[0], v[MATS - 1]);
+    }
+}
+
+}  // namespace
+
+template <class T, class O, int EPI>
+hipError_t launch_few(const DenseArgs &p, hipStream_t st)
+{
+    const dim3 grid((unsigned)ceil_div(p.N, 16));
+    if (p.M <= 16) few_kernel<T, O, EPI, 1, void><<<grid, dim3(kThreads), 0, st>>>(p);
+    else if (p.M <= 32) few_kernel<T, O, EPI, 2, void><<<grid, dim3(kThreads), 0, st>>>(p);
+    else few_kernel<T, O, EPI, 4, void><<<grid, dim3(kThreads), 0, st>>>(p);
+    return hipGetLastError();
+}
+
+template hipError_t launch_few<int8_t, float, kInt8>(const DenseArgs &, hipStream_t);
+template hipError_t launch_few<int8_t, f16_t, kInt8>(const DenseArgs &, hipStream_t);
+template hipError_t launch_few<int8_t, bf16_t, kInt8>(const DenseArgs &, hipStream_t);
+template hipError_t launch_few<int8_t, float, kInt8Gated>(const DenseArgs &, hipStream_t);
+template hipError_t launch_few<int8_t, f16_t, kInt8Gated>(const DenseArgs &, hipStream_t);
+template hipError_t launch_few<int8_t, bf16_t, kInt8Gated>(const DenseArgs &, hipStream_t);
+template hipError_t launch_few<f16_t, f16_t, kGated>(const DenseArgs &, hipStream_t);
+template hipError_t launch_few<bf16_t, bf16_t, kGated>(const DenseArgs &, hipStream_t);
+template hipError_t launch_few<f16_t, f16_t, kPlain>(const DenseArgs &, hipStream_t);
+template hipError_t launch_few<bf16_t, bf16_t, kPlain>(const DenseArgs &, hipStream_t);
+
+bool dense_few_real_supports(long long M, int K)
+{
+    return M <= kRealTokens && K <= kRealCols;
+}
+
+template <class X>
+static hipError_t few_real(const DenseArgs &p, int out_type, hipStream_t st)
+{
+    const dim3 grid((unsigned)ceil_div(p.N, 16));
+    const size_t lds = (size_t)p.M * ceil_div(p.K, kStep) * kStep;
+    if (out_type == XNOR_TYPE_FP32) few_kernel<int8_t, float, kInt8, 1, X><<<grid, dim3(kThreads), lds, st>>>(p);
+    else if (out_type == XNOR_TYPE_F16) few_kernel<int8_t, f16_t, kInt8, 1, X><<<grid, dim3(kThreads), lds, st>>>(p);
+    else few_kernel<int8_t, bf16_t, kInt8, 1, X><<<grid, dim3(kThreads), lds, st>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t launch_dense_few_real(const DenseArgs &p, int x_type, int out_type, hipStream_t st)
+{
+    return x_type == XNOR_TYPE_FP32 ? few_real<float>(p, out_type, st)
+           : x_type == XNOR_TYPE_F16 ? few_real<f16_t>(p, out_type, st) : few_real<bf16_t>(p, out_type, st);
+}
+
+}  // namespace xnor

@@ -1,0 +1,99 @@
+// How the products' kernels see their operands and finish their outputs.
+#pragma once
+
+#include "dense_common.hpp"
+
+namespace xnor {
+
+enum Epilogue { kPlain, kGated, kInt8, kInt8Gated };
+
+template <class T> struct Mat;
+template <> struct Mat<int8_t> {
+    typedef i32x4 acc;
+    static __device__ acc mul(i32x4 a, i32x4 b, acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+};
+template <> struct Mat<f16_t> {
+    typedef f32x4 acc;
+    static __device__ acc mul(i32x4 a, i32x4 b, acc c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mat<bf16_t> {
+    typedef f32x4 acc;
+    static __device__ acc mul(i32x4 a, i32x4 b, acc c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+
+constexpr int kStep = 128;      // bytes of a row that are taken together
+
+// Row r of a tile's b operand, whose first row stands for output n0: in the gated block 16 rows of the first matrix and the 16 of
+// the second for the same outputs take turns.
+template <bool GATED>
+__device__ inline const char *b_row(const DenseArgs &p, int n0, int r)
+{
+    if (!GATED) return (const char *)p.b + (long long)min(n0 + r, p.N - 1) * p.ldb;
+    const int n = min(n0 + (r >> 5) * 16 + (r & 15), p.N - 1);
+    return (const char *)(r & 16 ? p.b2 : p.b) + n * p.ldb;
+}
+
+// Four consecutive outputs n .. n+3 of token m.  Every value is formed in fp32 and rounded once, where it is stored.
+// s: the token's scale (8-bit operands).
+template <class T, class O, int EPI, class Acc>
+__device__ inline void finish(const DenseArgs &p, long long m, float s, int n, const Acc &v, const Acc &w)
+{
+    O out[4];
+    if constexpr (EPI == kInt8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = min(n + i, p.N - 1);
+            const float y = (float)v[i] * (s * p.b_scale[at]);
+            out[i] = (O)(p.bias ? y + p.bias[at] : y);
+        }
+        store_values((O *)p.out + m * p.ldo, n, p.N, out);
+    } else if constexpr (EPI == kPlain) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = (O)v[i];
+        const bool second = m >= p.split;
+        const long long r = second ? m - p.split : m;
+        if (r < p.valid) store_values((O *)(second ? p.out2 : p.out) + r * p.ldo, n, p.N, out);
+    } else {
+        float g[4], u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            g[i] = (float)v[i];
+            u[i] = (float)w[i];
+            if constexpr (EPI == kInt8Gated) {
+                const int at = min(n + i, p.N - 1);
+                g[i] *= s * p.b_scale[at];
+                u[i] *= s * p.b2_scale[at];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = p.act == XNOR_ACT_SILU ? act_value<XNOR_ACT_SILU>(g[i])
+                            : p.act == XNOR_ACT_GELU ? act_value<XNOR_ACT_GELU>(g[i]) : act_value<XNOR_ACT_RELU>(g[i]);
+            out[i] = (O)(a * u[i]);
+        }
+        store_values((O *)p.out + m * p.ldo, n, p.N, out);
+        if constexpr (EPI == kGated) {
+            if (p.out2) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[i] = (O)g[i];
+                store_values((O *)p.out2 + m * p.ldo2, n, p.N, out);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) out[i] = (O)u[i];
+                store_values((O *)p.out3 + m * p.ldo2, n, p.N, out);
+            }
+        }
+    }
+}
+
+// Tokens up to which a product goes to the kernel for few tokens, and its launcher (EPI an Epilogue).
+constexpr int kFewTokens = 64;
+template <class T, class O, int EPI>
+hipError_t launch_few(const DenseArgs &p, hipStream_t st);
+
+}  // namespace xnor

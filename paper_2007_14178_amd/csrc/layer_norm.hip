@@ -10,17 +10,13 @@ namespace {
 enum RowOutput { kReal, kLevels, kQuantize };       // layer norm; layer norm, quantised; quantisation alone
 
 constexpr int kBlock = 256;
+constexpr int kRowBlocks = 8;           // workgroups a compute unit, at most
 
-template <class P>
-__device__ inline float param(const P *p, int at, float none) { return p ? (float)p[at] : none; }
-
-// Sum or largest value over the THREADS threads of a row (a wave, or the whole workgroup).  `slots` is not reused before
-// another barrier has passed: callers alternate between two.
+// Over the THREADS threads of a row (a wave, or the whole workgroup).  `slots` is not written again before another barrier has passed.
 template <int THREADS, class Op>
 __device__ inline float row_reduce(float v, float *slots, Op op)
 {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v = op(v, __shfl_xor(v, d));
+    v = wave_reduce(v, op);
     if constexpr (THREADS == kWave) return v;
     if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -30,84 +26,114 @@ __device__ inline float row_reduce(float v, float *slots, Op op)
     return v;
 }
 
-// A row by THREADS threads, NV chunks of 16 bytes each in registers (NV = 0: read again for every sum, rows of any length).
+constexpr int block_of(int threads) { return threads < kBlock ? kBlock : threads; }
+
+// Rows by THREADS threads each, NV chunks of 16 bytes of a row in a thread's registers, and with them the parameters of its
+// columns, which are read once for all of a workgroup's rows; the next row is on its way while one is worked on.  (NV = 0: rows of any
+// length, read again for every sum.)
 template <class T, class P, int OUT, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS < kBlock ? kBlock : THREADS) void row_kernel(const RowArgs p)
+__global__ __launch_bounds__(block_of(THREADS)) void row_kernel(const RowArgs p)
 {
-    constexpr int V = Chunk<T>::kCount, ROWS = THREADS < kBlock ? kBlock / THREADS : 1;
-    __shared__ float slots[3][16];
+    constexpr int V = Chunk<T>::kCount, ROWS = block_of(THREADS) / THREADS, N = NV ? NV : 1;
+    __shared__ float slots[2][3][16];
     const int t = threadIdx.x % THREADS;
-    const long long row = p.first + (long long)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    const long long step = (long long)gridDim.x * ROWS;
+    long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS;
     if (row >= p.rows) return;                  // (rows share no barrier where a workgroup has several)
-    const T *x = (const T *)p.x + row * p.x_stride;
 
-    Chunk<T> held[NV ? NV : 1];
-    if constexpr (NV > 0) {
+    float gamma[N][V], beta[N][V];
+    Chunk<T> held[N], next[N];
+    auto fetch = [&](long long r, Chunk<T> (&to)[N]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) held[i] = load_chunk(x, (t + i * THREADS) * V, p.cols);
-    }
-    auto each = [&](auto f) __attribute__((always_inline)) {        // f(column of the chunk's first value, chunk)
-        if constexpr (NV > 0) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if ((t + i * THREADS) * V < p.cols) f((t + i * THREADS) * V, held[i]);
-        } else {
-            for (int at = t * V; at < p.cols; at += THREADS * V) f(at, load_chunk(x, at, p.cols));
-        }
+        for (int i = 0; i < NV; ++i) to[i] = load_chunk((const T *)p.x + r * p.x_stride, (t + i * THREADS) * V, p.cols);
     };
-    auto sum = [](float a, float b) { return a + b; };
-
-    float mean = 0.f, rstd = 1.f;
-    if constexpr (OUT != kQuantize) {
-        float s = 0.f;
-        each([&](int, const Chunk<T> &c) {
+    fetch(row, next);
+    if constexpr (NV > 0 && OUT != kQuantize) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) s += (float)c.v[k];
-        });
-        mean = row_reduce<THREADS>(s, slots[0], sum) / (float)p.cols;
-        float d2 = 0.f;         // about the mean: no difference of large squares
-        each([&](int at, const Chunk<T> &c) {
+        for (int i = 0; i < NV; ++i) {
+            load_params((const P *)p.gamma, (t + i * THREADS) * V, p.cols, 1.f, gamma[i]);
+            load_params((const P *)p.beta, (t + i * THREADS) * V, p.cols, 0.f, beta[i]);
+        }
+    }
+    for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) held[i] = next[i];
+        if (row + step < p.rows) fetch(row + step, next);
+        const T *x = (const T *)p.x + row * p.x_stride;
+        auto each = [&](auto f) __attribute__((always_inline)) {        // f(column of the chunk's first value, chunk, its number)
+            if constexpr (NV > 0) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+                    if ((t + i * THREADS) * V < p.cols) f((t + i * THREADS) * V, held[i], i);
+            } else {
+                for (int at = t * V; at < p.cols; at += THREADS * V) f(at, load_chunk(x, at, p.cols), 0);
+            }
+        };
+
+        float mean = 0.f, rstd = 1.f;
+        if constexpr (OUT != kQuantize) {
+            float s = 0.f;
+            each([&](int, const Chunk<T> &c, int) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) s += (float)c.v[k];
+            });
+            mean = row_reduce<THREADS>(s, slots[turn][0], Sum()) / (float)p.cols;
+            float d2 = 0.f;         // about the mean: no difference of large squares
+            each([&](int at, const Chunk<T> &c, int) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float d = (float)c.v[k] - mean;
+                    d2 += at + k < p.cols ? d * d : 0.f;
+                }
+            });
+            rstd = 1.f / sqrtf(row_reduce<THREADS>(d2, slots[turn][1], Sum()) / (float)p.cols + p.eps);
+            if (t == 0) {
+                if (p.mean) p.mean[row] = mean;
+                if (p.rstd) p.rstd[row] = rstd;
+            }
+        }
+        auto values = [&](int at, const Chunk<T> &c, int i, float (&to)[V]) __attribute__((always_inline)) {
+            if constexpr (NV == 0 && OUT != kQuantize) {
+                load_params((const P *)p.gamma, at, p.cols, 1.f, gamma[0]);
+                load_params((const P *)p.beta, at, p.cols, 0.f, beta[0]);
+            }
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                const float d = (float)c.v[k] - mean;
-                d2 += at + k < p.cols ? d * d : 0.f;
+                if constexpr (OUT == kQuantize) to[k] = (float)c.v[k];
+                else to[k] = at + k < p.cols ? ((float)c.v[k] - mean) * rstd * gamma[i][k] + beta[i][k] : 0.f;
             }
-        });
-        rstd = 1.f / sqrtf(row_reduce<THREADS>(d2, slots[1], sum) / (float)p.cols + p.eps);
-        if (t == 0) {
-            if (p.mean) p.mean[row] = mean;
-            if (p.rstd) p.rstd[row] = rstd;
+        };
+        if constexpr (OUT == kReal) {
+            T *y = (T *)p.y + row * p.y_stride;
+            each([&](int at, const Chunk<T> &c, int i) {
+                float v[V];
+                values(at, c, i, v);
+                T out[V];
+#pragma unroll
+                for (int k = 0; k < V; ++k) out[k] = (T)v[k];
+                store_values(y, at, p.cols, out);
+            });
+        } else {
+            float top = 0.f;
+            each([&](int at, const Chunk<T> &c, int i) {
+                float v[V];
+                values(at, c, i, v);
+#pragma unroll
+                for (int k = 0; k < V; ++k) top = MaxNan()(fabsf(v[k]), top);
+            });
+            top = row_reduce<THREADS>(top, slots[turn][2], MaxNan());
+            const RowLevels levels = row_levels(top);
+            if (t == 0) p.scale[row] = levels.scale;
+            int8_t *q = p.q + row * p.y_stride;
+            each([&](int at, const Chunk<T> &c, int i) {
+                float v[V];
+                values(at, c, i, v);
+                int8_t out[V];
+#pragma unroll
+                for (int k = 0; k < V; ++k) out[k] = level_of(v[k], levels);
+                store_values(q, at, p.cols, out);
+            });
         }
-    }
-    auto value = [&](int at, const Chunk<T> &c, int k) __attribute__((always_inline)) -> float {
-        if constexpr (OUT == kQuantize) return (float)c.v[k];
-        if (at + k >= p.cols) return 0.f;
-        return ((float)c.v[k] - mean) * rstd * param((const P *)p.gamma, at + k, 1.f) + param((const P *)p.beta, at + k, 0.f);
-    };
-    if constexpr (OUT == kReal) {
-        T *y = (T *)p.y + row * p.y_stride;
-        each([&](int at, const Chunk<T> &c) {
-            T out[V];
-#pragma unroll
-            for (int k = 0; k < V; ++k) out[k] = (T)value(at, c, k);
-            store_values(y, at, p.cols, out);
-        });
-    } else {
-        float top = 0.f;
-        each([&](int at, const Chunk<T> &c) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) top = max_nan(top, fabsf(value(at, c, k)));
-        });
-        top = row_reduce<THREADS>(top, slots[2], max_nan);
-        const RowLevels levels = row_levels(top);
-        if (t == 0) p.scale[row] = levels.scale;
-        int8_t *q = p.q + row * p.y_stride;
-        each([&](int at, const Chunk<T> &c) {
-            int8_t out[V];
-#pragma unroll
-            for (int k = 0; k < V; ++k) out[k] = level_of(value(at, c, k), levels);
-            store_values(q, at, p.cols, out);
-        });
     }
 }
 
@@ -119,16 +145,10 @@ hipError_t launch_rows(const RowArgs &p, hipStream_t st)
     const int chunks = ceil_div(p.cols, V);
     auto go = [&](auto threads, auto nv) {
         constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
-        constexpr int ROWS = THREADS < kBlock ? kBlock / THREADS : 1;
-        for (long long row = 0; row < p.rows; row += kMaxBlocks * ROWS) {
-            RowArgs q = p;
-            q.first = row;
-            q.rows = std::min(p.rows, row + kMaxBlocks * ROWS);
-            row_kernel<T, P, OUT, THREADS, NV><<<dim3((unsigned)((q.rows - row + ROWS - 1) / ROWS)), dim3(THREADS < kBlock ? kBlock : THREADS), 0, st>>>(q);
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-        }
-        return hipSuccess;
+        constexpr int ROWS = block_of(THREADS) / THREADS;
+        const long long blocks = (p.rows + ROWS - 1) / ROWS;
+        row_kernel<T, P, OUT, THREADS, NV><<<dim3((unsigned)std::min<long long>(blocks, kRowBlocks * compute_units())), dim3(block_of(THREADS)), 0, st>>>(p);
+        return hipGetLastError();
     };
     using std::integral_constant;
     if (chunks <= 64) return go(integral_constant<int, 64>(), integral_constant<int, 1>());
@@ -146,40 +166,47 @@ hipError_t launch_rows(const RowArgs &p, hipStream_t st)
 // registers; a second launch adds the parts in a fixed order.
 // ------------------------------------------------------------------------------------------------
 template <class T, class P, int THREADS, int NV>
-__global__ __launch_bounds__(THREADS < kBlock ? kBlock : THREADS) void norm_back_kernel(const NormBackArgs p)
+__global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const NormBackArgs p)
 {
-    constexpr int V = Chunk<T>::kCount, ROWS = THREADS < kBlock ? kBlock / THREADS : 1;
+    constexpr int V = Chunk<T>::kCount, ROWS = block_of(THREADS) / THREADS;
     __shared__ float slots[2][2][16];
     const int t = threadIdx.x % THREADS;
-    const long long first = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS, step = (long long)gridDim.x * ROWS;
-    float sg[NV][V] = {}, sb[NV][V] = {};
-    int turn = 0;
-    for (long long row = first; row < p.rows; row += step, turn ^= 1) {
-        const T *x = (const T *)p.x + row * p.x_stride, *dy = (const T *)p.dy + row * p.dy_stride;
-        Chunk<T> cx[NV], cd[NV];
+    const long long step = (long long)gridDim.x * ROWS;
+    long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    float gamma[NV][V], sg[NV][V] = {}, sb[NV][V] = {};
+    Chunk<T> cx[NV], cd[NV], nx[NV], nd[NV];
+    float mean = 0.f, rstd = 0.f, next_mean = 0.f, next_rstd = 0.f;
+    auto fetch = [&](long long r) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            cx[i] = load_chunk(x, (t + i * THREADS) * V, p.cols);
-            cd[i] = load_chunk(dy, (t + i * THREADS) * V, p.cols);
+            nx[i] = load_chunk((const T *)p.x + r * p.x_stride, (t + i * THREADS) * V, p.cols);
+            nd[i] = load_chunk((const T *)p.dy + r * p.dy_stride, (t + i * THREADS) * V, p.cols);
         }
-        const float mean = p.mean[row], rstd = p.rstd[row];
+        next_mean = p.mean[r];
+        next_rstd = p.rstd[r];
+    };
+    if (row < p.rows) fetch(row);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load_params((const P *)p.gamma, (t + i * THREADS) * V, p.cols, 1.f, gamma[i]);
+    const float share = 1.f / (float)p.cols;
+    for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) cx[i] = nx[i], cd[i] = nd[i];
+        mean = next_mean, rstd = next_rstd;
+        if (row + step < p.rows) fetch(row + step);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const int at = (t + i * THREADS) * V + k;
-                if (at < p.cols) {
-                    const float xh = ((float)cx[i].v[k] - mean) * rstd, d = (float)cd[i].v[k];
-                    const float pv = d * param((const P *)p.gamma, at, 1.f);
-                    s1 += pv;
-                    s2 += pv * xh;
-                    sg[i][k] += d * xh;
-                    sb[i][k] += d;
-                }
+            for (int k = 0; k < V; ++k) {       // (behind the row's end dy is 0, and with it every term)
+                const float xh = ((float)cx[i].v[k] - mean) * rstd, d = (float)cd[i].v[k], pv = d * gamma[i][k];
+                s1 += pv;
+                s2 += pv * xh;
+                sg[i][k] += d * xh;
+                sb[i][k] += d;
             }
-        s1 = wave_sum(s1);
-        s2 = wave_sum(s2);
+        s1 = wave_reduce(s1, Sum());
+        s2 = wave_reduce(s2, Sum());
         if constexpr (THREADS > kWave) {
             if ((threadIdx.x & 63) == 0) {
                 slots[turn][0][threadIdx.x >> 6] = s1;
@@ -193,8 +220,8 @@ __global__ __launch_bounds__(THREADS < kBlock ? kBlock : THREADS) void norm_back
                 s2 += slots[turn][1][i];
             }
         }
-        s1 /= (float)p.cols;
-        s2 /= (float)p.cols;
+        s1 *= share;
+        s2 *= share;
         T *dx = (T *)p.dx + row * p.dx_stride;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -204,8 +231,7 @@ __global__ __launch_bounds__(THREADS < kBlock ? kBlock : THREADS) void norm_back
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const float xh = ((float)cx[i].v[k] - mean) * rstd;
-                const float pv = (float)cd[i].v[k] * (at + k < p.cols ? param((const P *)p.gamma, at + k, 1.f) : 0.f);
-                out[k] = (T)(rstd * (pv - s1 - xh * s2));
+                out[k] = (T)(rstd * ((float)cd[i].v[k] * gamma[i][k] - s1 - xh * s2));
             }
             store_values(dx, at, p.cols, out);
         }
@@ -226,36 +252,35 @@ template <class T, class P>
 __global__ __launch_bounds__(1024) void norm_back_long_kernel(const NormBackArgs p)
 {
     constexpr int V = Chunk<T>::kCount, THREADS = 1024;
-    __shared__ float slots[2][16];
-    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
-    __syncthreads();        // (slots: the last row's sums have been read)
-    const T *x = (const T *)p.x + row * p.x_stride, *dy = (const T *)p.dy + row * p.dy_stride;
-    const float mean = p.mean[row], rstd = p.rstd[row];
-    auto sum = [](float a, float b) { return a + b; };
-    float s1 = 0.f, s2 = 0.f;
-    for (int at = threadIdx.x * V; at < p.cols; at += THREADS * V) {
-        const Chunk<T> cx = load_chunk(x, at, p.cols), cd = load_chunk(dy, at, p.cols);
+    __shared__ float slots[2][2][16];
+    int turn = 0;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
+        const T *x = (const T *)p.x + row * p.x_stride, *dy = (const T *)p.dy + row * p.dy_stride;
+        const float mean = p.mean[row], rstd = p.rstd[row];
+        float s1 = 0.f, s2 = 0.f;
+        for (int at = threadIdx.x * V; at < p.cols; at += THREADS * V) {
+            const Chunk<T> cx = load_chunk(x, at, p.cols), cd = load_chunk(dy, at, p.cols);
+            float gamma[V];
+            load_params((const P *)p.gamma, at, p.cols, 1.f, gamma);
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (at + k < p.cols) {
-                const float pv = (float)cd.v[k] * param((const P *)p.gamma, at + k, 1.f);
+            for (int k = 0; k < V; ++k) {
+                const float pv = (float)cd.v[k] * gamma[k];
                 s1 += pv;
                 s2 += pv * (((float)cx.v[k] - mean) * rstd);
             }
-    }
-    s1 = row_reduce<THREADS>(s1, slots[0], sum) / (float)p.cols;
-    s2 = row_reduce<THREADS>(s2, slots[1], sum) / (float)p.cols;
-    T *dx = (T *)p.dx + row * p.dx_stride;
-    for (int at = threadIdx.x * V; at < p.cols; at += THREADS * V) {
-        const Chunk<T> cx = load_chunk(x, at, p.cols), cd = load_chunk(dy, at, p.cols);
-        T out[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const float pv = at + k < p.cols ? (float)cd.v[k] * param((const P *)p.gamma, at + k, 1.f) : 0.f;
-            out[k] = (T)(rstd * (pv - s1 - ((float)cx.v[k] - mean) * rstd * s2));
         }
-        store_values(dx, at, p.cols, out);
-    }
+        s1 = row_reduce<THREADS>(s1, slots[turn][0], Sum()) / (float)p.cols;
+        s2 = row_reduce<THREADS>(s2, slots[turn][1], Sum()) / (float)p.cols;
+        T *dx = (T *)p.dx + row * p.dx_stride;
+        for (int at = threadIdx.x * V; at < p.cols; at += THREADS * V) {
+            const Chunk<T> cx = load_chunk(x, at, p.cols), cd = load_chunk(dy, at, p.cols);
+            float gamma[V];
+            load_params((const P *)p.gamma, at, p.cols, 1.f, gamma);
+            T out[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) out[k] = (T)(rstd * ((float)cd.v[k] * gamma[k] - s1 - ((float)cx.v[k] - mean) * rstd * s2));
+            store_values(dx, at, p.cols, out);
+        }
     }
 }
 
@@ -276,21 +301,23 @@ __global__ __launch_bounds__(kBlock) void norm_back_columns_kernel(const NormBac
     to[p.cols] = b;
 }
 
-// dgamma and dbeta from `parts` parts [part][gamma, beta][cols]: 16 columns a workgroup, 16 threads a column.
+// dgamma and dbeta from `parts` parts [part][gamma, beta][cols]: 32 columns a workgroup, eight threads a column.
 template <class P>
 __global__ __launch_bounds__(kBlock) void norm_back_parts_kernel(const float *partial, int parts, int cols, P *dgamma, P *dbeta)
 {
-    __shared__ float lds[16][17];
-    const int c = threadIdx.x & 15, s = threadIdx.x >> 4;
-    const long long col = (long long)blockIdx.x * 16 + c;          // over both vectors
+    __shared__ float lds[8][33];
+    const int c = threadIdx.x & 31, s = threadIdx.x >> 5;
+    const long long col = (long long)blockIdx.x * 32 + c;          // over both vectors
     float v = 0.f;
-    if (col < 2LL * cols)
-        for (int i = s; i < parts; i += 16) v += partial[(long long)i * 2 * cols + col];
+    if (col < 2LL * cols) {
+#pragma unroll 8
+        for (int i = s; i < parts; i += 8) v += partial[(long long)i * 2 * cols + col];
+    }
     lds[s][c] = v;
     __syncthreads();
     if (s == 0 && col < 2LL * cols) {
 #pragma unroll
-        for (int i = 1; i < 16; ++i) v += lds[i][c];
+        for (int i = 1; i < 8; ++i) v += lds[i][c];
         if (col < cols) dgamma[col] = (P)v;
         else dbeta[col - cols] = (P)v;
     }
@@ -329,7 +356,7 @@ hipError_t back(const NormBackArgs &p, int x_type, hipStream_t st)
         using std::integral_constant;
         auto go = [&](auto threads, auto nv) {
             constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
-            norm_back_kernel<T, P, THREADS, NV><<<dim3((unsigned)b.blocks), dim3(THREADS < kBlock ? kBlock : THREADS), 0, st>>>(p);
+            norm_back_kernel<T, P, THREADS, NV><<<dim3((unsigned)b.blocks), dim3(block_of(THREADS)), 0, st>>>(p);
         };
         if (b.nv == 0) {
             norm_back_long_kernel<T, P><<<dim3((unsigned)b.blocks), dim3(1024), 0, st>>>(p);
@@ -346,7 +373,7 @@ hipError_t back(const NormBackArgs &p, int x_type, hipStream_t st)
         if (e != hipSuccess) return e;
     }
     if (p.partial) {
-        norm_back_parts_kernel<P><<<dim3(ceil_div(2LL * p.cols, 16)), dim3(kBlock), 0, st>>>(p.partial, parts, p.cols, (P *)p.dgamma, (P *)p.dbeta);
+        norm_back_parts_kernel<P><<<dim3(ceil_div(2LL * p.cols, 32)), dim3(kBlock), 0, st>>>(p.partial, parts, p.cols, (P *)p.dgamma, (P *)p.dbeta);
         return hipGetLastError();
     }
     return hipSuccess;

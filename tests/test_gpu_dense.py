@@ -301,6 +301,68 @@ def test_int8_gated(xb, dtype, kind, M, F, K):
         assert (held[:, F:] == 5.0).all()
 
 
+# ---- sizes that fill the chip: some rows and columns of the results ---------------------------------------------------------
+
+LARGE = [(4100, 4200, 128), (4096, 4096, 64), (2100, 8200, 700), (9000, 1100, 1337), (4500, 2049, 2304)]
+
+
+def some(n, block=256):
+    """The first, the last and those around the edges of blocks."""
+    at = {0, 1, 15, 16, n // 2, n - 2, n - 1}
+    for e in range(block // 2, n, max(block // 2, n // 12 // (block // 2) * (block // 2))):
+        at |= {e - 1, e}
+    return torch.tensor(sorted(i for i in at if 0 <= i < n))
+
+
+@pytest.mark.parametrize("M,N,K", LARGE)
+def test_large_int8_matmul(xb, M, N, K):
+    for spare in (0, (-K) % 16):
+        a, b, sa, sb, bias = ints(1, M, K, spare), ints(2, N, K, spare), scales(3, M), scales(4, N), rand(5, N)
+        rows, cols = some(M), some(N)
+        for dtype in (F32, BF16):
+            held, out = spaced(M, N, dtype, 3, -7.0)
+            xb.xnor_int8_matmul(a, sa, b, sb, bias, out=out)
+            for r, c in ((rows, torch.arange(N)), (torch.arange(M), cols)):
+                want, bound = ref.int8_matmul(a[r], sa[r], b[c], sb[c], bias[c], dtype)
+                ref.assert_within(out[r.cuda()][:, c.cuda()], want, bound, f"spare {spare} {dtype}")
+            assert (held[:, N:] == -7.0).all()
+
+
+@pytest.mark.parametrize("M,F,K", LARGE)
+def test_large_gated(xb, M, F, K):
+    x, wg, wu = rand(1, M, K, dtype=BF16), rand(2, F, K, dtype=BF16, std=K ** -0.5), rand(3, F, K, dtype=BF16, std=K ** -0.5)
+    for spare in (0, 8):
+        held, h = spaced(M, F, BF16, spare, 5.0)
+        got = xb.xnor_gated_fwd(x, wg, wu, ref.GELU, h=h, want_pre=True)
+        for r, c in ((some(M), torch.arange(F)), (torch.arange(M), some(F))):
+            want, bound = ref.gated(x[r], wg[c], wu[c], ref.GELU, BF16)
+            for t, w, e, name in zip(got, want, bound, "hgu"):
+                ref.assert_within(t[r.cuda()][:, c.cuda()], w, e, name)
+        assert (held[:, F:] == 5.0).all()
+    a, sa, w8, u8, sg, su = ints(1, M, K), scales(2, M), ints(3, F, K), ints(4, F, K), scales(5, F) * 0.1, scales(6, F) * 0.1
+    h8 = xb.xnor_int8_gated(a, sa, w8, sg, u8, su, ref.SILU)
+    for r, c in ((some(M), torch.arange(F)), (torch.arange(M), some(F))):
+        want, bound = ref.int8_gated(a[r], sa[r], w8[c], sg[c], u8[c], su[c], ref.SILU, F32)
+        ref.assert_within(h8[r.cuda()][:, c.cuda()], want, bound, "8 bits")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=str)
+@pytest.mark.parametrize("M,F,K", [(4104, 2100, 2104), (2100, 4104, 4100), (9001, 1001, 1000)])
+def test_large_gated_backward(xb, dtype, M, F, K):
+    x = rand(1, M, K, dtype=dtype)
+    wg, wu = rand(2, F, K, dtype=dtype, std=K ** -0.5), rand(3, F, K, dtype=dtype, std=K ** -0.5)
+    dh, g, u = (rand(4 + i, M, F, dtype=dtype) for i in range(3))
+    dx, dwg, dwu = xb.xnor_gated_bwd(dh, x, wg, wu, g, u, ref.SILU)
+    r, c = some(M), some(F)
+    want, bound = ref.gated_back(dh[r], x[r], wg, wu, g[r], u[r], ref.SILU, dtype)
+    ref.assert_within(dx[r.cuda()], want[0], bound[0], "dx")
+    want, bound = ref.gated_back(dh[:, c], x, wg[c], wu[c], g[:, c], u[:, c], ref.SILU, dtype)
+    ref.assert_within(dwg[c.cuda()], want[1], bound[1], "dwg")
+    ref.assert_within(dwu[c.cuda()], want[2], bound[2], "dwu")
+    again = xb.xnor_gated_bwd(dh, x, wg, wu, g, u, ref.SILU)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dwg) and torch.equal(again[2], dwu)
+
+
 # ---- no tokens, long offsets, streams, graphs --------------------------------------------------------------------------
 
 
