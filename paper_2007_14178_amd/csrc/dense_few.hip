@@ -105,6 +105,8 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const DenseArgs p)
         }
     }
 
+    Columns<EPI> columns;
+    columns.load(p, n0 + g * 4);
     Acc acc[MATS][TT] = {};
     for (int s = from; s < to; s += U) {
         if (s > from) load_b(s);
@@ -142,7 +144,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const DenseArgs p)
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) v[k] += sums[w][k][j][lane];
         }
-        finish<T, O, EPI>(p, m, scale[j], n, v[0], v[MATS - 1]);
+        finish<T, O, EPI>(p, m, scale[j], n, columns, v[0], v[MATS - 1]);
     }
 }
 

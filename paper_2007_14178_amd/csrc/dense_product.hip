@@ -65,22 +65,15 @@ __global__ __launch_bounds__(256, 2) void dense_tile_kernel(const DenseArgs p, i
         }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const long long m = m0 + wm + j * 16 + (lane & 15);
-        if (m >= p.M) continue;
-        const float scale = p.a_scale ? p.a_scale[m] : 1.f;
-        if constexpr (GATED) {
+    for (int i = 0; i < 4; i += GATED ? 2 : 1) {
+        const int n = n0 + (GATED ? wn / 2 + i * 8 : wn + i * 16) + (lane >> 4) * 4;
+        if (n >= p.N) continue;
+        Columns<EPI> columns;
+        columns.load(p, n);
 #pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-                const int n = n0 + wn / 2 + i * 8 + (lane >> 4) * 4;
-                if (n < p.N) finish<T, O, EPI>(p, m, scale, n, acc[i][j], acc[i + 1][j]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int n = n0 + wn + i * 16 + (lane >> 4) * 4;
-                if (n < p.N) finish<T, O, EPI>(p, m, scale, n, acc[i][j], acc[i][j]);
-            }
+        for (int j = 0; j < 4; ++j) {
+            const long long m = m0 + wm + j * 16 + (lane & 15);
+            if (m < p.M) finish<T, O, EPI>(p, m, p.a_scale ? p.a_scale[m] : 1.f, n, columns, acc[i][j], acc[GATED ? i + 1 : i][j]);
         }
     }
 }
@@ -104,6 +97,10 @@ constexpr int kPart = 128 * kStep, kBuffer = 4 * kPart, kFetches = 2;
 
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) void lds_void;
+
+// Row r of b's part `half`: each wave's 32 rows of both parts are 64 consecutive ones of the tile, so that a wave's outputs of a token
+// are 64 consecutive values.
+__device__ inline int b_row_of(int half, int r) { return (r >> 5) * 64 + half * 32 + (r & 31); }
 
 struct TileMap {
     int tiles_n;
@@ -153,7 +150,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int i = 0; i < kFetches; ++i) {
             const int row = 16 * wave + 8 * i + (lane >> 3), chunk = ((lane & 7) ^ (lane >> 3)) * 16;
             at_a[h][i] = min(h * 128 + row, last_m) * (int)p.lda + chunk;
-            at_b[h][i] = min(GATED ? row : h * 128 + row, last_n) * (int)p.ldb + chunk;
+            at_b[h][i] = min(GATED ? row : b_row_of(h, row), last_n) * (int)p.ldb + chunk;
         }
     lds_char *const lds_wave = (lds_char *)lds + 16 * wave * kStep;
     // Part `part` (A0, A1, B0, B1) of a step into buffer step & 1; of a step behind the last one, which nothing reads, the last one's.
@@ -259,7 +256,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int i = 0; i < 4; ++i) {
             const int row = (t >> 3) + 64 * i, to = (row >> 7) * kPart + (row & 127) * kStep + ((chunk ^ (row & 7)) << 4);
             const Chunk<T> ca = load_chunk((const T *)(from_a + (long long)min(row, last_m) * p.lda), at, p.K);
-            const Chunk<T> cb = load_chunk((const T *)(from_b[row >> 7] + (long long)min(GATED ? row & 127 : row, last_n) * p.ldb), at, p.K);
+            const Chunk<T> cb = load_chunk((const T *)(from_b[row >> 7] + (long long)min(GATED ? row & 127 : b_row_of(row >> 7, row & 127), last_n) * p.ldb), at, p.K);
             *(i32x4 *)(lds + to) = __builtin_bit_cast(i32x4, ca);
             *(i32x4 *)(lds + 2 * kPart + to) = __builtin_bit_cast(i32x4, cb);
         }
@@ -267,23 +264,32 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         read_a(0, 0), read_a(1, 0), read_b(0, 0), read_b(1, 0);
         multiply(0, 0), multiply(0, 1), multiply(1, 0), multiply(1, 1);
     }
+    float scale[2][4];
+#pragma unroll
+    for (int ha = 0; ha < 2; ++ha)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) scale[ha][j] = p.a_scale ? p.a_scale[min(m0 + ha * 128 + wm + j * 16 + r, p.M - 1)] : 1.f;
+    constexpr int HB = GATED ? 1 : 2;
+    Columns<EPI> columns[HB][2];
+    int n[HB][2];
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            n[hb][i] = n0 + (GATED ? wn : b_row_of(hb, wn)) + i * 16 + g * 4;
+            if (n[hb][i] < p.N) columns[hb][i].load(p, n[hb][i]);
+        }
 #pragma unroll
     for (int ha = 0; ha < 2; ++ha)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const long long m = m0 + ha * 128 + wm + j * 16 + r;
             if (m >= p.M) continue;
-            const float scale = p.a_scale ? p.a_scale[m] : 1.f;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int n = n0 + wn + i * 16 + g * 4;
-                if constexpr (GATED) {
-                    if (n < p.N) finish<T, O, EPI>(p, m, scale, n, acc[ha][0][j][i], acc[ha][1][j][i]);
-                } else {
-                    if (n < p.N) finish<T, O, EPI>(p, m, scale, n, acc[ha][0][j][i], acc[ha][0][j][i]);
-                    if (n + 128 < p.N) finish<T, O, EPI>(p, m, scale, n + 128, acc[ha][1][j][i], acc[ha][1][j][i]);
-                }
-            }
+            for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (n[hb][i] < p.N) finish<T, O, EPI>(p, m, scale[ha][j], n[hb][i], columns[hb][i], acc[ha][hb][j][i], acc[ha][GATED ? 1 : hb][j][i]);
         }
 }
 

@@ -39,18 +39,28 @@ __device__ inline const char *b_row(const DenseArgs &p, int n0, int r)
     return (const char *)(r & 16 ? p.b2 : p.b) + n * p.ldb;
 }
 
-// Four consecutive outputs n .. n+3 of token m.  Every value is formed in fp32 and rounded once, where it is stored.
-// s: the token's scale (8-bit operands).
+// What four consecutive outputs n .. n+3 of a lane have in common for all its tokens.
+template <int EPI>
+struct Columns {
+    float scale[4], scale2[4], bias[4];
+    __device__ inline void load(const DenseArgs &p, int n)
+    {
+        if constexpr (EPI == kInt8 || EPI == kInt8Gated) load_params(p.b_scale, n, p.N, 0.f, scale);
+        if constexpr (EPI == kInt8Gated) load_params(p.b2_scale, n, p.N, 0.f, scale2);
+        if constexpr (EPI == kInt8) load_params(p.bias, n, p.N, 0.f, bias);
+    }
+};
+
+// These outputs of token m.  Every value is formed in fp32 and rounded once, where it is stored.  s: the token's scale (8-bit operands).
 template <class T, class O, int EPI, class Acc>
-__device__ inline void finish(const DenseArgs &p, long long m, float s, int n, const Acc &v, const Acc &w)
+__device__ inline void finish(const DenseArgs &p, long long m, float s, int n, const Columns<EPI> &c, const Acc &v, const Acc &w)
 {
     O out[4];
     if constexpr (EPI == kInt8) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int at = min(n + i, p.N - 1);
-            const float y = (float)v[i] * (s * p.b_scale[at]);
-            out[i] = (O)(p.bias ? y + p.bias[at] : y);
+            const float y = (float)v[i] * (s * c.scale[i]);
+            out[i] = (O)(p.bias ? y + c.bias[i] : y);
         }
         store_values((O *)p.out + m * p.ldo, n, p.N, out);
     } else if constexpr (EPI == kPlain) {
@@ -66,9 +76,8 @@ __device__ inline void finish(const DenseArgs &p, long long m, float s, int n, c
             g[i] = (float)v[i];
             u[i] = (float)w[i];
             if constexpr (EPI == kInt8Gated) {
-                const int at = min(n + i, p.N - 1);
-                g[i] *= s * p.b_scale[at];
-                u[i] *= s * p.b2_scale[at];
+                g[i] *= s * c.scale[i];
+                u[i] *= s * c.scale2[i];
             }
         }
 #pragma unroll

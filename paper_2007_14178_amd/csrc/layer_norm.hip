@@ -10,7 +10,6 @@ namespace {
 enum RowOutput { kReal, kLevels, kQuantize };       // layer norm; layer norm, quantised; quantisation alone
 
 constexpr int kBlock = 256;
-constexpr int kRowBlocks = 8;           // workgroups a compute unit, at most
 
 // Over the THREADS threads of a row (a wave, or the whole workgroup).  `slots` is not written again before another barrier has passed.
 template <int THREADS, class Op>
@@ -147,15 +146,22 @@ hipError_t launch_rows(const RowArgs &p, hipStream_t st)
         constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
         constexpr int ROWS = block_of(THREADS) / THREADS;
         const long long blocks = (p.rows + ROWS - 1) / ROWS;
-        row_kernel<T, P, OUT, THREADS, NV><<<dim3((unsigned)std::min<long long>(blocks, kRowBlocks * compute_units())), dim3(block_of(THREADS)), 0, st>>>(p);
+        row_kernel<T, P, OUT, THREADS, NV><<<dim3((unsigned)std::min<long long>(blocks, (THREADS >= 512 && OUT == kReal ? 4 : 16) * compute_units())), dim3(block_of(THREADS)), 0, st>>>(p);
         return hipGetLastError();
     };
     using std::integral_constant;
     if (chunks <= 64) return go(integral_constant<int, 64>(), integral_constant<int, 1>());
     if (chunks <= 128) return go(integral_constant<int, 64>(), integral_constant<int, 2>());
     if (chunks <= 256) return go(integral_constant<int, 256>(), integral_constant<int, 1>());
-    if (chunks <= 512) return go(integral_constant<int, 256>(), integral_constant<int, 2>());
-    if (chunks <= 1024) return go(integral_constant<int, 256>(), integral_constant<int, 4>());
+    // Real outputs: a chunk a thread (16384 x 4096 bf16 56 us, with two 67; 16384 x 8192 118 us, with four 169).  Levels take three sums
+    // or maxima over the workgroup, and fewer waves wait for each other (16384 x 4096 quantised norm 63 us, with one chunk 81).
+    if constexpr (OUT == kReal) {
+        if (chunks <= 512) return go(integral_constant<int, 512>(), integral_constant<int, 1>());
+        if (chunks <= 1024) return go(integral_constant<int, 1024>(), integral_constant<int, 1>());
+    } else {
+        if (chunks <= 512) return go(integral_constant<int, 256>(), integral_constant<int, 2>());
+        if (chunks <= 1024) return go(integral_constant<int, 512>(), integral_constant<int, 2>());
+    }
     if (chunks <= 4096) return go(integral_constant<int, 1024>(), integral_constant<int, 4>());
     return go(integral_constant<int, 1024>(), integral_constant<int, 0>());
 }
@@ -333,8 +339,9 @@ BackPlan back_plan(int x_type, long long rows, int cols)
     const int chunks = ceil_div(cols, x_type == XNOR_TYPE_FP32 ? 4 : 8);
     BackPlan b{};
     if (chunks <= 128) b.threads = 64, b.nv = chunks <= 64 ? 1 : 2;
-    else if (chunks <= 1024) b.threads = 256, b.nv = chunks <= 256 ? 1 : chunks <= 512 ? 2 : 4;
-    else if (chunks <= 4096) b.threads = 1024, b.nv = 4;
+    else if (chunks <= 256) b.threads = 256, b.nv = 1;
+    else if (chunks <= 512) b.threads = 512, b.nv = 1;
+    else if (chunks <= 4096) b.threads = 1024, b.nv = chunks <= 1024 ? 1 : chunks <= 2048 ? 2 : 4;
     if (b.nv == 0) {
         b.blocks = (int)std::min(rows, kMaxBlocks);
         b.parts = (int)std::min<long long>(rows, 64);
@@ -364,10 +371,12 @@ hipError_t back(const NormBackArgs &p, int x_type, hipStream_t st)
         } else if (b.threads == 64) {
             b.nv == 1 ? go(integral_constant<int, 64>(), integral_constant<int, 1>()) : go(integral_constant<int, 64>(), integral_constant<int, 2>());
         } else if (b.threads == 256) {
-            b.nv == 1   ? go(integral_constant<int, 256>(), integral_constant<int, 1>())
-            : b.nv == 2 ? go(integral_constant<int, 256>(), integral_constant<int, 2>()) : go(integral_constant<int, 256>(), integral_constant<int, 4>());
+            go(integral_constant<int, 256>(), integral_constant<int, 1>());
+        } else if (b.threads == 512) {
+            go(integral_constant<int, 512>(), integral_constant<int, 1>());
         } else {
-            go(integral_constant<int, 1024>(), integral_constant<int, 4>());
+            b.nv == 1   ? go(integral_constant<int, 1024>(), integral_constant<int, 1>())
+            : b.nv == 2 ? go(integral_constant<int, 1024>(), integral_constant<int, 2>()) : go(integral_constant<int, 1024>(), integral_constant<int, 4>());
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
