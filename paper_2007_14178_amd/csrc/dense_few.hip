@@ -17,7 +17,7 @@ template <class T, class O, int EPI, int TT, class X>
 __global__ __launch_bounds__(kThreads) void few_kernel(const DenseArgs p)
 {
     constexpr bool GATED = EPI == kGated || EPI == kInt8Gated, REAL = !std::is_void<X>::value;
-    constexpr int MATS = GATED ? 2 : 1, U = 4;
+    constexpr int MATS = GATED ? 2 : 1, U = TT < 4 ? 4 : 2;
     typedef Mat<T> Mul;
     typedef typename Mul::acc Acc;
     __shared__ Acc sums[kWaves][MATS][TT][kWave];
@@ -49,7 +49,6 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const DenseArgs p)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int at = ((s + u) * kStep + g * 32 + i * 16) / (int)sizeof(T);
-                    vb[k][u][i] = i32x4{};
                     if (s + u < to) vb[k][u][i] = __builtin_bit_cast(i32x4, load_chunk(b[k], at, p.K));
                 }
     };
@@ -110,22 +109,29 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const DenseArgs p)
     Acc acc[MATS][TT] = {};
     for (int s = from; s < to; s += U) {
         if (s > from) load_b(s);
+        i32x4 va[U][2][TT];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (s + u >= to) break;
+        for (int u = 0; u < U; ++u)
+            if (s + u < to) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int at = (s + u) * kStep + g * 32 + i * 16;
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < TT; ++j) {
-                    i32x4 va;
-                    if constexpr (REAL) va = *(const i32x4 *)(levels + min(r, (int)p.M - 1) * held_bytes + at);
-                    else va = __builtin_bit_cast(i32x4, load_chunk(a[j], at / (int)sizeof(T), p.K));
-#pragma unroll
-                    for (int k = 0; k < MATS; ++k) acc[k][j] = Mul::mul(vb[k][u][i], va, acc[k][j]);
-                }
+                    for (int j = 0; j < TT; ++j) {
+                        const int at = (s + u) * kStep + g * 32 + i * 16;
+                        if constexpr (REAL) va[u][i][j] = *(const i32x4 *)(levels + min(r, (int)p.M - 1) * held_bytes + at);
+                        else va[u][i][j] = __builtin_bit_cast(i32x4, load_chunk(a[j], at / (int)sizeof(T), p.K));
+                    }
             }
-        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (s + u < to) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < TT; ++j)
+#pragma unroll
+                        for (int k = 0; k < MATS; ++k) acc[k][j] = Mul::mul(vb[k][u][i], va[u][i][j], acc[k][j]);
+            }
     }
 #pragma unroll
     for (int k = 0; k < MATS; ++k)

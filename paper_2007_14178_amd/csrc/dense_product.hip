@@ -79,21 +79,22 @@ __global__ __launch_bounds__(256, 2) void dense_tile_kernel(const DenseArgs p, i
 }
 
 // ------------------------------------------------------------------------------------------------
-// 256 tokens x 256 rows of b, eight waves of 128 x 64 (64 x 32 of each quarter), one workgroup a compute unit.
+// Tiles whose rows are fetched straight into LDS.  WM x WN waves share a tile of 2 P tokens x 2 P rows of b, P = 16 WM WN: 256 x 256 with
+// eight waves, one workgroup a compute unit, or 128 x 128 with four.
 //
-// LDS holds two steps of the contraction, each as four parts of 128 rows: the tokens' halves A0, A1 and b's B0, B1 (in the
-// gated block the two matrices' rows for the same outputs).  A step is four phases of 16 matrix instructions a wave, one for each pair
-// of halves, in the order A0 P, A0 Q, A1 Q, A1 P with P = B0, Q = B1 in even steps and the reverse in odd ones: each phase then
-// needs one half more than the one before, and reads it from LDS while the last one's instructions run:
-//     phase     instructions     reads from LDS     its LDS part is refilled in
-//       0       A0 P             Q                  the next phase
-//       1       A0 Q             A1                 the next phase
-//       2       A1 Q             the next A0        the next phase
-//       3       A1 P             the next step's first b half (this step's Q place)
-// A part's rows are fetched seven phases before they are read, straight into LDS (16 bytes a lane, two instructions a wave and
-// part); at a phase's end six younger fetches may be under way, and that is what the wave waits for.
+// LDS holds STEPS steps of the contraction, each as four parts of P rows: the tokens' halves A0, A1 and b's B0, B1 (in the
+// gated block the two matrices' rows for the same outputs).  A step is four phases, one for each pair of halves, in the order A0 X, A0 Y,
+// A1 Y, A1 X with X = B0, Y = B1 in even steps and the reverse in odd ones: each phase then needs one half more than the one
+// before, and reads it from LDS while the last one's instructions run:
+//     phase     instructions     reads from LDS
+//       0       A0 X             Y
+//       1       A0 Y             A1
+//       2       A1 Y             the next step's A0
+//       3       A1 X             the next step's first b half (into Y's registers)
+// What a phase has read is refilled in the next one with the rows of STEPS steps further on (16 bytes a lane, two instructions
+// a wave and part), 4 STEPS - 1 phases before they are read; at a phase's end the 4 STEPS - 2 youngest fetches may be under way.
 // ------------------------------------------------------------------------------------------------
-constexpr int kPart = 128 * kStep, kBuffer = 4 * kPart, kFetches = 2;
+constexpr int kFetches = 2;
 
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) void lds_void;
@@ -120,26 +121,45 @@ __device__ inline bool tile_of(const TileMap &t, int *tm, int *tn)
     return true;
 }
 
-template <class T, class O, int EPI>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void dense_large_kernel(const DenseArgs p, const TileMap map)
+template <int WM_, int WN_, int STEPS_, int GROUPS_>
+struct Shape {
+    static constexpr int WM = WM_, WN = WN_, STEPS = STEPS_, WAVES = WM * WN, ROWS = 16 * WAVES;   // ROWS: of a part
+    static constexpr int GROUPS = GROUPS_;                          // groups of so many waves, a share of the contraction each
+    static constexpr int RM = WN, RN = WM;                          // 16-row fragments of a part that a wave takes
+    static constexpr int kPart = ROWS * kStep, kBuffer = 4 * kPart, kLds = STEPS * kBuffer;
+    static constexpr int kYoung = (4 * STEPS - 2) * kFetches;
+    static_assert(RN == 2 && (STEPS & (STEPS - 1)) == 0 && GROUPS <= 2, "");
+};
+typedef Shape<2, 4, 2, 1> Large;
+typedef Shape<2, 2, 2, 1> Medium;
+typedef Shape<2, 2, 2, 2> Split;
+
+template <class T, class O, int EPI, class S>
+__global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void dense_direct_kernel(const DenseArgs p, const TileMap map)
 {
     constexpr bool GATED = EPI == kGated || EPI == kInt8Gated;
+    constexpr int ROWS = S::ROWS, RM = S::RM, RN = S::RN, kPart = S::kPart, kBuffer = S::kBuffer, STEPS = S::STEPS;
     typedef Mat<T> X;
     typedef typename X::acc Acc;
-    extern __shared__ __align__(1024) char lds[];
+    extern __shared__ __align__(1024) char lds_all[];
     int tm, tn;
     if (!tile_of(map, &tm, &tn)) return;
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = lane & 15, g = lane >> 4;
-    const long long m0 = p.first + (long long)tm * 256;
-    const int n0 = tn * (GATED ? 128 : 256);
-    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 32;
-    const int bytes = p.K * (int)sizeof(T), steps = bytes / kStep;
+    const int group = S::GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (S::WAVES * kWave));
+    const int t = S::GROUPS == 1 ? threadIdx.x : threadIdx.x % (S::WAVES * kWave);
+    const int lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = lane & 15, g = lane >> 4;
+    char *const lds = lds_all + group * S::kLds;
+    const long long m0 = p.first + (long long)tm * 2 * ROWS;
+    const int n0 = tn * (GATED ? ROWS : 2 * ROWS);
+    const int wm = wave % S::WM * RM * 16, wn = wave / S::WM * RN * 16;
+    // A group's whole steps; what is left over, whole or not, is a step more for some groups, through registers.
+    const int bytes = p.K * (int)sizeof(T), steps = bytes / kStep / S::GROUPS, first = group * steps;
+    const int rest = S::GROUPS * steps, left = (bytes + kStep - 1) / kStep - rest;
 
     // Fetches: instruction i of a wave fills rows 16 wave + 8 i + lane / 8 of a part, and the lane brings the 16 bytes that
     // belong at its place: chunk c of row r stands at place c ^ (r & 7), which spreads a column of rows over the banks.
     const char *const from_a = (const char *)p.a + m0 * p.lda;
-    const char *const from_b[2] = {(const char *)p.b + (long long)n0 * p.ldb, GATED ? (const char *)p.b2 + (long long)n0 * p.ldb : (const char *)p.b + (long long)n0 * p.ldb};
-    const int last_m = (int)min(p.M - 1 - m0, 255LL), last_n = min(p.N - 1 - n0, GATED ? 127 : 255);
+    const char *const from_b[2] = {(const char *)p.b + (long long)n0 * p.ldb, (const char *)(GATED ? p.b2 : p.b) + (long long)n0 * p.ldb};
+    const int last_m = (int)min(p.M - 1 - m0, 2LL * ROWS - 1), last_n = min(p.N - 1 - n0, (GATED ? 1 : 2) * ROWS - 1);
     const auto rsrc_a = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_a), 0, (int)(last_m * p.lda + bytes), 0x00027000);
     const auto rsrc_b0 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_b[0]), 0, (int)(last_n * p.ldb + bytes), 0x00027000);
     const auto rsrc_b1 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_b[1]), 0, (int)(last_n * p.ldb + bytes), 0x00027000);
@@ -149,15 +169,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
         for (int i = 0; i < kFetches; ++i) {
             const int row = 16 * wave + 8 * i + (lane >> 3), chunk = ((lane & 7) ^ (lane >> 3)) * 16;
-            at_a[h][i] = min(h * 128 + row, last_m) * (int)p.lda + chunk;
+            at_a[h][i] = min(h * ROWS + row, last_m) * (int)p.lda + chunk;
             at_b[h][i] = min(GATED ? row : b_row_of(h, row), last_n) * (int)p.ldb + chunk;
         }
     lds_char *const lds_wave = (lds_char *)lds + 16 * wave * kStep;
-    // Part `part` (A0, A1, B0, B1) of a step into buffer step & 1; of a step behind the last one, which nothing reads, the last one's.
+    // Part `part` (A0, A1, B0, B1) of a step into its buffer; of a step behind the last one, which nothing reads, the last one's.
     auto fetch = [&](auto part, int step) __attribute__((always_inline)) {
         constexpr int PART = decltype(part)::value;
-        lds_char *const to = lds_wave + (step & 1) * kBuffer + PART * kPart;
-        const int k = min(step, steps - 1) * kStep;
+        lds_char *const to = lds_wave + (step & (STEPS - 1)) * kBuffer + PART * kPart;
+        const int k = (first + min(step, steps - 1)) * kStep;
 #pragma unroll
         for (int i = 0; i < kFetches; ++i) {
             const int at = PART < 2 ? at_a[PART & 1][i] : at_b[PART & 1][i];
@@ -167,35 +187,35 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     };
     // The lane's places in a part for the two halves of a step; a fragment is 16 rows further on.
     const uint32_t place0 = r * kStep + ((g ^ (r & 7)) << 4), place1 = place0 ^ 64;
-    i32x4 a[2][4][2], b[2][2][2];
-    auto read_a = [&](int h, int buffer) __attribute__((always_inline)) {
-        const char *part = lds + buffer * kBuffer + h * kPart + wm * kStep;
+    i32x4 a[2][RM][2], b[2][RN][2];
+    auto read_a = [&](int h, int step) __attribute__((always_inline)) {
+        const char *part = lds + (step & (STEPS - 1)) * kBuffer + h * kPart + wm * kStep;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < RM; ++j) {
             a[h][j][0] = *(const i32x4 *)(part + place0 + j * 16 * kStep);
             a[h][j][1] = *(const i32x4 *)(part + place1 + j * 16 * kStep);
         }
     };
-    auto read_b = [&](int h, int buffer) __attribute__((always_inline)) {
-        const char *part = lds + buffer * kBuffer + (2 + h) * kPart + wn * kStep;
+    auto read_b = [&](int h, int step) __attribute__((always_inline)) {
+        const char *part = lds + (step & (STEPS - 1)) * kBuffer + (2 + h) * kPart + wn * kStep;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < RN; ++j) {
             b[h][j][0] = *(const i32x4 *)(part + place0 + j * 16 * kStep);
             b[h][j][1] = *(const i32x4 *)(part + place1 + j * 16 * kStep);
         }
     };
-    Acc acc[2][2][4][2] = {};       // [token half][b half][16 tokens][16 rows of b]
+    Acc acc[2][2][RM][RN] = {};     // [token half][b half][16 tokens][16 rows of b]
     auto multiply = [&](int ha, int hb) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < RM; ++j)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) acc[ha][hb][j][i] = X::mul(b[hb][i][h], a[ha][j][h], acc[ha][hb][j][i]);
+                for (int i = 0; i < RN; ++i) acc[ha][hb][j][i] = X::mul(b[hb][i][h], a[ha][j][h], acc[ha][hb][j][i]);
     };
     auto end_phase = [&]() __attribute__((always_inline)) {
         __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(S::kYoung) : "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
     using std::integral_constant;
@@ -205,96 +225,127 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const integral_constant<int, 3> B1{};
 
     if (steps > 0) {
-        fetch(A0, 0), fetch(B0, 0), fetch(B1, 0), fetch(A1, 0), fetch(A0, 1), fetch(B1, 1), fetch(B0, 1);
+#pragma unroll
+        for (int s = 0; s < STEPS; s += 2) {
+            fetch(A0, s), fetch(B0, s), fetch(B1, s), fetch(A1, s);
+            fetch(A0, s + 1), fetch(B1, s + 1), fetch(B0, s + 1);
+            if (s + 2 < STEPS) fetch(A1, s + 1);
+        }
         end_phase();
         read_a(0, 0);
-        fetch(A1, 1);
+        fetch(A1, STEPS - 1);
         end_phase();
         read_b(0, 0);
-        fetch(A0, 2);
+        fetch(A0, STEPS);
         end_phase();
         for (int s = 0; s < steps; s += 2) {
-            read_b(1, 0);
-            fetch(B0, s + 2);
+            read_b(1, s);
+            fetch(B0, s + STEPS);
             multiply(0, 0);
             end_phase();
-            read_a(1, 0);
-            fetch(B1, s + 2);
+            read_a(1, s);
+            fetch(B1, s + STEPS);
             multiply(0, 1);
             end_phase();
-            read_a(0, 1);
-            fetch(A1, s + 2);
+            read_a(0, s + 1);
+            fetch(A1, s + STEPS);
             multiply(1, 1);
             end_phase();
-            read_b(1, 1);
-            fetch(A0, s + 3);
+            read_b(1, s + 1);
+            fetch(A0, s + 1 + STEPS);
             multiply(1, 0);
             end_phase();
             if (s + 1 >= steps) break;
-            read_b(0, 1);
-            fetch(B1, s + 3);
+            read_b(0, s + 1);
+            fetch(B1, s + 1 + STEPS);
             multiply(0, 1);
             end_phase();
-            read_a(1, 1);
-            fetch(B0, s + 3);
+            read_a(1, s + 1);
+            fetch(B0, s + 1 + STEPS);
             multiply(0, 0);
             end_phase();
-            read_a(0, 0);
-            fetch(A1, s + 3);
+            read_a(0, s + 2);
+            fetch(A1, s + 1 + STEPS);
             multiply(1, 0);
             end_phase();
-            read_b(0, 0);
-            fetch(A0, s + 4);
+            read_b(0, s + 2);
+            fetch(A0, s + 2 + STEPS);
             multiply(1, 1);
             end_phase();
         }
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
     }
-    if (steps * kStep < bytes) {        // the contraction's end, through registers
-        const int chunk = t & 7, at = (steps * kStep + chunk * 16) / (int)sizeof(T);
+    if (left > 0) {         // the contraction's end
+        const int chunk = t & 7, at = ((rest + group) * kStep + chunk * 16) / (int)sizeof(T);       // (zeros behind it)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = (t >> 3) + 64 * i, to = (row >> 7) * kPart + (row & 127) * kStep + ((chunk ^ (row & 7)) << 4);
-            const Chunk<T> ca = load_chunk((const T *)(from_a + (long long)min(row, last_m) * p.lda), at, p.K);
-            const Chunk<T> cb = load_chunk((const T *)(from_b[row >> 7] + (long long)min(GATED ? row & 127 : b_row_of(row >> 7, row & 127), last_n) * p.ldb), at, p.K);
-            *(i32x4 *)(lds + to) = __builtin_bit_cast(i32x4, ca);
-            *(i32x4 *)(lds + 2 * kPart + to) = __builtin_bit_cast(i32x4, cb);
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = (t >> 3) + 8 * S::WAVES * i, to = row * kStep + ((chunk ^ (row & 7)) << 4);
+                const Chunk<T> ca = load_chunk((const T *)(from_a + (long long)min(h * ROWS + row, last_m) * p.lda), at, p.K);
+                const Chunk<T> cb = load_chunk((const T *)(from_b[h] + (long long)min(GATED ? row : b_row_of(h, row), last_n) * p.ldb), at, p.K);
+                *(i32x4 *)(lds + h * kPart + to) = __builtin_bit_cast(i32x4, ca);
+                *(i32x4 *)(lds + (2 + h) * kPart + to) = __builtin_bit_cast(i32x4, cb);
+            }
         __syncthreads();
         read_a(0, 0), read_a(1, 0), read_b(0, 0), read_b(1, 0);
         multiply(0, 0), multiply(0, 1), multiply(1, 0), multiply(1, 1);
     }
-    float scale[2][4];
+    // Two groups: each finishes one half of the tokens, with the other's sums of it.
+    constexpr int HALVES = S::GROUPS == 1 ? 2 : 1;
+    if constexpr (S::GROUPS == 2) {
+        __syncthreads();
+        Acc *const slots = (Acc *)lds_all + wave * 2 * RM * RN * kWave + lane;
 #pragma unroll
-    for (int ha = 0; ha < 2; ++ha)
+        for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) scale[ha][j] = p.a_scale ? p.a_scale[min(m0 + ha * 128 + wm + j * 16 + r, p.M - 1)] : 1.f;
+            for (int j = 0; j < RM; ++j)
+#pragma unroll
+                for (int i = 0; i < RN; ++i) {
+                    const int at = ((hb * RM + j) * RN + i) * kWave;
+                    slots[group * S::WAVES * 2 * RM * RN * kWave + at] = group ? acc[0][hb][j][i] : acc[1][hb][j][i];
+                    if (group) acc[0][hb][j][i] = acc[1][hb][j][i];
+                }
+        __syncthreads();
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+            for (int j = 0; j < RM; ++j)
+#pragma unroll
+                for (int i = 0; i < RN; ++i)
+                    acc[0][hb][j][i] += slots[(1 - group) * S::WAVES * 2 * RM * RN * kWave + ((hb * RM + j) * RN + i) * kWave];
+    }
+    float scale[HALVES][RM];
+#pragma unroll
+    for (int ha = 0; ha < HALVES; ++ha)
+#pragma unroll
+        for (int j = 0; j < RM; ++j) scale[ha][j] = p.a_scale ? p.a_scale[min(m0 + (group + ha) * ROWS + wm + j * 16 + r, p.M - 1)] : 1.f;
     constexpr int HB = GATED ? 1 : 2;
-    Columns<EPI> columns[HB][2];
-    int n[HB][2];
+    Columns<EPI> columns[HB][RN];
+    int n[HB][RN];
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < RN; ++i) {
             n[hb][i] = n0 + (GATED ? wn : b_row_of(hb, wn)) + i * 16 + g * 4;
             if (n[hb][i] < p.N) columns[hb][i].load(p, n[hb][i]);
         }
 #pragma unroll
-    for (int ha = 0; ha < 2; ++ha)
+    for (int ha = 0; ha < HALVES; ++ha)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long long m = m0 + ha * 128 + wm + j * 16 + r;
+        for (int j = 0; j < RM; ++j) {
+            const long long m = m0 + (group + ha) * ROWS + wm + j * 16 + r;
             if (m >= p.M) continue;
 #pragma unroll
             for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < RN; ++i)
                     if (n[hb][i] < p.N) finish<T, O, EPI>(p, m, scale[ha][j], n[hb][i], columns[hb][i], acc[ha][hb][j][i], acc[ha][GATED ? 1 : hb][j][i]);
         }
 }
 
 // Whether the fetches straight into LDS take the operands: rows at multiples of 16 bytes, a tile's rows within 31 bits of its first.
-bool large_supports(const DenseArgs &p, int size)
+bool direct_supports(const DenseArgs &p, int size)
 {
     auto fits = [&](const void *q, long long ld) {
         return (reinterpret_cast<uintptr_t>(q) & 15) == 0 && (ld & 15) == 0 && 255 * ld + (long long)p.K * size < 0x7fffffffLL;
@@ -302,27 +353,28 @@ bool large_supports(const DenseArgs &p, int size)
     return fits(p.a, p.lda) && fits(p.b, p.ldb) && (!p.b2 || fits(p.b2, p.ldb));
 }
 
-template <class T, class O, int EPI>
-hipError_t launch_large(const DenseArgs &p, hipStream_t st)
+template <class T, class O, int EPI, class S>
+hipError_t launch_direct(const DenseArgs &p, hipStream_t st)
 {
     static std::atomic<bool> raised[64];
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev < 0 || dev >= 64 || !raised[dev].load(std::memory_order_relaxed)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_large_kernel<T, O, EPI>), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kBuffer);
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_direct_kernel<T, O, EPI, S>), hipFuncAttributeMaxDynamicSharedMemorySize, S::GROUPS * S::kLds);
         if (e != hipSuccess) return e;
         if (dev >= 0 && dev < 64) raised[dev].store(true, std::memory_order_relaxed);
     }
-    constexpr int TN = EPI == kGated || EPI == kInt8Gated ? 128 : 256;
+    constexpr int TM = 2 * S::ROWS, TN = (EPI == kGated || EPI == kInt8Gated ? 1 : 2) * S::ROWS;
     TileMap map{ceil_div(p.N, TN), 0};
-    const long long rows = std::max<long long>(1, kMaxBlocks / map.tiles_n) * 256;
+    // (a launch has fewer than 2^32 threads: more tokens than that gives in several)
+    const long long rows = std::max<long long>(1, kMaxBlocks / map.tiles_n) * TM;
     for (long long m = 0; m < p.M; m += rows) {
         DenseArgs q = p;
         q.first = m;
         q.M = std::min(p.M, m + rows);
-        map.tiles = map.tiles_n * ((q.M - m + 255) / 256);
-        dense_large_kernel<T, O, EPI><<<dim3((unsigned)((map.tiles + 7) / 8 * 8)), dim3(512), 2 * kBuffer, st>>>(q, map);
+        map.tiles = map.tiles_n * ((q.M - m + TM - 1) / TM);
+        dense_direct_kernel<T, O, EPI, S><<<dim3((unsigned)((map.tiles + 7) / 8 * 8)), dim3(S::GROUPS * S::WAVES * kWave), S::GROUPS * S::kLds, st>>>(q, map);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -330,14 +382,10 @@ hipError_t launch_large(const DenseArgs &p, hipStream_t st)
 }
 
 template <class T, class O, int EPI>
-hipError_t launch(const DenseArgs &p, hipStream_t st)
+hipError_t launch_tiles(const DenseArgs &p, hipStream_t st)
 {
     constexpr int TN = EPI == kGated || EPI == kInt8Gated ? 64 : 128;
-    if (p.M == 0) return hipSuccess;
-    if (p.M <= kFewTokens) return launch_few<T, O, EPI>(p, st);
-    if (large_supports(p, sizeof(T)) && p.M * (long long)p.N >= 256LL * 256 * 128) return launch_large<T, O, EPI>(p, st);
     const int tiles_n = ceil_div(p.N, TN);
-    // (a launch has fewer than 2^32 threads: more tokens than that gives in several)
     const long long rows = std::max<long long>(1, kMaxBlocks / tiles_n) * 128;
     for (long long m = 0; m < p.M; m += rows) {
         DenseArgs q = p;
@@ -348,6 +396,31 @@ hipError_t launch(const DenseArgs &p, hipStream_t st)
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
+}
+
+// Which kernel.  Up to 16 tokens the one that reads b once; up to 64 too where it has no more than a workgroup a unit (each of them reads
+// all tokens: 64 tokens x 4096 x 4096 12.3 us, on tiles 16.8; x 8192 x 8192 41 us, 28) or rows that the fetches into LDS do not take.
+// Then by tiles of 128 x 128: where a unit gets no more than one, two groups of waves share its contraction (256 x 4096 x 4096
+// 8 bits 17.0 us, without 19.8).  Else by what the rounds of workgroups take, in steps of a 256 x 256 tile: one tile of these a unit, or two
+// of a quarter at 0.56 of the time, a step; and some time for the tile's begin and end, which only two workgroups on a unit overlap.
+// (2048 x 4096 x 4096 8 bits 38.7 us on small tiles, 49.5 on large ones; 4096 x 4096 x 4096 70.5 and 67.9; 6144: 104 and 110; 16-bit gated block of
+// 3584 x 4096 x 4096 209 and 195; 100352 x 512 x 512 8 bits 65 and 71.)
+template <class T, class O, int EPI>
+hipError_t launch(const DenseArgs &p, hipStream_t st)
+{
+    constexpr bool GATED = EPI == kGated || EPI == kInt8Gated;
+    if (p.M == 0) return hipSuccess;
+    const bool direct = direct_supports(p, sizeof(T));
+    const long long units = compute_units();
+    if (p.M <= 16 || (p.M <= kFewTokens && (!direct || p.N <= 16 * units))) return launch_few<T, O, EPI>(p, st);
+    if (!direct) return launch_tiles<T, O, EPI>(p, st);
+    const int n = GATED ? 2 : 1;        // matrices
+    const long long small = ((p.M + 127) / 128) * ceil_div((long long)p.N * n, 128), large = ((p.M + 255) / 256) * ceil_div((long long)p.N * n, 256);
+    if (small <= units) return launch_direct<T, O, EPI, Split>(p, st);
+    const double steps = (double)p.K * sizeof(T) / kStep;
+    const double small_time = (double)((small + 2 * units - 1) / (2 * units)) * (0.56 * steps + 2.5);
+    const double large_time = (double)((large + units - 1) / units) * (steps + 5);
+    return small_time < large_time ? launch_direct<T, O, EPI, Medium>(p, st) : launch_direct<T, O, EPI, Large>(p, st);
 }
 
 }  // namespace
