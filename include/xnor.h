@@ -481,7 +481,8 @@ int xnor_int8_matmul(const int8_t *a, long long a_stride, const float *a_scale, 
 
 /*
  * A linear layer with 8-bit weights on real tokens: xnor_int8_quantize of x and xnor_int8_matmul with w, the same values.
- *   workspace   16-byte aligned, xnor_int8_linear_workspace_bytes bytes (host only); its contents mean nothing afterwards
+ *   workspace   16-byte aligned, xnor_int8_linear_workspace_bytes bytes (host only; 0 for one or two tokens of up to 8192 values,
+ *               which are quantised by the product's own launch: then it may be NULL); its contents mean nothing afterwards
  */
 int xnor_int8_linear_workspace_bytes(long long M, int K, size_t *bytes);
 int xnor_int8_linear(const void *x, int x_type, long long x_stride, const int8_t *w, long long w_stride, const float *w_scale,
@@ -525,13 +526,21 @@ int xnor_layer_norm_bwd(const void *dy, long long dy_stride, const void *x, int 
  *   wg, wu   in   [F][K] (one stride)
  *   h        out  [M][F]
  *   g, u     out  [M][F] (one stride), rounded, for the backward pass; or both NULL.  h is formed from g and u before they are rounded.
+ * _ws: with a workspace, into which operands whose rows do not all start at multiples of 16 bytes are copied first where that is faster
+ * (the same values; XNOR_E_ALIGN if it is not 16-byte aligned; one that is too small, or NULL, is not used).
+ * xnor_gated_fwd_workspace_bytes (host only) is 0 where none would be used with these strides.
  * Gradients, from those of h and the g and u that the forward pass left:
  *     dg = dh * u * act'(g), du = dh * act(g);  dx = dg wg + du wu, dwg = dg^T x, dwu = du^T x
  * dg and du are rounded to the block's type before the products, as the matrix instructions take them.
  *   workspace  16-byte aligned, xnor_gated_bwd_workspace_bytes bytes (host only); its contents mean nothing afterwards
+ * F and K of the gradients are at most 2^20.
  */
 int xnor_gated_fwd(const void *x, int type, long long x_stride, const void *wg, const void *wu, long long w_stride, int act,
                    long long M, int F, int K, void *h, long long h_stride, void *g, void *u, long long gu_stride, void *stream);
+int xnor_gated_fwd_workspace_bytes(long long M, int F, int K, long long x_stride, long long w_stride, size_t *bytes);
+int xnor_gated_fwd_ws(const void *x, int type, long long x_stride, const void *wg, const void *wu, long long w_stride, int act,
+                      long long M, int F, int K, void *h, long long h_stride, void *g, void *u, long long gu_stride, void *workspace,
+                      size_t workspace_bytes, void *stream);
 int xnor_gated_bwd_workspace_bytes(long long M, int F, int K, size_t *bytes);
 int xnor_gated_bwd(const void *dh, long long dh_stride, const void *x, int type, long long x_stride, const void *wg,
                    const void *wu, long long w_stride, const void *g, const void *u, long long gu_stride, int act, long long M,

@@ -69,7 +69,7 @@ int norm_forward(const void *x, int x_type, long long rows, int cols, long long 
     return hip_status(launch_layer_norm(a, x_type, p_type, (hipStream_t)stream));
 }
 
-size_t q_stride_of(int K) { return ((size_t)K + 15) / 16 * 16; }
+size_t q_stride_of(int K) { return ((size_t)K + 127) / 128 * 128; }       // whole cache lines
 
 }  // namespace
 
@@ -107,7 +107,7 @@ int xnor_int8_linear_workspace_bytes(long long M, int K, size_t *bytes)
 {
     if (!bytes) return XNOR_E_NULL;
     if (M < 0 || M > kMaxRows || K <= 0 || K > kMaxInt8Cols) return XNOR_E_SHAPE;
-    *bytes = (size_t)M * q_stride_of(K) + (size_t)M * sizeof(float);
+    *bytes = dense_few_real_supports(M, K) ? 0 : (size_t)M * q_stride_of(K) + (size_t)M * sizeof(float);
     return XNOR_OK;
 }
 
@@ -117,14 +117,14 @@ int xnor_int8_linear(const void *x, int x_type, long long x_stride, const int8_t
 {
     const int xs = value_size(x_type), os = value_size(out_type);
     if (!xs || !os) return XNOR_E_UNSUPPORTED;
-    const Matrix all[] = {{x, M, K, x_stride, xs, false}, {w, N, K, w_stride, 1, false}, vec(w_scale, N, 4), {out, M, N, out_stride, os, true},
-                          vec(workspace, M, 16)};
-    if (const int rc = check(all)) return rc;
-    if (!aligned(bias, 4)) return XNOR_E_ALIGN;
     size_t need;
     if (const int rc = xnor_int8_linear_workspace_bytes(M, K, &need)) return rc;
+    const Matrix all[] = {{x, M, K, x_stride, xs, false}, {w, N, K, w_stride, 1, false}, vec(w_scale, N, 4), {out, M, N, out_stride, os, true},
+                          vec(workspace, need ? M : 0, 16)};
+    if (const int rc = check(all)) return rc;
+    if (!aligned(bias, 4)) return XNOR_E_ALIGN;
     if (workspace_bytes < need) return XNOR_E_WORKSPACE;
-    if (M > 0 && dense_few_real_supports(M, K)) {
+    if (M > 0 && need == 0) {
         DenseArgs d{};
         d.a = x, d.lda = x_stride * xs, d.b = w, d.ldb = w_stride, d.b_scale = w_scale, d.bias = bias;
         d.M = M, d.N = N, d.K = K, d.out = out, d.ldo = out_stride;
@@ -187,23 +187,41 @@ int xnor_layer_norm_bwd(const void *dy, long long dy_stride, const void *x, int 
 int xnor_gated_fwd(const void *x, int type, long long x_stride, const void *wg, const void *wu, long long w_stride, int act, long long M, int F,
                    int K, void *h, long long h_stride, void *g, void *u, long long gu_stride, void *stream)
 {
+    return xnor_gated_fwd_ws(x, type, x_stride, wg, wu, w_stride, act, M, F, K, h, h_stride, g, u, gu_stride, nullptr, 0, stream);
+}
+
+int xnor_gated_fwd_workspace_bytes(long long M, int F, int K, long long x_stride, long long w_stride, size_t *bytes)
+{
+    if (!bytes) return XNOR_E_NULL;
+    if (M < 0 || M > kMaxRows || F <= 0 || F > kMaxCols || K <= 0 || K > kMaxCols || x_stride < 0 || w_stride < 0) return XNOR_E_SHAPE;
+    *bytes = (x_stride % 8 || w_stride % 8) && gated_fwd_copy_pays(M, F, K) ? gated_fwd_workspace(M, F, K) : 0;
+    return XNOR_OK;
+}
+
+int xnor_gated_fwd_ws(const void *x, int type, long long x_stride, const void *wg, const void *wu, long long w_stride, int act, long long M, int F,
+                      int K, void *h, long long h_stride, void *g, void *u, long long gu_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
     if (value_size(type) != 2 || !known_act(act)) return XNOR_E_UNSUPPORTED;
     if (M > 0 && !g != !u) return XNOR_E_NULL;
     const long long kept = g ? M : 0;
     const Matrix all[] = {{x, M, K, x_stride, 2, false}, {wg, F, K, w_stride, 2, false}, {wu, F, K, w_stride, 2, false}, {h, M, F, h_stride, 2, true},
                           {g, kept, F, g ? gu_stride : F, 2, true}, {u, kept, F, g ? gu_stride : F, 2, true}};
     if (const int rc = check(all)) return rc;
+    if (!aligned(workspace, 16)) return XNOR_E_ALIGN;
     DenseArgs d{};
     d.a = x, d.lda = 2 * x_stride, d.b = wg, d.b2 = wu, d.ldb = 2 * w_stride, d.act = act;
     d.M = M, d.N = F, d.K = K, d.out = h, d.ldo = h_stride, d.out2 = g, d.out3 = u, d.ldo2 = gu_stride;
+    if (workspace && !dense_direct_supports(d, type) && gated_fwd_copy_pays(M, F, K) && workspace_bytes >= gated_fwd_workspace(M, F, K)) {
+        const hipError_t e = gated_fwd_copy(&d, workspace, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_status(e);
+    }
     return hip_status(launch_dense_gated(d, type, (hipStream_t)stream));
 }
 
 int xnor_gated_bwd_workspace_bytes(long long M, int F, int K, size_t *bytes)
 {
     if (!bytes) return XNOR_E_NULL;
-    // (a launch's operand is [M][2 F], its rows taken as one contraction)
-    if (M < 0 || M > kMaxRows || F <= 0 || F > kMaxCols / 2 || K <= 0 || K > kMaxCols) return XNOR_E_SHAPE;
+    if (M < 0 || M > kMaxRows || F <= 0 || F > kMaxGatedBack || K <= 0 || K > kMaxGatedBack) return XNOR_E_SHAPE;
     *bytes = gated_bwd_workspace(M, F, K);
     return XNOR_OK;
 }

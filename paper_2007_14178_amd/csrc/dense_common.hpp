@@ -135,8 +135,8 @@ __device__ inline float act_slope(float g)
     return g > 0.f ? 1.f : (g != g ? g : 0.f);
 }
 
-// One product of the dense operators: out[m][n] = sum_k a[m][k] b[n][k], both operands with the contraction along their rows.
-// Strides of a and b are in bytes, of outputs in values.
+// One product of the dense operators: out[m][n] = sum_k a[m][k] b[n][k], both operands with the contraction along their rows (or
+// across them: launch_dense_across).  Strides of a and b are in bytes, of outputs in values.
 struct DenseArgs {
     const void *a;              // [M][K]
     const void *b, *b2;         // [N][K]; b2: the gated block's second matrix
@@ -145,7 +145,9 @@ struct DenseArgs {
     int N, K;                   // K in values
     void *out, *out2, *out3;    // gated: h, and g and u or NULL.  Plain: rows from `split` on go to out2
     long long ldo, ldo2;
-    long long split, valid;     // plain: of the rows of either output the first `valid` are written
+    long long split, valid;     // plain: of the rows of either output the first `valid` are written, and of a row `out_cols` values
+    int out_cols;
+    int seam, deep;             // b across: contraction values from `seam` on are b2's rows, of which, as of b's, there are `deep`
     const float *a_scale, *b_scale, *b2_scale, *bias;
     int act;
     long long first;            // (set by the launchers: the launch's first token)
@@ -153,7 +155,11 @@ struct DenseArgs {
 
 constexpr long long kMaxBlocks = 1 << 22;      // of a launch, for up to 1024 threads each: fewer than 2^32 threads
 
-hipError_t launch_dense(const DenseArgs &p, int type, hipStream_t st);                       // 16-bit: out = a b^T
+// 16-bit out = a b^T with b as [K][N], and a as [M][K] or [K][M] (a_across): rows at multiples of 16 bytes, N and (a_across) M of 8 values,
+// a stride of b that holds its rows; seam a multiple of 64 values.  Rows of 64 contraction values within 31 bits.
+hipError_t launch_dense_across(const DenseArgs &p, bool a_across, int type, hipStream_t st);
+// Whether the products' rows are where the fast kernels take them (16-byte boundaries); elsewhere they run slower.
+bool dense_direct_supports(const DenseArgs &p, int type);
 hipError_t launch_dense_gated(const DenseArgs &p, int type, hipStream_t st);                 // 16-bit
 hipError_t launch_dense_int8(const DenseArgs &p, int out_type, hipStream_t st);
 hipError_t launch_dense_int8_gated(const DenseArgs &p, int out_type, hipStream_t st);
@@ -196,7 +202,12 @@ struct GatedBackArgs {
     void *dx, *dwg, *dwu;
     void *workspace;
 };
+constexpr int kMaxGatedBack = 1 << 20;         // F and K of the backward pass: 255 rows of [dg du] within 31 bits
+size_t gated_fwd_workspace(long long M, int F, int K);
+bool gated_fwd_copy_pays(long long M, int F, int K);
 size_t gated_bwd_workspace(long long M, int F, int K);
+// The operands of a gated product copied to 16-byte boundaries in `workspace`, and p changed to them.
+hipError_t gated_fwd_copy(DenseArgs *p, void *workspace, hipStream_t st);
 hipError_t launch_gated_bwd(const GatedBackArgs &p, int type, hipStream_t st);
 
 }  // namespace xnor

@@ -174,8 +174,6 @@ template hipError_t launch_few<int8_t, f16_t, kInt8Gated>(const DenseArgs &, hip
 template hipError_t launch_few<int8_t, bf16_t, kInt8Gated>(const DenseArgs &, hipStream_t);
 template hipError_t launch_few<f16_t, f16_t, kGated>(const DenseArgs &, hipStream_t);
 template hipError_t launch_few<bf16_t, bf16_t, kGated>(const DenseArgs &, hipStream_t);
-template hipError_t launch_few<f16_t, f16_t, kPlain>(const DenseArgs &, hipStream_t);
-template hipError_t launch_few<bf16_t, bf16_t, kPlain>(const DenseArgs &, hipStream_t);
 
 bool dense_few_real_supports(long long M, int K)
 {

@@ -12,42 +12,47 @@
 namespace xnor {
 namespace {
 
-// 128 tokens x 128 rows of b, four waves of 64 x 64, rows of any alignment and length staged through registers.
+// 128 tokens x 128 rows of b, four waves of 64 x 64, rows of any alignment and length staged through registers: a step's rows are on
+// their way while the one before is worked on.
 template <class T, class O, int EPI>
 __global__ __launch_bounds__(256, 2) void dense_tile_kernel(const DenseArgs p, int tiles_n)
 {
     constexpr bool GATED = EPI == kGated || EPI == kInt8Gated;
     constexpr int TN = GATED ? 64 : 128;        // outputs n of a tile
     typedef Mat<T> X;
-    __shared__ __align__(16) char lds[2 * 128 * kStep];
-    char *la = lds, *lb = lds + 128 * kStep;
+    __shared__ __align__(16) char lds[2][2 * 128 * kStep];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int n0 = (int)(blockIdx.x % (unsigned)tiles_n) * TN;
     const long long m0 = p.first + (long long)(blockIdx.x / (unsigned)tiles_n) * 128;
     const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
 
     typename X::acc acc[4][4] = {};
-    const int steps = (int)(((long long)p.K * (int)sizeof(T) + kStep - 1) / kStep);
-    for (int s = 0; s < steps; ++s) {
-        i32x4 va[4], vb[4];
-        const int chunk = t & 7, at = (s * kStep + chunk * 16) / (int)sizeof(T);
+    const int steps = (int)(((long long)p.K * (int)sizeof(T) + kStep - 1) / kStep), chunk = t & 7;
+    const T *a[4], *b[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = (t >> 3) + 32 * i;
-            const long long m = m0 + r < p.M ? m0 + r : p.M - 1;
-            const Chunk<T> ca = load_chunk((const T *)((const char *)p.a + m * p.lda), at, p.K);
-            const Chunk<T> cb = load_chunk((const T *)b_row<GATED>(p, n0, r), at, p.K);
-            va[i] = __builtin_bit_cast(i32x4, ca);
-            vb[i] = __builtin_bit_cast(i32x4, cb);
-        }
-        __syncthreads();
+    for (int i = 0; i < 4; ++i) {
+        const int r = (t >> 3) + 32 * i;
+        a[i] = (const T *)((const char *)p.a + min(m0 + r, p.M - 1) * p.lda);
+        b[i] = (const T *)b_row<GATED>(p, n0, r);
+    }
+    Chunk<T> va[4], vb[4];
+    auto fetch = [&](int s) __attribute__((always_inline)) {
+        const int at = (s * kStep + chunk * 16) / (int)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) va[i] = load_chunk(a[i], at, p.K), vb[i] = load_chunk(b[i], at, p.K);
+    };
+    if (steps > 0) fetch(0);
+    for (int s = 0; s < steps; ++s) {
+        char *const la = lds[s & 1], *const lb = la + 128 * kStep;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = (t >> 3) + 32 * i, to = r * kStep + ((chunk ^ (r & 7)) << 4);
-            *(i32x4 *)(la + to) = va[i];
-            *(i32x4 *)(lb + to) = vb[i];
+            *(i32x4 *)(la + to) = __builtin_bit_cast(i32x4, va[i]);
+            *(i32x4 *)(lb + to) = __builtin_bit_cast(i32x4, vb[i]);
         }
-        __syncthreads();
+        if (s + 1 < steps) fetch(s + 1);
+        // (LDS alone is waited for: the fetches are not)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             i32x4 fa[4], fb[4];
@@ -98,6 +103,29 @@ constexpr int kFetches = 2;
 
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) void lds_void;
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t lds_short4;
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+// Eight bytes of each of 16 lanes are four rows of 16 values: lane i gets the four of column i.
+__device__ inline i32x2 read_transposed(const lds_char *from)
+{
+#ifdef __HIP_DEVICE_COMPILE__        // (the host's pass does not know the builtin)
+    return __builtin_bit_cast(i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4 *)from));
+#else
+    return i32x2{};
+#endif
+}
+
+// 16 bytes a lane from a buffer straight into LDS, the wave's 1024 from `to` on.  As an instruction of our own beside transposing reads:
+// before each of these the compiler would wait for all such fetches of its builtin.  (Nothing else in these kernels uses m0.)
+template <class Rsrc>
+__device__ inline void fetch_16(Rsrc rsrc, int at, int from, lds_char *to)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"((uint32_t)(uintptr_t)to), "v"(at), "s"(rsrc), "s"(from) : "memory");
+#endif
+}
 
 // Row r of b's part `half`: each wave's 32 rows of both parts are 64 consecutive ones of the tile, so that a wave's outputs of a token
 // are 64 consecutive values.
@@ -116,8 +144,8 @@ __device__ inline bool tile_of(const TileMap &t, int *tm, int *tn)
     if ((blockIdx.x >> 3) >= eighth || i >= t.tiles) return false;
     const int rows = (int)(t.tiles / t.tiles_n), group = (int)(i / (8 * t.tiles_n)), in = (int)(i - (long long)group * 8 * t.tiles_n);
     const int high = min(8, rows - group * 8);
-    *tn = in / high;
-    *tm = group * 8 + in % high;
+    *tn = __builtin_amdgcn_readfirstlane(in / high);         // (a quotient is a vector register otherwise)
+    *tm = __builtin_amdgcn_readfirstlane(group * 8 + in % high);
     return true;
 }
 
@@ -134,10 +162,19 @@ typedef Shape<2, 4, 2, 1> Large;
 typedef Shape<2, 2, 2, 1> Medium;
 typedef Shape<2, 2, 2, 2> Split;
 
-template <class T, class O, int EPI, class S>
+//
+// TA, TB: that operand (of 16-bit values) lies with the contraction across its rows, as [K][M] or [K][N].  A part of it is then 64 rows
+// of P values, and the transposing reads of LDS hand a lane its eight values along the contraction.  32 values c of row k stand
+// at place c ^ across_key(k), which spreads the rows of one read over the banks.  Rows behind the contraction's end are beyond what
+// the buffer's descriptor admits and arrive as zeros.
+__device__ inline int across_key(int k, int places) { return places == 8 ? (k & 3) | (k >> 3 & 1) << 2 : (k >> 1 & 1) | (k >> 3 & 1) << 1; }
+
+template <class T, class O, int EPI, class S, bool TA = false, bool TB = false>
 __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu_waves_per_eu(2, 2))) void dense_direct_kernel(const DenseArgs p, const TileMap map)
 {
     constexpr bool GATED = EPI == kGated || EPI == kInt8Gated;
+    constexpr int PITCH = S::ROWS * 2, PLACES = PITCH / 32, DEEP = kStep / 2;       // operands across: bytes of a row, its places, rows of a step
+    static_assert(!TA || TB, "");
     constexpr int ROWS = S::ROWS, RM = S::RM, RN = S::RN, kPart = S::kPart, kBuffer = S::kBuffer, STEPS = S::STEPS;
     typedef Mat<T> X;
     typedef typename X::acc Acc;
@@ -152,13 +189,14 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
     const int n0 = tn * (GATED ? ROWS : 2 * ROWS);
     const int wm = wave % S::WM * RM * 16, wn = wave / S::WM * RN * 16;
     // A group's whole steps; what is left over, whole or not, is a step more for some groups, through registers.
-    const int bytes = p.K * (int)sizeof(T), steps = bytes / kStep / S::GROUPS, first = group * steps;
-    const int rest = S::GROUPS * steps, left = (bytes + kStep - 1) / kStep - rest;
+    // (Operands across have no such step.)
+    const int bytes = p.K * (int)sizeof(T), whole = (bytes + (TB ? kStep - 1 : 0)) / kStep, steps = (whole + (TB ? S::GROUPS - 1 : 0)) / S::GROUPS;
+    const int first = group * steps, rest = S::GROUPS * steps, left = TB ? 0 : (bytes + kStep - 1) / kStep - rest;
 
     // Fetches: instruction i of a wave fills rows 16 wave + 8 i + lane / 8 of a part, and the lane brings the 16 bytes that
     // belong at its place: chunk c of row r stands at place c ^ (r & 7), which spreads a column of rows over the banks.
-    const char *const from_a = (const char *)p.a + m0 * p.lda;
-    const char *const from_b[2] = {(const char *)p.b + (long long)n0 * p.ldb, (const char *)(GATED ? p.b2 : p.b) + (long long)n0 * p.ldb};
+    const char *const from_a = (const char *)p.a + m0 * (TA ? 2 : p.lda);
+    const char *const from_b[2] = {(const char *)p.b + n0 * (TB ? 2 : p.ldb), (const char *)(p.b2 ? p.b2 : p.b) + n0 * (TB ? 2 : p.ldb)};
     const int last_m = (int)min(p.M - 1 - m0, 2LL * ROWS - 1), last_n = min(p.N - 1 - n0, (GATED ? 1 : 2) * ROWS - 1);
     const auto rsrc_a = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_a), 0, (int)(last_m * p.lda + bytes), 0x00027000);
     const auto rsrc_b0 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_b[0]), 0, (int)(last_n * p.ldb + bytes), 0x00027000);
@@ -169,37 +207,73 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
 #pragma unroll
         for (int i = 0; i < kFetches; ++i) {
             const int row = 16 * wave + 8 * i + (lane >> 3), chunk = ((lane & 7) ^ (lane >> 3)) * 16;
-            at_a[h][i] = min(h * ROWS + row, last_m) * (int)p.lda + chunk;
-            at_b[h][i] = min(GATED ? row : b_row_of(h, row), last_n) * (int)p.ldb + chunk;
+            const int l = (2 * wave + i) * 1024 + lane * 16, k = l / PITCH, c = ((l % PITCH / 16) ^ across_key(k, PLACES) << 1) * 8;
+            // (operands across: 8 | M, N, so that the last 8 columns of a tile are whole)
+            at_a[h][i] = TA ? k * (int)p.lda + min(h * ROWS + c, last_m - 7) * 2 : min(h * ROWS + row, last_m) * (int)p.lda + chunk;
+            at_b[h][i] = TB ? k * (int)p.ldb + min(b_row_of(h, c), last_n - 7) * 2 : min(GATED ? row : b_row_of(h, row), last_n) * (int)p.ldb + chunk;
         }
     lds_char *const lds_wave = (lds_char *)lds + 16 * wave * kStep;
     // Part `part` (A0, A1, B0, B1) of a step into its buffer; of a step behind the last one, which nothing reads, the last one's.
     auto fetch = [&](auto part, int step) __attribute__((always_inline)) {
         constexpr int PART = decltype(part)::value;
         lds_char *const to = lds_wave + (step & (STEPS - 1)) * kBuffer + PART * kPart;
-        const int k = (first + min(step, steps - 1)) * kStep;
+        const int at_step = first + min(step, steps - 1);
+        if constexpr (PART < 2 ? TA : TB) {
+            const int k = at_step * DEEP;
+            const bool second = PART >= 2 && k >= p.seam;
+            // DEEP rows from `row` on: those that there are, up to the tile's last column
+            const long long ld = PART < 2 ? p.lda : p.ldb;
+            const int row = second ? k - p.seam : k, there = min(max((PART < 2 ? p.K : p.deep) - row, 0), DEEP);
+            const int short_by = (int)ld - ((PART < 2 ? last_m : last_n) + 1) * 2;          // (the last row's columns end with the tile's)
+            const int size = __builtin_amdgcn_readfirstlane(max(there * (int)ld - short_by, 0));
+            const char *const from = (PART < 2 ? from_a : from_b[second]) + row * ld;
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from), 0, size, 0x00027000);
 #pragma unroll
-        for (int i = 0; i < kFetches; ++i) {
-            const int at = PART < 2 ? at_a[PART & 1][i] : at_b[PART & 1][i];
-            const auto rsrc = PART < 2 ? rsrc_a : PART == 2 ? rsrc_b0 : rsrc_b1;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void *)(to + i * 8 * kStep), 16, at, k, 0, 0);
+            for (int i = 0; i < kFetches; ++i)
+                fetch_16(rsrc, PART < 2 ? at_a[PART & 1][i] : at_b[PART & 1][i], 0, to + i * 8 * kStep);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kFetches; ++i) {
+                const int at = PART < 2 ? at_a[PART & 1][i] : at_b[PART & 1][i];
+                const auto rsrc = PART < 2 ? rsrc_a : PART == 2 ? rsrc_b0 : rsrc_b1;
+                if constexpr (TB) fetch_16(rsrc, at, at_step * kStep, to + i * 8 * kStep);
+                else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void *)(to + i * 8 * kStep), 16, at, at_step * kStep, 0, 0);
+            }
         }
     };
     // The lane's places in a part for the two halves of a step; a fragment is 16 rows further on.
     const uint32_t place0 = r * kStep + ((g ^ (r & 7)) << 4), place1 = place0 ^ 64;
+    // ... and in a part of an operand across: four lanes a row of 16 values, four rows 16 lanes.
+    const uint32_t across_row = (g * 8 + (r >> 2)) * PITCH + (r & 3) * 8, key = across_key(g * 8 + (r >> 2), PLACES);
+    auto read_across = [&](const char *part, int fragment, i32x4 (&to)[2]) __attribute__((always_inline)) {
+        const lds_char *const from = (const lds_char *)part + across_row + ((fragment ^ key) << 5);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const i32x2 low = read_transposed(from + h * 32 * PITCH), high = read_transposed(from + (h * 32 + 4) * PITCH);
+            to[h] = i32x4{low.x, low.y, high.x, high.y};
+        }
+    };
     i32x4 a[2][RM][2], b[2][RN][2];
     auto read_a = [&](int h, int step) __attribute__((always_inline)) {
-        const char *part = lds + (step & (STEPS - 1)) * kBuffer + h * kPart + wm * kStep;
+        const char *const all = lds + (step & (STEPS - 1)) * kBuffer + h * kPart, *const part = all + wm * kStep;
 #pragma unroll
         for (int j = 0; j < RM; ++j) {
+            if constexpr (TA) {
+                read_across(all, wm / 16 + j, a[h][j]);
+                continue;
+            }
             a[h][j][0] = *(const i32x4 *)(part + place0 + j * 16 * kStep);
             a[h][j][1] = *(const i32x4 *)(part + place1 + j * 16 * kStep);
         }
     };
     auto read_b = [&](int h, int step) __attribute__((always_inline)) {
-        const char *part = lds + (step & (STEPS - 1)) * kBuffer + (2 + h) * kPart + wn * kStep;
+        const char *const all = lds + (step & (STEPS - 1)) * kBuffer + (2 + h) * kPart, *const part = all + wn * kStep;
 #pragma unroll
         for (int j = 0; j < RN; ++j) {
+            if constexpr (TB) {
+                read_across(all, wn / 16 + j, b[h][j]);
+                continue;
+            }
             b[h][j][0] = *(const i32x4 *)(part + place0 + j * 16 * kStep);
             b[h][j][1] = *(const i32x4 *)(part + place1 + j * 16 * kStep);
         }
@@ -275,7 +349,7 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
         }
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
     }
-    if (left > 0) {         // the contraction's end
+    if (!TB && left > 0) {         // the contraction's end, through registers
         const int chunk = t & 7, at = ((rest + group) * kStep + chunk * 16) / (int)sizeof(T);       // (zeros behind it)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -353,7 +427,7 @@ bool direct_supports(const DenseArgs &p, int size)
     return fits(p.a, p.lda) && fits(p.b, p.ldb) && (!p.b2 || fits(p.b2, p.ldb));
 }
 
-template <class T, class O, int EPI, class S>
+template <class T, class O, int EPI, class S, bool TA = false, bool TB = false>
 hipError_t launch_direct(const DenseArgs &p, hipStream_t st)
 {
     static std::atomic<bool> raised[64];
@@ -361,7 +435,7 @@ hipError_t launch_direct(const DenseArgs &p, hipStream_t st)
     hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
     if (dev < 0 || dev >= 64 || !raised[dev].load(std::memory_order_relaxed)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_direct_kernel<T, O, EPI, S>), hipFuncAttributeMaxDynamicSharedMemorySize, S::GROUPS * S::kLds);
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_direct_kernel<T, O, EPI, S, TA, TB>), hipFuncAttributeMaxDynamicSharedMemorySize, S::GROUPS * S::kLds);
         if (e != hipSuccess) return e;
         if (dev >= 0 && dev < 64) raised[dev].store(true, std::memory_order_relaxed);
     }
@@ -374,7 +448,7 @@ hipError_t launch_direct(const DenseArgs &p, hipStream_t st)
         q.first = m;
         q.M = std::min(p.M, m + rows);
         map.tiles = map.tiles_n * ((q.M - m + TM - 1) / TM);
-        dense_direct_kernel<T, O, EPI, S><<<dim3((unsigned)((map.tiles + 7) / 8 * 8)), dim3(S::GROUPS * S::WAVES * kWave), S::GROUPS * S::kLds, st>>>(q, map);
+        dense_direct_kernel<T, O, EPI, S, TA, TB><<<dim3((unsigned)((map.tiles + 7) / 8 * 8)), dim3(S::GROUPS * S::WAVES * kWave), S::GROUPS * S::kLds, st>>>(q, map);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -398,37 +472,54 @@ hipError_t launch_tiles(const DenseArgs &p, hipStream_t st)
     return hipSuccess;
 }
 
+// By which tiles: `small` and `large` of them of 128 x 128 and 256 x 256.  Where a unit gets no more than one small one, two groups of
+// waves share its contraction (256 x 4096 x 4096 8 bits 17.0 us, without 19.8).  Else by what the rounds of workgroups take, in steps of a
+// large tile: one of these a unit, or two small ones at 0.56 of the time, a step; and some time for the tile's begin and end, which
+// only two workgroups on a unit overlap.  (2048 x 4096 x 4096 8 bits 38.7 us on small tiles, 49.5 on large ones; 4096 x 4096 x 4096 70.5 and 67.9;
+// 6144: 104 and 110; 16-bit gated block of 3584 x 4096 x 4096 209 and 195; 100352 x 512 x 512 8 bits 65 and 71.)
+enum Tiles { kSplit, kMedium, kLarge };
+Tiles tiles_of(long long small, long long large, double steps)
+{
+    const long long units = compute_units();
+    if (small <= units) return kSplit;
+    const double small_time = (double)((small + 2 * units - 1) / (2 * units)) * (0.56 * steps + 2.5);
+    const double large_time = (double)((large + units - 1) / units) * (steps + 5);
+    return small_time < large_time ? kMedium : kLarge;
+}
+
+template <class T, class O, int EPI, bool TA = false, bool TB = false>
+hipError_t launch_by_tiles(const DenseArgs &p, hipStream_t st)
+{
+    constexpr int MATS = EPI == kGated || EPI == kInt8Gated ? 2 : 1;
+    const long long small = ((p.M + 127) / 128) * ceil_div((long long)p.N * MATS, 128), large = ((p.M + 255) / 256) * ceil_div((long long)p.N * MATS, 256);
+    switch (tiles_of(small, large, (double)p.K * sizeof(T) / kStep)) {
+        case kSplit: return launch_direct<T, O, EPI, Split, TA, TB>(p, st);
+        case kMedium: return launch_direct<T, O, EPI, Medium, TA, TB>(p, st);
+        default: return launch_direct<T, O, EPI, Large, TA, TB>(p, st);
+    }
+}
+
 // Which kernel.  Up to 16 tokens the one that reads b once; up to 64 too where it has no more than a workgroup a unit (each of them reads
 // all tokens: 64 tokens x 4096 x 4096 12.3 us, on tiles 16.8; x 8192 x 8192 41 us, 28) or rows that the fetches into LDS do not take.
-// Then by tiles of 128 x 128: where a unit gets no more than one, two groups of waves share its contraction (256 x 4096 x 4096
-// 8 bits 17.0 us, without 19.8).  Else by what the rounds of workgroups take, in steps of a 256 x 256 tile: one tile of these a unit, or two
-// of a quarter at 0.56 of the time, a step; and some time for the tile's begin and end, which only two workgroups on a unit overlap.
-// (2048 x 4096 x 4096 8 bits 38.7 us on small tiles, 49.5 on large ones; 4096 x 4096 x 4096 70.5 and 67.9; 6144: 104 and 110; 16-bit gated block of
-// 3584 x 4096 x 4096 209 and 195; 100352 x 512 x 512 8 bits 65 and 71.)
 template <class T, class O, int EPI>
 hipError_t launch(const DenseArgs &p, hipStream_t st)
 {
-    constexpr bool GATED = EPI == kGated || EPI == kInt8Gated;
     if (p.M == 0) return hipSuccess;
     const bool direct = direct_supports(p, sizeof(T));
-    const long long units = compute_units();
-    if (p.M <= 16 || (p.M <= kFewTokens && (!direct || p.N <= 16 * units))) return launch_few<T, O, EPI>(p, st);
-    if (!direct) return launch_tiles<T, O, EPI>(p, st);
-    const int n = GATED ? 2 : 1;        // matrices
-    const long long small = ((p.M + 127) / 128) * ceil_div((long long)p.N * n, 128), large = ((p.M + 255) / 256) * ceil_div((long long)p.N * n, 256);
-    if (small <= units) return launch_direct<T, O, EPI, Split>(p, st);
-    const double steps = (double)p.K * sizeof(T) / kStep;
-    const double small_time = (double)((small + 2 * units - 1) / (2 * units)) * (0.56 * steps + 2.5);
-    const double large_time = (double)((large + units - 1) / units) * (steps + 5);
-    return small_time < large_time ? launch_direct<T, O, EPI, Medium>(p, st) : launch_direct<T, O, EPI, Large>(p, st);
+    if (p.M <= 16 || (p.M <= kFewTokens && (!direct || p.N <= 16 * compute_units()))) return launch_few<T, O, EPI>(p, st);
+    return direct ? launch_by_tiles<T, O, EPI>(p, st) : launch_tiles<T, O, EPI>(p, st);
 }
 
 }  // namespace
 
-hipError_t launch_dense(const DenseArgs &p, int type, hipStream_t st)
+hipError_t launch_dense_across(const DenseArgs &p, bool a_across, int type, hipStream_t st)
 {
-    return type == XNOR_TYPE_F16 ? launch<f16_t, f16_t, kPlain>(p, st) : launch<bf16_t, bf16_t, kPlain>(p, st);
+    if (p.M == 0) return hipSuccess;
+    if (type == XNOR_TYPE_F16) return a_across ? launch_by_tiles<f16_t, f16_t, kPlain, true, true>(p, st) : launch_by_tiles<f16_t, f16_t, kPlain, false, true>(p, st);
+    return a_across ? launch_by_tiles<bf16_t, bf16_t, kPlain, true, true>(p, st) : launch_by_tiles<bf16_t, bf16_t, kPlain, false, true>(p, st);
 }
+
+bool dense_direct_supports(const DenseArgs &p, int type) { return direct_supports(p, type == XNOR_TYPE_FP32 ? 4 : 2); }
 
 hipError_t launch_dense_gated(const DenseArgs &p, int type, hipStream_t st)
 {

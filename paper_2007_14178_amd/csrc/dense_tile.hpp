@@ -68,7 +68,7 @@ __device__ inline void finish(const DenseArgs &p, long long m, float s, int n, c
         for (int i = 0; i < 4; ++i) out[i] = (O)v[i];
         const bool second = m >= p.split;
         const long long r = second ? m - p.split : m;
-        if (r < p.valid) store_values((O *)(second ? p.out2 : p.out) + r * p.ldo, n, p.N, out);
+        if (r < p.valid) store_values((O *)(second ? p.out2 : p.out) + r * p.ldo, n, p.out_cols, out);
     } else {
         float g[4], u[4];
 #pragma unroll

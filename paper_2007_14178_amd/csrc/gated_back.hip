@@ -1,8 +1,9 @@
-// Backward pass of the gated block h = act(g) u, g = x wg^T, u = x wu^T:
+// Around the gated block's products: rows copied to 16-byte boundaries where the products would read them slowly, and the backward
+// pass of h = act(g) u, g = x wg^T, u = x wu^T:
 //   dg = dh u act'(g)   du = dh act(g)   dx = dg wg + du wu   dwg = dg^T x   dwu = du^T x
-// The products run on the kernel that takes rows along the contraction, so this file lays the operands out so: [dg du] by token
-// and transposed, x and [wg wu] transposed.  dg and du are rounded to the block's type, which the matrix instructions
-// take; everything else is summed in fp32 and rounded once.
+// One pass forms [dg du] by token; the two products read it and the block's own operands as they lie, across their rows where the
+// contraction goes across.  dg and du are rounded to the block's type, which the matrix instructions take; everything
+// else is summed in fp32 and rounded once.
 #include <algorithm>
 
 #include "dense_common.hpp"
@@ -10,179 +11,150 @@
 namespace xnor {
 namespace {
 
-constexpr int kTile = 64;
+size_t pad(long long n, int to) { return (size_t)((n + to - 1) / to * to); }
 
-size_t pad(long long n) { return (size_t)((n + 7) / 8 * 8); }
-
-// A 64 x 64 tile of 16-bit values, written by rows and read by columns.  (A row is 66 values: columns spread over the banks.)
-template <class T>
-struct Tile {
-    T v[kTile][kTile + 2];
+struct Copy {
+    const uint16_t *from;
+    uint16_t *to;
+    long long rows, stride;
 };
 
-// dst[c][r] = tile[r][c] for the tile at (r0, c0) of a matrix of `rows` rows; c below `cols`.
-template <class T>
-__device__ inline void store_transposed(const Tile<T> &tile, T *dst, long long ld, long long r0, long long rows, int c0, int cols)
+// i / n for i < total
+__device__ inline long long row_of(long long i, int n, long long total) { return total >> 32 ? i / n : (long long)((uint32_t)i / (uint32_t)n); }
+
+// Up to three matrices of `cols` 16-bit values a row to rows of `stride` values, whole cache lines (777 x 2501 x 968: products 20 us with, 27 us without); what is behind a row's end is zero.
+__global__ __launch_bounds__(256) void copy_rows_kernel(const Copy a, const Copy b, const Copy c, int cols, int stride)
 {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int c = (threadIdx.x >> 3) + 32 * i, r = (threadIdx.x & 7) * 8;
-        if (c0 + c >= cols || r0 + r >= rows) continue;
-        T out[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) out[k] = tile.v[r + k][c];
-        T *to = dst + (c0 + c) * ld + r0 + r;
-        const int n = (int)min(rows - (r0 + r), 8LL);
-        store_values(to, 0, n, out);
+    const Copy &m = blockIdx.y == 0 ? a : blockIdx.y == 1 ? b : c;
+    const int chunks = stride / 8;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < m.rows * chunks; i += gridDim.x * 256LL) {
+        const long long row = row_of(i, chunks, m.rows * chunks);
+        const int at = (int)(i - row * chunks) * 8;
+        const Chunk<uint16_t> v = load_chunk(m.from + row * m.stride, at, cols);
+        __builtin_memcpy(m.to + row * stride + at, &v, 16);
     }
 }
 
-// dst[c][r] = src[r][c].  `dst_rows` >= cols: rows behind the matrix are zeros.
-template <class T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T *src, long long ld_src, long long rows, int cols, T *dst, long long ld_dst, int tiles_c)
+hipError_t copy_rows(const Copy (&m)[3], int count, int cols, int stride, hipStream_t st)
 {
-    __shared__ Tile<T> tile;
-    const int c0 = (int)(blockIdx.x % (unsigned)tiles_c) * kTile;
-    const long long r0 = (long long)(blockIdx.x / (unsigned)tiles_c) * kTile;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = (threadIdx.x >> 3) + 32 * i, c = (threadIdx.x & 7) * 8;
-        Chunk<T> v{};
-        if (r0 + r < rows && c0 + c < cols) v = load_chunk(src + (r0 + r) * ld_src + c0, c, cols - c0);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) tile.v[r][c + k] = v.v[k];
-    }
-    __syncthreads();
-    store_transposed(tile, dst, ld_dst, r0, rows, c0, cols);
+    long long most = 0;
+    for (int i = 0; i < count; ++i) most = std::max(most, m[i].rows * (stride / 8));
+    if (most == 0) return hipSuccess;
+    const long long blocks = std::min<long long>((most + 255) / 256, 8 * compute_units());
+    copy_rows_kernel<<<dim3((unsigned)blocks, (unsigned)count), dim3(256), 0, st>>>(m[0], m[1], m[2], cols, stride);
+    return hipGetLastError();
 }
 
-// [dg du] by token (row stride 2 fp, zeros behind F in each half) and transposed (rows f and fp + f).
+// [dg du] by token: rows of 2 fp values, zeros behind F in each half.
 template <class T, int ACT>
-__global__ __launch_bounds__(256) void gate_back_kernel(const GatedBackArgs p, T *dgu, T *dgu_t, int fp, long long mp, int tiles_f)
+__global__ __launch_bounds__(256) void gate_back_kernel(const GatedBackArgs p, T *dgu, int fp)
 {
-    __shared__ Tile<T> tg, tu;
-    const int f0 = (int)(blockIdx.x % (unsigned)tiles_f) * kTile;
-    const long long m0 = (long long)(blockIdx.x / (unsigned)tiles_f) * kTile;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = (threadIdx.x >> 3) + 32 * i, c = (threadIdx.x & 7) * 8;
-        const long long m = m0 + r;
+    const int chunks = fp / 8;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < p.M * chunks; i += gridDim.x * 256LL) {
+        const long long m = row_of(i, chunks, p.M * chunks);
+        const int f = (int)(i - m * chunks) * 8;
         T dg[8] = {}, du[8] = {};
-        if (m < p.M && f0 + c < p.F) {
-            const Chunk<T> dh = load_chunk((const T *)p.dh + m * p.dh_stride + f0, c, p.F - f0);
-            const Chunk<T> g = load_chunk((const T *)p.g + m * p.gu_stride + f0, c, p.F - f0);
-            const Chunk<T> u = load_chunk((const T *)p.u + m * p.gu_stride + f0, c, p.F - f0);
+        if (f < p.F) {
+            const Chunk<T> dh = load_chunk((const T *)p.dh + m * p.dh_stride, f, p.F);
+            const Chunk<T> g = load_chunk((const T *)p.g + m * p.gu_stride, f, p.F);
+            const Chunk<T> u = load_chunk((const T *)p.u + m * p.gu_stride, f, p.F);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                if (f0 + c + k >= p.F) break;
+                if (f + k >= p.F) break;
                 const float d = (float)dh.v[k], gv = (float)g.v[k];
                 dg[k] = (T)(d * (float)u.v[k] * act_slope<ACT>(gv));
                 du[k] = (T)(d * act_value<ACT>(gv));
             }
         }
-        if (m < p.M && f0 + c < fp) {
-            __builtin_memcpy(dgu + m * 2 * fp + f0 + c, dg, 16);
-            __builtin_memcpy(dgu + m * 2 * fp + fp + f0 + c, du, 16);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            tg.v[r][c + k] = dg[k];
-            tu.v[r][c + k] = du[k];
-        }
+        __builtin_memcpy(dgu + m * 2 * fp + f, dg, 16);
+        __builtin_memcpy(dgu + m * 2 * fp + fp + f, du, 16);
     }
-    __syncthreads();
-    store_transposed(tg, dgu_t, mp, m0, p.M, f0, fp);
-    store_transposed(tu, dgu_t + (long long)fp * mp, mp, m0, p.M, f0, fp);
 }
 
-// Zeros in columns F .. fp of both halves of w^T's K rows.
-template <class T>
-__global__ __launch_bounds__(256) void clear_pads_kernel(T *wt, int K, int F, int fp)
-{
-    const int i = blockIdx.x * 256 + threadIdx.x, n = fp - F;
-    if (i >= K * 2 * n) return;
-    const int k = i / (2 * n), j = i % (2 * n);
-    wt[(long long)k * 2 * fp + (j / n) * fp + F + j % n] = T(0);
-}
-
-template <class T>
-hipError_t transpose(const T *src, long long ld_src, long long rows, int cols, T *dst, long long ld_dst, hipStream_t st)
-{
-    const int tiles_c = ceil_div(cols, kTile);
-    const long long most = std::max<long long>(1, kMaxBlocks / tiles_c) * kTile;
-    for (long long r = 0; r < rows; r += most) {
-        const long long n = std::min(most, rows - r);
-        transpose_kernel<T><<<dim3((unsigned)(tiles_c * ((n + kTile - 1) / kTile))), dim3(256), 0, st>>>(src + r * ld_src, ld_src, n, cols, dst + r, ld_dst, tiles_c);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
-}
-
+// The workspace: copies of x and the weights for rows that do not lie as the products want them, and [dg du].
 struct Layout {
-    size_t fp, mp, dgu, dgu_t, xt, wt, bytes;
+    size_t fp, kp, x, wg, wu, dgu, bytes;
 };
-Layout layout(long long M, int F, int K)
+Layout layout(long long M, int F, int K, bool backward)
 {
     Layout l;
-    l.fp = pad(F), l.mp = pad(M);
+    l.fp = pad(F, 64), l.kp = pad(K, 64);          // (rows of whole cache lines)
     size_t at = 0;
     auto take = [&](size_t values) { const size_t here = at; at += (values * 2 + 255) / 256 * 256; return here; };
-    l.dgu = take((size_t)M * 2 * l.fp);
-    l.dgu_t = take(2 * l.fp * l.mp);
-    l.xt = take((size_t)K * l.mp);
-    l.wt = take((size_t)K * 2 * l.fp);
+    l.x = take((size_t)M * l.kp);
+    l.wg = take((size_t)F * l.kp);
+    l.wu = take((size_t)F * l.kp);
+    l.dgu = take(backward ? (size_t)M * 2 * l.fp : 0);
     l.bytes = at;
     return l;
 }
 
-template <class T>
-hipError_t run(const GatedBackArgs &p, int type, hipStream_t st)
+// Rows as launch_dense_across takes them.
+bool lies_well(const void *p, long long stride, int K)
 {
-    const Layout l = layout(p.M, p.F, p.K);
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride % 8 == 0 && K % 8 == 0 && stride >= K && stride < (1 << 23);
+}
+
+template <class T>
+hipError_t run(GatedBackArgs p, int type, hipStream_t st)
+{
+    const Layout l = layout(p.M, p.F, p.K, true);
     char *ws = (char *)p.workspace;
-    T *dgu = (T *)(ws + l.dgu), *dgu_t = (T *)(ws + l.dgu_t), *xt = (T *)(ws + l.xt), *wt = (T *)(ws + l.wt);
+    T *dgu = (T *)(ws + l.dgu);
     const int fp = (int)l.fp;
+    int n = p.K;            // columns of the products: K, or K and the zeros behind it in the copies
     hipError_t e;
-    const int tiles_f = ceil_div(fp, kTile);
-    const long long most = std::max<long long>(1, kMaxBlocks / tiles_f) * kTile;
-    for (long long m = 0; m < p.M; m += most) {
-        GatedBackArgs q = p;
-        q.M = std::min(most, p.M - m);
-        q.dh = (const T *)p.dh + m * p.dh_stride;
-        q.g = (const T *)p.g + m * p.gu_stride;
-        q.u = (const T *)p.u + m * p.gu_stride;
-        const dim3 grid((unsigned)(tiles_f * ((q.M + kTile - 1) / kTile)));
-        T *by_token = dgu + m * 2 * fp, *by_unit = dgu_t + m;
-        if (p.act == XNOR_ACT_SILU) gate_back_kernel<T, XNOR_ACT_SILU><<<grid, dim3(256), 0, st>>>(q, by_token, by_unit, fp, (long long)l.mp, tiles_f);
-        else if (p.act == XNOR_ACT_GELU) gate_back_kernel<T, XNOR_ACT_GELU><<<grid, dim3(256), 0, st>>>(q, by_token, by_unit, fp, (long long)l.mp, tiles_f);
-        else gate_back_kernel<T, XNOR_ACT_RELU><<<grid, dim3(256), 0, st>>>(q, by_token, by_unit, fp, (long long)l.mp, tiles_f);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (!lies_well(p.x, p.x_stride, p.K) || !lies_well(p.wg, p.w_stride, p.K) || !lies_well(p.wu, p.w_stride, p.K)) {
+        const Copy copies[3] = {{(const uint16_t *)p.x, (uint16_t *)(ws + l.x), p.M, p.x_stride}, {(const uint16_t *)p.wg, (uint16_t *)(ws + l.wg), p.F, p.w_stride},
+                                {(const uint16_t *)p.wu, (uint16_t *)(ws + l.wu), p.F, p.w_stride}};
+        if ((e = copy_rows(copies, 3, p.K, (int)l.kp, st)) != hipSuccess) return e;
+        p.x = ws + l.x, p.wg = ws + l.wg, p.wu = ws + l.wu;
+        p.x_stride = p.w_stride = (long long)l.kp;
+        n = (int)l.kp;
     }
     if (p.M > 0) {
-        if ((e = transpose((const T *)p.x, p.x_stride, p.M, p.K, xt, (long long)l.mp, st)) != hipSuccess) return e;
-        if ((e = transpose((const T *)p.wg, p.w_stride, p.F, p.K, wt, 2LL * fp, st)) != hipSuccess) return e;
-        if ((e = transpose((const T *)p.wu, p.w_stride, p.F, p.K, wt + fp, 2LL * fp, st)) != hipSuccess) return e;
-        if (fp > p.F) {
-            clear_pads_kernel<T><<<dim3(ceil_div((long long)p.K * 2 * (fp - p.F), 256)), dim3(256), 0, st>>>(wt, p.K, p.F, fp);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
+        const unsigned blocks = (unsigned)std::min<long long>((p.M * (fp / 8) + 255) / 256, 16 * compute_units());
+        if (p.act == XNOR_ACT_SILU) gate_back_kernel<T, XNOR_ACT_SILU><<<dim3(blocks), dim3(256), 0, st>>>(p, dgu, fp);
+        else if (p.act == XNOR_ACT_GELU) gate_back_kernel<T, XNOR_ACT_GELU><<<dim3(blocks), dim3(256), 0, st>>>(p, dgu, fp);
+        else gate_back_kernel<T, XNOR_ACT_RELU><<<dim3(blocks), dim3(256), 0, st>>>(p, dgu, fp);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
         DenseArgs d{};
-        d.a = dgu, d.lda = 4LL * fp, d.b = wt, d.ldb = 4LL * fp;
-        d.M = p.M, d.N = p.K, d.K = 2 * fp;
-        d.out = p.dx, d.ldo = p.dx_stride, d.split = d.valid = p.M;
-        if ((e = launch_dense(d, type, st)) != hipSuccess) return e;
+        d.a = dgu, d.lda = 4LL * fp, d.b = p.wg, d.b2 = p.wu, d.ldb = 2 * p.w_stride;
+        d.M = p.M, d.N = n, d.K = 2 * fp, d.seam = fp, d.deep = p.F;
+        d.out = p.dx, d.ldo = p.dx_stride, d.split = d.valid = p.M, d.out_cols = p.K;
+        if ((e = launch_dense_across(d, false, type, st)) != hipSuccess) return e;
     }
     DenseArgs d{};
-    d.a = dgu_t, d.lda = 2LL * l.mp, d.b = xt, d.ldb = 2LL * l.mp;
-    d.M = 2LL * fp, d.N = p.K, d.K = (int)p.M;
-    d.out = p.dwg, d.out2 = p.dwu, d.ldo = p.dw_stride, d.split = fp, d.valid = p.F;
-    return launch_dense(d, type, st);
+    d.a = dgu, d.lda = 4LL * fp, d.b = p.x, d.ldb = 2 * p.x_stride;
+    d.M = 2LL * fp, d.N = n, d.K = d.deep = (int)p.M, d.seam = 0x7fffffff;
+    d.out = p.dwg, d.out2 = p.dwu, d.ldo = p.dw_stride, d.split = fp, d.valid = p.F, d.out_cols = p.K;
+    return launch_dense_across(d, true, type, st);
 }
 
 }  // namespace
 
-size_t gated_bwd_workspace(long long M, int F, int K) { return layout(M, F, K).bytes; }
+size_t gated_fwd_workspace(long long M, int F, int K) { return layout(M, F, K, false).bytes; }
+size_t gated_bwd_workspace(long long M, int F, int K) { return layout(M, F, K, true).bytes; }
+
+// Products of rows that lie badly take about 0.9 us more a step of 64 values and round of 512 tiles of 128 x 64; the copy takes its launch and 2.7 TB/s
+// read and written.  (16 bits: 777 x 2501 x 1001 27 us either way, 300 x 1000 x 3001 51 and 34 us, 4096 x 4096 x 4095 374 and 241.)
+bool gated_fwd_copy_pays(long long M, int F, int K)
+{
+    if (M <= 64) return false;          // (few tokens: the weights are read once)
+    const double tiles = (double)((M + 127) / 128) * ceil_div(F, 64), rounds = (double)(long long)((tiles + 511) / 512);
+    return rounds * (K / 64.0) * 0.9 > 4.0 + ((double)M + 2.0 * F) * K * 4 / 2.7e6;
+}
+
+hipError_t gated_fwd_copy(DenseArgs *p, void *workspace, hipStream_t st)
+{
+    const Layout l = layout(p->M, p->N, p->K, false);
+    char *ws = (char *)workspace;
+    const Copy copies[3] = {{(const uint16_t *)p->a, (uint16_t *)(ws + l.x), p->M, p->lda / 2}, {(const uint16_t *)p->b, (uint16_t *)(ws + l.wg), p->N, p->ldb / 2},
+                            {(const uint16_t *)p->b2, (uint16_t *)(ws + l.wu), p->N, p->ldb / 2}};
+    p->a = ws + l.x, p->b = ws + l.wg, p->b2 = ws + l.wu;
+    p->lda = p->ldb = 2 * (long long)l.kp;
+    return copy_rows(copies, 3, p->K, (int)l.kp, st);
+}
 
 hipError_t launch_gated_bwd(const GatedBackArgs &p, int type, hipStream_t st)
 {
