@@ -190,8 +190,11 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
     const int wm = wave % S::WM * RM * 16, wn = wave / S::WM * RN * 16;
     // A group's whole steps; what is left over, whole or not, is a step more for some groups, through registers.
     // (Operands across have no such step.)
-    const int bytes = p.K * (int)sizeof(T), whole = (bytes + (TB ? kStep - 1 : 0)) / kStep, steps = (whole + (TB ? S::GROUPS - 1 : 0)) / S::GROUPS;
-    const int first = group * steps, rest = S::GROUPS * steps, left = TB ? 0 : (bytes + kStep - 1) / kStep - rest;
+    // (kSums: a workgroup has one of p.parts shares.)
+    const int part = EPI == kSums ? blockIdx.y : 0;
+    const int bytes = p.K * (int)sizeof(T), whole = (bytes + (TB ? kStep - 1 : 0)) / kStep;
+    const int share = EPI == kSums ? (whole + p.parts - 1) / p.parts : (whole + (TB ? S::GROUPS - 1 : 0)) / S::GROUPS;
+    const int first = (EPI == kSums ? part : group) * share, steps = EPI == kSums ? min(max(whole - first, 0), share) : share, rest = S::GROUPS * steps, left = TB ? 0 : (bytes + kStep - 1) / kStep - rest;
 
     // Fetches: instruction i of a wave fills rows 16 wave + 8 i + lane / 8 of a part, and the lane brings the 16 bytes that
     // belong at its place: chunk c of row r stands at place c ^ (r & 7), which spreads a column of rows over the banks.
@@ -414,7 +417,8 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
             for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
                 for (int i = 0; i < RN; ++i)
-                    if (n[hb][i] < p.N) finish<T, O, EPI>(p, m, scale[ha][j], n[hb][i], columns[hb][i], acc[ha][hb][j][i], acc[ha][GATED ? 1 : hb][j][i]);
+                    if (n[hb][i] < p.N)
+                        finish<T, O, EPI>(p, m + (EPI == kSums ? part * p.M : 0), scale[ha][j], n[hb][i], columns[hb][i], acc[ha][hb][j][i], acc[ha][GATED ? 1 : hb][j][i]);
         }
 }
 
@@ -448,7 +452,7 @@ hipError_t launch_direct(const DenseArgs &p, hipStream_t st)
         q.first = m;
         q.M = std::min(p.M, m + rows);
         map.tiles = map.tiles_n * ((q.M - m + TM - 1) / TM);
-        dense_direct_kernel<T, O, EPI, S, TA, TB><<<dim3((unsigned)((map.tiles + 7) / 8 * 8)), dim3(S::GROUPS * S::WAVES * kWave), S::GROUPS * S::kLds, st>>>(q, map);
+        dense_direct_kernel<T, O, EPI, S, TA, TB><<<dim3((unsigned)((map.tiles + 7) / 8 * 8), EPI == kSums ? p.parts : 1), dim3(S::GROUPS * S::WAVES * kWave), S::GROUPS * S::kLds, st>>>(q, map);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -515,6 +519,7 @@ hipError_t launch(const DenseArgs &p, hipStream_t st)
 hipError_t launch_dense_across(const DenseArgs &p, bool a_across, int type, hipStream_t st)
 {
     if (p.M == 0) return hipSuccess;
+    if (p.parts > 1) return type == XNOR_TYPE_F16 ? launch_direct<f16_t, float, kSums, Medium, false, true>(p, st) : launch_direct<bf16_t, float, kSums, Medium, false, true>(p, st);
     if (type == XNOR_TYPE_F16) return a_across ? launch_by_tiles<f16_t, f16_t, kPlain, true, true>(p, st) : launch_by_tiles<f16_t, f16_t, kPlain, false, true>(p, st);
     return a_across ? launch_by_tiles<bf16_t, bf16_t, kPlain, true, true>(p, st) : launch_by_tiles<bf16_t, bf16_t, kPlain, false, true>(p, st);
 }

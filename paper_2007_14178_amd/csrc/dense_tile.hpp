@@ -5,7 +5,7 @@
 
 namespace xnor {
 
-enum Epilogue { kPlain, kGated, kInt8, kInt8Gated };
+enum Epilogue { kPlain, kGated, kInt8, kInt8Gated, kSums };     // kSums: fp32 sums over a part of the contraction
 
 template <class T> struct Mat;
 template <> struct Mat<int8_t> {
@@ -63,6 +63,10 @@ __device__ inline void finish(const DenseArgs &p, long long m, float s, int n, c
             out[i] = (O)(p.bias ? y + c.bias[i] : y);
         }
         store_values((O *)p.out + m * p.ldo, n, p.N, out);
+    } else if constexpr (EPI == kSums) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = v[i];
+        store_values((O *)p.out + m * p.ldo, n, p.N, out);
     } else if constexpr (EPI == kPlain) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) out[i] = (O)v[i];
@@ -82,7 +86,7 @@ __device__ inline void finish(const DenseArgs &p, long long m, float s, int n, c
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float a = p.act == XNOR_ACT_SILU ? act_value<XNOR_ACT_SILU>(g[i])
+            const float a = p.act == XNOR_ACT_SILU ? act_value<XNOR_ACT_SILU, sizeof(O) == 2>(g[i])
                             : p.act == XNOR_ACT_GELU ? act_value<XNOR_ACT_GELU>(g[i]) : act_value<XNOR_ACT_RELU>(g[i]);
             out[i] = (O)(a * u[i]);
         }

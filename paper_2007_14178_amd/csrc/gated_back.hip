@@ -71,9 +71,39 @@ __global__ __launch_bounds__(256) void gate_back_kernel(const GatedBackArgs p, T
     }
 }
 
+// Shares of the contraction of dx, whose sums are added by another launch: where its tiles of 128 x 128 would leave most of the chip idle,
+// as many as make two workgroups a unit, of four steps of 64 values at least.  (6 tokens x 1152 x 3200 57 us without, 30 us so; 128 x 4096 x 8192 222 and 122.)
+int dx_parts(long long M, int fp, int n)
+{
+    const long long tiles = (M + 127) / 128 * ceil_div(n, 128);
+    const int parts = (int)std::min<long long>(2 * kPlanUnits / std::max(tiles, 1LL), 2 * fp / 64 / 4);
+    return parts >= 3 ? parts : 1;
+}
+
+// out[m][n] = the sum over parts of sums[part][m][n], four values a thread.
+template <class T>
+__global__ __launch_bounds__(256) void add_parts_kernel(const float *sums, int parts, long long M, int n, T *out, long long ldo, int out_cols)
+{
+    const long long total = M * (n / 4);
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < total; i += gridDim.x * 256LL) {
+        const long long m = row_of(i, n / 4, total);
+        const int at = (int)(i - m * (n / 4)) * 4;
+        float v[4] = {};
+        for (int part = 0; part < parts; ++part) {
+            float4 w;
+            __builtin_memcpy(&w, sums + (part * M + m) * n + at, 16);
+            v[0] += w.x, v[1] += w.y, v[2] += w.z, v[3] += w.w;
+        }
+        T to[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) to[k] = (T)v[k];
+        store_values(out + m * ldo, at, out_cols, to);
+    }
+}
+
 // The workspace: copies of x and the weights for rows that do not lie as the products want them, and [dg du].
 struct Layout {
-    size_t fp, kp, x, wg, wu, dgu, bytes;
+    size_t fp, kp, x, wg, wu, dgu, sums, bytes;
 };
 Layout layout(long long M, int F, int K, bool backward)
 {
@@ -85,6 +115,8 @@ Layout layout(long long M, int F, int K, bool backward)
     l.wg = take((size_t)F * l.kp);
     l.wu = take((size_t)F * l.kp);
     l.dgu = take(backward ? (size_t)M * 2 * l.fp : 0);
+    const int parts = backward ? dx_parts(M, (int)l.fp, (int)l.kp) : 1;        // (of the copies' width: the products' own needs no more)
+    l.sums = take(parts > 1 ? 2 * (size_t)parts * M * l.kp : 0);
     l.bytes = at;
     return l;
 }
@@ -122,7 +154,14 @@ hipError_t run(GatedBackArgs p, int type, hipStream_t st)
         d.a = dgu, d.lda = 4LL * fp, d.b = p.wg, d.b2 = p.wu, d.ldb = 2 * p.w_stride;
         d.M = p.M, d.N = n, d.K = 2 * fp, d.seam = fp, d.deep = p.F;
         d.out = p.dx, d.ldo = p.dx_stride, d.split = d.valid = p.M, d.out_cols = p.K;
+        d.parts = dx_parts(p.M, fp, (int)l.kp);
+        if (d.parts > 1) d.out = ws + l.sums, d.ldo = n;
         if ((e = launch_dense_across(d, false, type, st)) != hipSuccess) return e;
+        if (d.parts > 1) {
+            const unsigned blocks = (unsigned)std::min<long long>((p.M * (n / 4) + 255) / 256, 8 * compute_units());
+            add_parts_kernel<T><<<dim3(blocks), dim3(256), 0, st>>>((const float *)(ws + l.sums), d.parts, p.M, n, (T *)p.dx, p.dx_stride, p.K);
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+        }
     }
     DenseArgs d{};
     d.a = dgu, d.lda = 4LL * fp, d.b = p.x, d.ldb = 2 * p.x_stride;

@@ -243,7 +243,28 @@ __global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const Norm
         }
     }
     if (!p.partial) return;
-    float *to = p.partial + ((long long)blockIdx.x * ROWS + threadIdx.x / THREADS) * 2 * p.cols;
+    float *to = p.partial + (long long)blockIdx.x * 2 * p.cols;
+    if constexpr (ROWS > 1) {       // the waves' sums become the workgroup's: wave after wave, in LDS
+        __shared__ float held[2][NV * THREADS * V];
+        for (int w = 0; w < ROWS; ++w) {
+            if ((int)threadIdx.x / THREADS == w) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        const int at = (i * V + k) * THREADS + t;
+                        held[0][at] = w ? held[0][at] + sg[i][k] : sg[i][k];
+                        held[1][at] = w ? held[1][at] + sb[i][k] : sb[i][k];
+                    }
+            }
+            __syncthreads();
+        }
+        if ((int)threadIdx.x >= THREADS) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < V; ++k) sg[i][k] = held[0][(i * V + k) * THREADS + t], sb[i][k] = held[1][(i * V + k) * THREADS + t];
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int at = (t + i * THREADS) * V;
@@ -341,16 +362,18 @@ BackPlan back_plan(int x_type, long long rows, int cols)
     if (chunks <= 128) b.threads = 64, b.nv = chunks <= 64 ? 1 : 2;
     else if (chunks <= 256) b.threads = 256, b.nv = 1;
     else if (chunks <= 512) b.threads = 512, b.nv = 1;
-    else if (chunks <= 4096) b.threads = 1024, b.nv = chunks <= 1024 ? 1 : chunks <= 2048 ? 2 : 4;
+    else if (chunks <= 2048) b.threads = 1024, b.nv = chunks <= 1024 ? 1 : 2;
     if (b.nv == 0) {
         b.blocks = (int)std::min(rows, kMaxBlocks);
         b.parts = (int)std::min<long long>(rows, 64);
         return b;
     }
-    const int rows_a_block = b.threads < kBlock ? kBlock / b.threads : 1;
-    const long long want = std::max<long long>(1, std::min<long long>(2 * kPlanUnits, (rows + rows_a_block * 4 - 1) / (rows_a_block * 4)));
-    b.blocks = (int)want;
-    b.parts = b.blocks * rows_a_block;
+    // Two workgroups a unit, of 256 threads three: their registers, and the parts that they leave, have more run slower
+    // (16384 x 4096 bf16 110 us, with three 131; 16384 x 2048 50 us, with two 57); and four rows a thread, where there are fewer.
+    const int rows_a_block = b.threads < kBlock ? kBlock / b.threads : 1, most = (b.threads == 256 ? 3 : 2) * kPlanUnits;
+    const long long want = std::max<long long>(1, std::min<long long>(most, (rows + rows_a_block * 4 - 1) / (rows_a_block * 4)));
+    b.blocks = (int)want;         // (a part each)
+    b.parts = b.blocks;
     return b;
 }
 
@@ -375,8 +398,7 @@ hipError_t back(const NormBackArgs &p, int x_type, hipStream_t st)
         } else if (b.threads == 512) {
             go(integral_constant<int, 512>(), integral_constant<int, 1>());
         } else {
-            b.nv == 1   ? go(integral_constant<int, 1024>(), integral_constant<int, 1>())
-            : b.nv == 2 ? go(integral_constant<int, 1024>(), integral_constant<int, 2>()) : go(integral_constant<int, 1024>(), integral_constant<int, 4>());
+            b.nv == 1 ? go(integral_constant<int, 1024>(), integral_constant<int, 1>()) : go(integral_constant<int, 1024>(), integral_constant<int, 2>());
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
