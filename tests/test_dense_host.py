@@ -86,6 +86,13 @@ def test_gated_refuses(xb):
     with_bad([OK, 1, 64, OK, OK, 64, 0, 4, 8, 64, OK, 8, OK, OK, 8, None], xb.lib.xnor_gated_fwd, [
         *((k, None, xb.E_NULL) for k in (0, 3, 4, 10, 12, 13)), (1, 0, xb.E_UNSUPPORTED), (6, 3, xb.E_UNSUPPORTED), (7, -1, xb.E_SHAPE),
         (8, 0, xb.E_SHAPE), (9, 0, xb.E_SHAPE), (11, 7, xb.E_SHAPE), (14, 7, xb.E_SHAPE), (0, ODD, xb.E_ALIGN), (4, ODD, xb.E_ALIGN)])
+    # (..., gu_stride, workspace, bytes, stream): a workspace is optional, but has to be aligned
+    with_bad([OK, 1, 64, OK, OK, 64, 0, 4, 8, 64, OK, 8, OK, OK, 8, OK, 64, None], xb.lib.xnor_gated_fwd_ws, [
+        *((k, None, xb.E_NULL) for k in (0, 3, 4, 10, 12, 13)), (1, 0, xb.E_UNSUPPORTED), (9, 0, xb.E_SHAPE), (15, ctypes.c_void_p(0x1008), xb.E_ALIGN)])
+    n = ctypes.c_size_t()
+    assert xb.lib.xnor_gated_fwd_workspace_bytes(4, 8, 64, 64, 64, None) == xb.E_NULL
+    for M, F, K, stride in ((-1, 8, 64, 64), (4, 0, 64, 64), (4, 8, 0, 64), (4, 8, 64, -1)):
+        assert xb.lib.xnor_gated_fwd_workspace_bytes(M, F, K, stride, 64, ctypes.byref(n)) == xb.E_SHAPE
     need = xb.xnor_gated_bwd_workspace_bytes(4, 8, 64)
     # (dh, dh_stride, x, type, x_stride, wg, wu, w_stride, g, u, gu_stride, act, M, F, K, dx, dx_stride, dwg, dwu, dw_stride, workspace, bytes, stream)
     with_bad([OK, 8, OK, 1, 64, OK, OK, 64, OK, OK, 8, 0, 4, 8, 64, OK, 64, OK, OK, 64, OK, need, None], xb.lib.xnor_gated_bwd, [

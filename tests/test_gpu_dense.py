@@ -303,7 +303,7 @@ def test_int8_gated(xb, dtype, kind, M, F, K):
 
 # ---- sizes that fill the chip: some rows and columns of the results ---------------------------------------------------------
 
-LARGE = [(4100, 4200, 128), (4096, 4096, 64), (2100, 8200, 700), (9000, 1100, 1337), (4500, 2049, 2304)]
+LARGE = [(4100, 4200, 128), (4096, 4096, 64), (2100, 8200, 700), (9000, 1100, 1337), (4500, 2049, 2304), (2000, 8100, 1000)]
 
 
 def some(n, block=256):
@@ -347,7 +347,7 @@ def test_large_gated(xb, M, F, K):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16], ids=str)
-@pytest.mark.parametrize("M,F,K", [(4104, 2100, 2104), (2100, 4104, 4100), (9001, 1001, 1000)])
+@pytest.mark.parametrize("M,F,K", [(4104, 2100, 2104), (2100, 4104, 4100), (9001, 1001, 1000), (1500, 300, 2048), (5, 3000, 1200)])
 def test_large_gated_backward(xb, dtype, M, F, K):
     x = rand(1, M, K, dtype=dtype)
     wg, wu = rand(2, F, K, dtype=dtype, std=K ** -0.5), rand(3, F, K, dtype=dtype, std=K ** -0.5)
@@ -361,6 +361,40 @@ def test_large_gated_backward(xb, dtype, M, F, K):
     ref.assert_within(dwu[c.cuda()], want[2], bound[2], "dwu")
     again = xb.xnor_gated_bwd(dh, x, wg, wu, g, u, ref.SILU)
     assert torch.equal(again[0], dx) and torch.equal(again[1], dwg) and torch.equal(again[2], dwu)
+
+
+def test_gated_backward_keeps_to_its_rows(xb):
+    """What lies behind the operands' rows and columns, here infinities, reaches no result: contraction ends inside a step of 64."""
+    M, F, K = 70, 100, 72
+    def inside(rows, cols, seed, **kw):
+        t = torch.full((rows + 3, cols + 8), float("inf"), dtype=BF16, device="cuda")
+        t[:rows, :cols] = rand(seed, rows, cols, dtype=BF16, **kw)
+        return t[:rows, :cols]
+    x, wg, wu, dh, g, u = (inside(r, c, i) for i, (r, c) in enumerate(((M, K), (F, K), (F, K), (M, F), (M, F), (M, F))))
+    got = xb.xnor_gated_bwd(dh, x, wg, wu, g, u)
+    want, bound = ref.gated_back(dh, x, wg, wu, g, u, ref.SILU, BF16)
+    for t, w, e, name in zip(got, want, bound, ("dx", "dwg", "dwu")):
+        ref.assert_within(t, w, e, name)
+    h = xb.xnor_gated_fwd(x, wg, wu)
+    want, bound = ref.gated(x, wg, wu, ref.SILU, BF16)
+    ref.assert_within(h, want[0], bound[0], "h")
+
+
+def test_gated_forward_workspace(xb):
+    """Rows of odd stride, with the copies that a workspace allows and without: the same values."""
+    M, F, K = 300, 400, 3001
+    x, wg, wu = rand(1, M, K, dtype=F16), rand(2, F, K, dtype=F16, std=0.02), rand(3, F, K, dtype=F16, std=0.02)
+    need = xb.xnor_gated_fwd_workspace_bytes(M, F, K, K, K)
+    assert need > 0 and xb.xnor_gated_fwd_workspace_bytes(M, F, K, 3008, 3008) == 0 and xb.xnor_gated_fwd_workspace_bytes(8, F, K, K, K) == 0
+    want, bound = ref.gated(x, wg, wu, ref.GELU, F16)
+    for workspace in (None, torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty(16, dtype=torch.uint8, device="cuda")):
+        got = xb.xnor_gated_fwd(x, wg, wu, ref.GELU, want_pre=True, workspace=workspace)
+        for t, w, e, name in zip(got, want, bound, "hgu"):
+            ref.assert_within(t, w, e, name)
+    # rows of one value apart and all of one row: strides that no fetch of whole chunks takes
+    one = rand(4, 1, K, dtype=F16).expand(M, K)
+    want, bound = ref.gated(one, wg, wu, ref.SILU, F16)
+    ref.assert_within(xb.xnor_gated_fwd(one, wg, wu), want[0], bound[0], "stride 0")
 
 
 # ---- no tokens, long offsets, streams, graphs --------------------------------------------------------------------------
