@@ -17,7 +17,8 @@ template <class T, class O, int EPI, int TT, class X>
 __global__ __launch_bounds__(kThreads) void few_kernel(const DenseArgs p)
 {
     constexpr bool GATED = EPI == kGated || EPI == kInt8Gated, REAL = !std::is_void<X>::value;
-    constexpr int MATS = GATED ? 2 : 1, U = TT < 4 ? 4 : 2;
+    // U: steps whose loads are on their way together (gated, one token x 4096 x 8192 8 bits: 13.6 us, with four 14.9).
+    constexpr int MATS = GATED ? 2 : 1, U = TT < 4 && !GATED ? 4 : 2;
     typedef Mat<T> Mul;
     typedef typename Mul::acc Acc;
     __shared__ Acc sums[kWaves][MATS][TT][kWave];

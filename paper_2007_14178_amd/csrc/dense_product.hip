@@ -291,6 +291,11 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
                 for (int i = 0; i < RN; ++i) acc[ha][hb][j][i] = X::mul(b[hb][i][h], a[ha][j][h], acc[ha][hb][j][i]);
     };
     auto end_phase = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2 * RM * RN; ++i) {         // reads of LDS between the matrix instructions, not before them: 1.5 to 3 %
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        }
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(S::kYoung) : "memory");
         __builtin_amdgcn_sched_barrier(0);
