@@ -188,7 +188,9 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
     const long long m0 = p.first + (long long)tm * 2 * ROWS;
     const int n0 = tn * (GATED ? ROWS : 2 * ROWS);
     const int wm = wave % S::WM * RM * 16, wn = wave / S::WM * RN * 16;
-    // A group's whole steps; what is left over, whole or not, is a step more for some groups, through registers.
+    // A group's whole steps; what is left over, whole or not, is a step more for some groups.  END: it is fetched as the others are, and what
+    // it brings from behind the contraction's end is masked (the eight waves of the large tile have no registers left for that).
+    constexpr bool END = S::WAVES == 4 && !TB;
     // (Operands across have no such step.)
     // (kSums: a workgroup has one of p.parts shares.)
     const int part = EPI == kSums ? blockIdx.y : 0;
@@ -201,9 +203,11 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
     const char *const from_a = (const char *)p.a + m0 * (TA ? 2 : p.lda);
     const char *const from_b[2] = {(const char *)p.b + n0 * (TB ? 2 : p.ldb), (const char *)(p.b2 ? p.b2 : p.b) + n0 * (TB ? 2 : p.ldb)};
     const int last_m = (int)min(p.M - 1 - m0, 2LL * ROWS - 1), last_n = min(p.N - 1 - n0, (GATED ? 1 : 2) * ROWS - 1);
-    const auto rsrc_a = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_a), 0, (int)(last_m * p.lda + bytes), 0x00027000);
-    const auto rsrc_b0 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_b[0]), 0, (int)(last_n * p.ldb + bytes), 0x00027000);
-    const auto rsrc_b1 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_b[1]), 0, (int)(last_n * p.ldb + bytes), 0x00027000);
+    // (END: to the end of the 16 bytes that the last row ends in; rows start at multiples of 16)
+    const int upto = END ? (bytes + 15) & ~15 : bytes;
+    const auto rsrc_a = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_a), 0, (int)(last_m * p.lda + upto), 0x00027000);
+    const auto rsrc_b0 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_b[0]), 0, (int)(last_n * p.ldb + upto), 0x00027000);
+    const auto rsrc_b1 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(from_b[1]), 0, (int)(last_n * p.ldb + upto), 0x00027000);
     int at_a[2][kFetches], at_b[2][kFetches];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -216,11 +220,12 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
             at_b[h][i] = TB ? k * (int)p.ldb + min(b_row_of(h, c), last_n - 7) * 2 : min(GATED ? row : b_row_of(h, row), last_n) * (int)p.ldb + chunk;
         }
     lds_char *const lds_wave = (lds_char *)lds + 16 * wave * kStep;
+    const int last = steps - 1 + (END && group < left ? 1 : 0);
     // Part `part` (A0, A1, B0, B1) of a step into its buffer; of a step behind the last one, which nothing reads, the last one's.
     auto fetch = [&](auto part, int step) __attribute__((always_inline)) {
         constexpr int PART = decltype(part)::value;
         lds_char *const to = lds_wave + (step & (STEPS - 1)) * kBuffer + PART * kPart;
-        const int at_step = first + min(step, steps - 1);
+        const int s = min(step, last), at_step = s < steps ? first + s : rest + group;
         if constexpr (PART < 2 ? TA : TB) {
             const int k = at_step * DEEP;
             const bool second = PART >= 2 && k >= p.seam;
@@ -237,10 +242,11 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
         } else {
 #pragma unroll
             for (int i = 0; i < kFetches; ++i) {
-                const int at = PART < 2 ? at_a[PART & 1][i] : at_b[PART & 1][i];
+                const int at = PART < 2 ? at_a[PART & 1][i] : at_b[PART & 1][i], k = at_step * kStep;
                 const auto rsrc = PART < 2 ? rsrc_a : PART == 2 ? rsrc_b0 : rsrc_b1;
-                if constexpr (TB) fetch_16(rsrc, at, at_step * kStep, to + i * 8 * kStep);
-                else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void *)(to + i * 8 * kStep), 16, at, at_step * kStep, 0, 0);
+                // (END: the whole offset in the lane's own, as a scalar one does not count where the buffer's end is checked)
+                if constexpr (TB) fetch_16(rsrc, at, k, to + i * 8 * kStep);
+                else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void *)(to + i * 8 * kStep), 16, END ? at + k : at, END ? 0 : k, 0, 0);
             }
         }
     };
@@ -306,7 +312,7 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
     const integral_constant<int, 2> B0{};
     const integral_constant<int, 3> B1{};
 
-    if (steps > 0) {
+    if (steps > 0 || (END && left > 0)) {
 #pragma unroll
         for (int s = 0; s < STEPS; s += 2) {
             fetch(A0, s), fetch(B0, s), fetch(B1, s), fetch(A1, s);
@@ -357,8 +363,29 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
         }
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
     }
-    if (!TB && left > 0) {         // the contraction's end, through registers
-        const int chunk = t & 7, at = ((rest + group) * kStep + chunk * 16) / (int)sizeof(T);       // (zeros behind it)
+    if constexpr (END) {
+        if (group < left) {
+            auto masked = [&](i32x4 (&v)[2]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int there = min(max(bytes - ((rest + group) * kStep + (h * 4 + g) * 16 + i * 4), 0), 4);
+                        v[h][i] &= there == 4 ? -1 : (1 << 8 * there) - 1;
+                    }
+            };
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                read_a(h, steps), read_b(h, steps);
+#pragma unroll
+                for (int j = 0; j < RM; ++j) masked(a[h][j]);
+#pragma unroll
+                for (int j = 0; j < RN; ++j) masked(b[h][j]);
+            }
+            multiply(0, 0), multiply(0, 1), multiply(1, 0), multiply(1, 1);
+        }
+    } else if (!TB && left > 0) {       // through registers
+        const int chunk = t & 7, at = (rest * kStep + chunk * 16) / (int)sizeof(T);       // (zeros behind the end)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll

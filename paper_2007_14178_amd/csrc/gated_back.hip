@@ -192,7 +192,9 @@ hipError_t gated_fwd_copy(DenseArgs *p, void *workspace, hipStream_t st)
                             {(const uint16_t *)p->b2, (uint16_t *)(ws + l.wu), p->N, p->ldb / 2}};
     p->a = ws + l.x, p->b = ws + l.wg, p->b2 = ws + l.wu;
     p->lda = p->ldb = 2 * (long long)l.kp;
-    return copy_rows(copies, 3, p->K, (int)l.kp, st);
+    const int K = p->K;
+    p->K = (int)l.kp;           // (with the zeros behind a row)
+    return copy_rows(copies, 3, K, (int)l.kp, st);
 }
 
 hipError_t launch_gated_bwd(const GatedBackArgs &p, int type, hipStream_t st)
