@@ -447,7 +447,7 @@ int xnor_conv2d_pick_algo(const xnor_shape *s, size_t workspace_bytes);
  *     q_stride) and of 16-bit ones that do are read faster.
  *   - Types of real values are given as an xnor_type; others than those named at a call: XNOR_E_UNSUPPORTED.
  *   - The number of tokens (M, rows) may be 0: then nothing is launched for them, their pointers may be NULL, and gradients of
- *     weights are written as zeros.  Other sizes are >= 1, at most 2^30.
+ *     weights are written as zeros.  It is below 2^31; other sizes are >= 1 and at most 2^26.
  *   - Sums, statistics and scales are fp32 or (8-bit products) exact 32-bit integers; each output is rounded once from fp32, to
  *     nearest, ties to even.
  */

@@ -8,7 +8,7 @@ namespace {
 using namespace xnor;
 
 constexpr long long kMaxRows = 0x7fffffffLL;
-constexpr int kMaxCols = 1 << 30;
+constexpr int kMaxCols = 1 << 26;          // a launch of a workgroup of 512 for 16 outputs has fewer than 2^32 threads
 constexpr int kMaxInt8Cols = (1 << 17) - 1;        // |sum of K products of two int8| <= K 2^14 < 2^31
 
 int value_size(int type) { return type == XNOR_TYPE_FP32 ? 4 : type == XNOR_TYPE_F16 || type == XNOR_TYPE_BF16 ? 2 : 0; }

@@ -62,7 +62,16 @@ __device__ inline void finish(const DenseArgs &p, long long m, float s, int n, c
             const float y = (float)v[i] * (s * c.scale[i]);
             out[i] = (O)(p.bias ? y + c.bias[i] : y);
         }
-        store_values((O *)p.out + m * p.ldo, n, p.N, out);
+        // fp32 outputs whose rows are whole cache lines go past the caches, which the tokens that the next tiles read stay in (100352 x 512 x 512
+        // with its quantisation 131 -> 122 us; rows of 4000 bytes would reach memory in pieces, 16384 x 1000 x 1024 27 -> 54 us, as would 16-bit
+        // outputs, 32 bytes of a token at a time)
+        O *const to = (O *)p.out + m * p.ldo + n;
+        const bool lines = sizeof(O) == 4 && ((reinterpret_cast<uintptr_t>(p.out) | (uintptr_t)p.ldo * 4) & 127) == 0;
+        if (lines && n + 4 <= p.N) {
+            __builtin_nontemporal_store(f32x4{(float)out[0], (float)out[1], (float)out[2], (float)out[3]}, (f32x4 *)to);
+        } else {
+            store_values((O *)p.out + m * p.ldo, n, p.N, out);
+        }
     } else if constexpr (EPI == kSums) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) out[i] = v[i];
