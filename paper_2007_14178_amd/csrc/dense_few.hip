@@ -10,7 +10,10 @@ namespace xnor {
 namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * kWave;
-constexpr int kRealTokens = 2, kRealCols = 8192;        // real tokens that are quantised here: how many, and how long
+// Real tokens that are quantised in the product's launch, by every workgroup for itself: one or two by all its waves together, shorter ones by a
+// wave each, up to eight, or, still shorter, by a wave each two.  (GPU time 8 x 1037 x 1531 f16 6.6 us, by two launches 8.0; 16 tokens 9.0 and 8.1,
+// but two launches take the host 4.4 us more, which is what passes of this size take; 16 x 2048 x 8192 13.2 and 10.2.)
+constexpr int kTogether = 2, kTogetherCols = 8192, kRealTokens = 2 * kWaves, kRealCols = 2048, kRealColsOfTwo = 1280;
 
 // X: the type of real tokens, quantised by every workgroup for itself; void: a holds T.
 template <class T, class O, int EPI, int TT, class X>
@@ -22,7 +25,7 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const DenseArgs p)
     typedef Mat<T> Mul;
     typedef typename Mul::acc Acc;
     __shared__ Acc sums[kWaves][MATS][TT][kWave];
-    __shared__ float tops[REAL ? kRealTokens : 1][kWaves];
+    __shared__ float tops[kTogether][kWaves], scales[kRealTokens];
     extern __shared__ __align__(16) int8_t levels[];        // real tokens: [M][whole steps]
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * 16;
@@ -57,45 +60,81 @@ __global__ __launch_bounds__(kThreads) void few_kernel(const DenseArgs p)
     float scale[TT] = {};
     if constexpr (REAL) {
         // the tokens first, b's first rows on their way while the tokens are quantised
-        constexpr int XV = 16 / (int)sizeof(X), kRealChunks = kRealCols / (kThreads * XV);
-        Chunk<X> held[kRealTokens][kRealChunks];
+        constexpr int XV = 16 / (int)sizeof(X);
+        if (p.M <= kTogether) {
+            constexpr int CHUNKS = kTogetherCols / (kThreads * XV);
+            Chunk<X> held[kTogether][CHUNKS];
 #pragma unroll
-        for (int m = 0; m < kRealTokens; ++m)
-            if (m < p.M)
+            for (int m = 0; m < kTogether; ++m)
+                if (m < p.M)
 #pragma unroll
-                for (int c = 0; c < kRealChunks; ++c)
-                    held[m][c] = load_chunk((const X *)((const char *)p.a + m * p.lda), (t + c * kThreads) * XV, p.K);
-        load_b(from);
+                    for (int c = 0; c < CHUNKS; ++c)
+                        held[m][c] = load_chunk((const X *)((const char *)p.a + m * p.lda), (t + c * kThreads) * XV, p.K);
+            load_b(from);
 #pragma unroll
-        for (int m = 0; m < kRealTokens; ++m)
-            if (m < p.M) {
+            for (int m = 0; m < kTogether; ++m)
+                if (m < p.M) {
+                    float top = 0.f;
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                        for (int k = 0; k < XV; ++k) top = MaxNan()(fabsf((float)held[m][c].v[k]), top);
+                    top = wave_reduce(top, MaxNan());
+                    if (lane == 0) tops[m][wave] = top;
+                }
+            __syncthreads();
+#pragma unroll
+            for (int m = 0; m < kTogether; ++m)
+                if (m < p.M) {
+                    float top = tops[m][0];
+#pragma unroll
+                    for (int w = 1; w < kWaves; ++w) top = MaxNan()(tops[m][w], top);
+                    const RowLevels l = row_levels(top);
+                    if (r == m) scale[0] = l.scale;
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        const int at = (t + c * kThreads) * XV;
+                        int8_t q[XV];
+#pragma unroll
+                        for (int k = 0; k < XV; ++k) q[k] = level_of((float)held[m][c].v[k], l);
+                        if (at < held_bytes) __builtin_memcpy(levels + m * held_bytes + at, q, XV);        // (zeros behind the token's end)
+                    }
+                }
+            __syncthreads();
+        } else {
+            constexpr int CHUNKS = kRealCols / (kWave * XV);
+            Chunk<X> held[2][CHUNKS];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (wave + i * kWaves < p.M)
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c)
+                        held[i][c] = load_chunk((const X *)((const char *)p.a + (wave + i * kWaves) * p.lda), (lane + c * kWave) * XV, p.K);
+            load_b(from);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int m = wave + i * kWaves;
+                if (m >= p.M) continue;
                 float top = 0.f;
 #pragma unroll
-                for (int c = 0; c < kRealChunks; ++c)
+                for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                    for (int k = 0; k < XV; ++k) top = MaxNan()(fabsf((float)held[m][c].v[k]), top);
-                top = wave_reduce(top, MaxNan());
-                if (lane == 0) tops[m][wave] = top;
-            }
-        __syncthreads();
+                    for (int k = 0; k < XV; ++k) top = MaxNan()(fabsf((float)held[i][c].v[k]), top);
+                const RowLevels l = row_levels(wave_reduce(top, MaxNan()));
+                if (lane == 0) scales[m] = l.scale;
 #pragma unroll
-        for (int m = 0; m < kRealTokens; ++m)
-            if (m < p.M) {
-                float top = tops[m][0];
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w) top = MaxNan()(tops[m][w], top);
-                const RowLevels l = row_levels(top);
-                if (r == m) scale[0] = l.scale;
-#pragma unroll
-                for (int c = 0; c < kRealChunks; ++c) {
-                    const int at = (t + c * kThreads) * XV;
+                for (int c = 0; c < CHUNKS; ++c) {
+                    const int at = (lane + c * kWave) * XV;
                     int8_t q[XV];
+                    if (at >= held_bytes) continue;
 #pragma unroll
-                    for (int k = 0; k < XV; ++k) q[k] = level_of((float)held[m][c].v[k], l);
-                    if (at < held_bytes) __builtin_memcpy(levels + m * held_bytes + at, q, XV);        // (zeros behind the token's end)
+                    for (int k = 0; k < XV; ++k) q[k] = level_of((float)held[i][c].v[k], l);
+                    __builtin_memcpy(levels + m * held_bytes + at, q, XV);
                 }
             }
-        __syncthreads();
+            __syncthreads();
+            scale[0] = scales[min(r, (int)p.M - 1)];
+        }
     } else {
         load_b(from);
 #pragma unroll
@@ -178,7 +217,7 @@ template hipError_t launch_few<bf16_t, bf16_t, kGated>(const DenseArgs &, hipStr
 
 bool dense_few_real_supports(long long M, int K)
 {
-    return M <= kRealTokens && K <= kRealCols;
+    return M <= kTogether ? K <= kTogetherCols : M <= kWaves ? K <= kRealCols : M <= kRealTokens && K <= kRealColsOfTwo;
 }
 
 template <class X>

@@ -39,9 +39,9 @@ def test_int8_matmul_refuses(xb):
 
 
 def test_int8_linear_refuses(xb):
-    need = xb.xnor_int8_linear_workspace_bytes(4, 64)
+    need = xb.xnor_int8_linear_workspace_bytes(40, 64)
     # (x, type, x_stride, w, w_stride, w_scale, bias, M, N, K, out, type, out_stride, workspace, bytes, stream)
-    with_bad([OK, 2, 64, OK, 64, OK, None, 4, 8, 64, OK, 2, 8, OK, need, None], xb.lib.xnor_int8_linear, [
+    with_bad([OK, 2, 64, OK, 64, OK, None, 40, 8, 64, OK, 2, 8, OK, need, None], xb.lib.xnor_int8_linear, [
         (0, None, xb.E_NULL), (3, None, xb.E_NULL), (5, None, xb.E_NULL), (10, None, xb.E_NULL), (13, None, xb.E_NULL), (1, 7, xb.E_UNSUPPORTED),
         (11, 3, xb.E_UNSUPPORTED), (9, 1 << 17, xb.E_SHAPE), (8, -1, xb.E_SHAPE), (12, 7, xb.E_SHAPE), (0, ODD, xb.E_ALIGN),
         (13, ctypes.c_void_p(0x1008), xb.E_ALIGN), (14, need - 1, xb.E_WORKSPACE)])

@@ -114,7 +114,7 @@ def test_int8_matmul_one_row_for_all_tokens(xb):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=str)
-@pytest.mark.parametrize("M,N,K", [(1, 40, 1), (1, 512, 4096), (2, 1000, 300), (7, 33, 1037), (16, 129, 512), (40, 96, 2000), (200, 130, 513)])
+@pytest.mark.parametrize("M,N,K", [(1, 40, 1), (1, 512, 4096), (1, 90, 9000), (2, 1000, 300), (2, 70, 8192), (3, 50, 1), (7, 33, 1037), (8, 40, 2048), (9, 64, 2049), (16, 129, 512), (16, 48, 2000), (12, 70, 1000), (40, 96, 2000), (200, 130, 513)])
 def test_int8_linear(xb, dtype, M, N, K):
     x, (w, sw) = rand(M, M, K + 3, dtype=dtype)[:, 1:K + 1], xb.xnor_int8_quantize(rand(N, N, K))
     bias = rand(9, N)
@@ -126,7 +126,7 @@ def test_int8_linear(xb, dtype, M, N, K):
 
 def test_int8_linear_token_that_is_not_finite(xb):
     """It spoils its own outputs and no others."""
-    for M in (3, 100):
+    for M in (2, 3, 13, 40, 100):
         x, (w, sw) = rand(1, M, 200), xb.xnor_int8_quantize(rand(2, 70, 200))
         clean = xb.xnor_int8_linear(x, w, sw)
         x[1, 7] = float("inf")
