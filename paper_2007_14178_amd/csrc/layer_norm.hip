@@ -162,7 +162,10 @@ hipError_t launch_rows(const RowArgs &p, hipStream_t st)
         if (chunks <= 512) return go(integral_constant<int, 256>(), integral_constant<int, 2>());
         if (chunks <= 1024) return go(integral_constant<int, 512>(), integral_constant<int, 2>());
     }
-    if (chunks <= 4096) return go(integral_constant<int, 1024>(), integral_constant<int, 4>());
+    if (chunks <= 2048) return go(integral_constant<int, 1024>(), integral_constant<int, 2>());
+    // (four chunks of eight values and their parameters do not fit in registers: 2048 x 30000 bf16 208 us, read again for every sum 108 us)
+    if constexpr (OUT == kQuantize || V == 4)
+        if (chunks <= 4096) return go(integral_constant<int, 1024>(), integral_constant<int, 4>());
     return go(integral_constant<int, 1024>(), integral_constant<int, 0>());
 }
 
