@@ -95,8 +95,9 @@ __device__ inline void finish(const DenseArgs &p, long long m, float s, int n, c
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float a = p.act == XNOR_ACT_SILU ? act_value<XNOR_ACT_SILU, sizeof(O) == 2>(g[i])
-                            : p.act == XNOR_ACT_GELU ? act_value<XNOR_ACT_GELU>(g[i]) : act_value<XNOR_ACT_RELU>(g[i]);
+            constexpr bool SHORT = sizeof(O) == 2;
+            const float a = p.act == XNOR_ACT_SILU ? act_value<XNOR_ACT_SILU, SHORT>(g[i])
+                            : p.act == XNOR_ACT_GELU ? act_value<XNOR_ACT_GELU, SHORT>(g[i]) : act_value<XNOR_ACT_RELU, SHORT>(g[i]);
             out[i] = (O)(a * u[i]);
         }
         store_values((O *)p.out + m * p.ldo, n, p.N, out);

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256) void gate_back_kernel(const GatedBackArgs p, T
                 if (f + k >= p.F) break;
                 const float d = (float)dh.v[k], gv = (float)g.v[k];
                 dg[k] = (T)(d * (float)u.v[k] * act_slope<ACT>(gv));
-                du[k] = (T)(d * act_value<ACT>(gv));
+                du[k] = (T)(d * act_value<ACT, true>(gv));
             }
         }
         __builtin_memcpy(dgu + m * 2 * fp + f, dg, 16);
