@@ -135,7 +135,7 @@ __device__ inline float erfc_short(float z)
 
 // Activations of the gated block and their derivatives, in fp32.  ACT: an xnor_act.  SHORT: for results that are rounded to 16 bits: by the
 // exponential and reciprocal instructions, within a few roundings of |g| (2000 x 4096 x 8192 silu on 8 bits 125 us with the functions, 120 us
-// so; 4096 x 4096 x 8192 gelu on f16 460 us and 437 us).
+// so; 4096 x 4096 x 8192 gelu on f16 459 us and 439, silu 438).
 template <bool SHORT>
 __device__ inline float sigmoid(float g)
 {

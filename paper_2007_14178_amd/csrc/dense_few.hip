@@ -1,4 +1,5 @@
-// Products for few tokens (a decoding step): b is read once, by as many waves as there are, and that is what they take.
+// Products for few tokens (a decoding step): b is read once, by as many waves as there are, and that is what they take (gated, one token x 4096 x
+// 8192 8 bits 13.4 us, 5.0 TB/s; one token x 4096 x 4096 with its quantisation 6.6 us, a launch and two chains of loads).
 //
 // A workgroup has 16 rows of b (of each matrix in the gated block), its eight waves an eighth of the contraction each, whose sums are
 // added in LDS.  The tokens are columns of the matrix instruction: up to 16 cost what one costs.
