@@ -174,9 +174,11 @@ hipError_t launch_rows(const RowArgs &p, hipStream_t st)
 // Backward.  p = dy gamma, xh = (x - mean) rstd: dx = rstd (p - mean(p) - xh mean(p xh)), dgamma = sum over rows of dy xh,
 // dbeta = sum over rows of dy.  A workgroup takes every gridDim.x-th row and keeps its columns' part of the two sums in
 // registers; a second launch adds the parts in a fixed order.  Memory bounds it: x and dy read, dx written (16384 x 4096 bf16
-// 109 us, 3.7 TB/s; fp32 5.4 TB/s: 16-bit rows have twice the arithmetic, and the same two sums over the workgroup, to a byte).
+// 90 us, 4.5 TB/s; 100000 x 512 f16 71 us, with one row on its way 109).
 // ------------------------------------------------------------------------------------------------
-template <class T, class P, int THREADS, int NV>
+// WHOLE: rows of whole chunks.  Two rows are then on their way while one is worked on: no load depends on a branch, which would make
+// a wait for one row a wait for both.
+template <class T, class P, int THREADS, int NV, bool WHOLE>
 __global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const NormBackArgs p)
 {
     constexpr int V = Chunk<T>::kCount, ROWS = block_of(THREADS) / THREADS;
@@ -185,26 +187,46 @@ __global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const Norm
     const long long step = (long long)gridDim.x * ROWS;
     long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS;
     float gamma[NV][V], sg[NV][V] = {}, sb[NV][V] = {};
-    Chunk<T> cx[NV], cd[NV], nx[NV], nd[NV];
-    float mean = 0.f, rstd = 0.f, next_mean = 0.f, next_rstd = 0.f;
-    auto fetch = [&](long long r) __attribute__((always_inline)) {
+    constexpr int DEEP = WHOLE ? 2 : 1;
+    Chunk<T> nx[DEEP][NV], nd[DEEP][NV];
+    float next_mean[DEEP], next_rstd[DEEP];
+    auto fetch = [&](auto slot, long long r) __attribute__((always_inline)) {
+        constexpr int D = decltype(slot)::value;
+        if constexpr (WHOLE) r = r < p.rows ? r : row;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            nx[i] = load_chunk((const T *)p.x + r * p.x_stride, (t + i * THREADS) * V, p.cols);
-            nd[i] = load_chunk((const T *)p.dy + r * p.dy_stride, (t + i * THREADS) * V, p.cols);
+            const int at = (t + i * THREADS) * V;
+            if constexpr (WHOLE) {
+                const int c = at < p.cols ? at : 0;
+                __builtin_memcpy(&nx[D][i], (const T *)p.x + r * p.x_stride + c, 16);
+                __builtin_memcpy(&nd[D][i], (const T *)p.dy + r * p.dy_stride + c, 16);
+            } else {
+                nx[D][i] = load_chunk((const T *)p.x + r * p.x_stride, at, p.cols);
+                nd[D][i] = load_chunk((const T *)p.dy + r * p.dy_stride, at, p.cols);
+            }
         }
-        next_mean = p.mean[r];
-        next_rstd = p.rstd[r];
+        next_mean[D] = p.mean[r];
+        next_rstd[D] = p.rstd[r];
     };
-    if (row < p.rows) fetch(row);
+    using std::integral_constant;
+    if (row < p.rows) {
+        fetch(integral_constant<int, 0>(), row);
+        if constexpr (WHOLE) fetch(integral_constant<int, 1>(), row + step);
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) load_params((const P *)p.gamma, (t + i * THREADS) * V, p.cols, 1.f, gamma[i]);
     const float share = 1.f / (float)p.cols;
-    for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
+    auto work = [&](auto slot, int turn) __attribute__((always_inline)) {
+        constexpr int D = decltype(slot)::value;
+        Chunk<T> cx[NV], cd[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) cx[i] = nx[i], cd[i] = nd[i];
-        mean = next_mean, rstd = next_rstd;
-        if (row + step < p.rows) fetch(row + step);
+        for (int i = 0; i < NV; ++i) {
+            cx[i] = nx[D][i], cd[i] = nd[D][i];
+            if constexpr (WHOLE)
+                if ((t + i * THREADS) * V >= p.cols) cd[i] = Chunk<T>{};
+        }
+        const float mean = next_mean[D], rstd = next_rstd[D];
+        if (WHOLE || row + step < p.rows) fetch(slot, row + DEEP * step);
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -246,6 +268,17 @@ __global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const Norm
             }
             store_values(dx, at, p.cols, out);
         }
+    };
+    if constexpr (WHOLE) {
+        while (row < p.rows) {
+            work(integral_constant<int, 0>(), 0);
+            row += step;
+            if (row >= p.rows) break;
+            work(integral_constant<int, 1>(), 1);
+            row += step;
+        }
+    } else {
+        for (int turn = 0; row < p.rows; row += step, turn ^= 1) work(integral_constant<int, 0>(), turn);
     }
     if (!p.partial) return;
     float *to = p.partial + (long long)blockIdx.x * 2 * p.cols;
@@ -374,7 +407,7 @@ BackPlan back_plan(int x_type, long long rows, int cols)
         return b;
     }
     // Two workgroups a unit, of 256 threads three: their registers, and the parts that they leave, have more run slower
-    // (16384 x 4096 bf16 110 us, with three 131; 16384 x 2048 50 us, with two 57); and four rows a thread, where there are fewer.
+    // (16384 x 4096 bf16, one row on its way: 110 us, with three 131; 16384 x 2048 50 us, with two 57); and four rows a thread, where there are fewer.
     const int rows_a_block = b.threads < kBlock ? kBlock / b.threads : 1, most = (b.threads == 256 ? 3 : 2) * kPlanUnits;
     const long long want = std::max<long long>(1, std::min<long long>(most, (rows + rows_a_block * 4 - 1) / (rows_a_block * 4)));
     b.blocks = (int)want;         // (a part each)
@@ -391,7 +424,9 @@ hipError_t back(const NormBackArgs &p, int x_type, hipStream_t st)
         using std::integral_constant;
         auto go = [&](auto threads, auto nv) {
             constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
-            norm_back_kernel<T, P, THREADS, NV><<<dim3((unsigned)b.blocks), dim3(block_of(THREADS)), 0, st>>>(p);
+            if constexpr (THREADS < 1024 || NV == 1)        // (what two chunks of 1024 threads hold leaves no registers for a second row)
+                if (p.cols % Chunk<T>::kCount == 0) return norm_back_kernel<T, P, THREADS, NV, true><<<dim3((unsigned)b.blocks), dim3(block_of(THREADS)), 0, st>>>(p);
+            norm_back_kernel<T, P, THREADS, NV, false><<<dim3((unsigned)b.blocks), dim3(block_of(THREADS)), 0, st>>>(p);
         };
         if (b.nv == 0) {
             norm_back_long_kernel<T, P><<<dim3((unsigned)b.blocks), dim3(1024), 0, st>>>(p);
