@@ -1,6 +1,6 @@
 // Operators on the rows of a matrix: layer norm forward (real or quantised output) and backward, and the quantisation of rows
-// to 8 bits.  All are bound by memory: a row is read once into registers, where its sums are formed, and written once.  (16384 x 4096 bf16 55 us,
-// 4.9 TB/s, as a large copy; 16384 x 8192 bf16 quantised 94 us, 4.3 TB/s; 100352 x 512 fp32 quantised 45 us, 5.7 TB/s.)
+// to 8 bits.  All are bound by memory: a row is read once into registers, where its sums are formed, and written once.  (16384 x 4096 bf16 47 us,
+// 5.7 TB/s; 16384 x 8192 bf16 quantised 77 us, 5.2 TB/s; 100352 x 512 fp32 quantised 40 us, 6.4 TB/s.)
 #include <algorithm>
 
 #include "dense_common.hpp"
@@ -26,28 +26,55 @@ __device__ inline float row_reduce(float v, float *slots, Op op)
     return v;
 }
 
+// The chunk that starts `at` values into a row of `cols`, zeros where `there` is false or behind its end, by one load that no branch
+// stands before: where one does, a wait for a row is a wait for what was asked for behind it too.  Rows of whole chunks at multiples of 16 bytes;
+// the row the same for the whole wave.
+template <class T>
+__device__ inline Chunk<T> load_whole(const T *row, bool there, int cols, int at)
+{
+    Chunk<T> c{};
+#ifdef __HIP_DEVICE_COMPILE__        // (the host's pass does not know the builtins)
+    const auto from = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(row), 0, there ? cols * (int)sizeof(T) : 0, 0x00027000);
+    const auto raw = __builtin_amdgcn_raw_buffer_load_b128(from, at * (int)sizeof(T), 0, 0);
+    __builtin_memcpy(&c, &raw, 16);
+#endif
+    return c;
+}
+inline bool whole_rows(const void *x, long long stride, int cols, int value_bytes)
+{
+    return (((uintptr_t)x | (uintptr_t)(stride * value_bytes) | (uintptr_t)cols * value_bytes) & 15) == 0;
+}
+
 constexpr int block_of(int threads) { return threads < kBlock ? kBlock : threads; }
 
 // Rows by THREADS threads each, NV chunks of 16 bytes of a row in a thread's registers, and with them the parameters of its
 // columns, which are read once for all of a workgroup's rows; the next row is on its way while one is worked on.  (NV = 0: rows of any
-// length, read again for every sum.)
-template <class T, class P, int OUT, int THREADS, int NV>
+// length, read again for every sum.)  WHOLE: load_whole takes the rows, and two are on their way.
+template <class T, class P, int OUT, int THREADS, int NV, bool WHOLE>
 __global__ __launch_bounds__(block_of(THREADS)) void row_kernel(const RowArgs p)
 {
     constexpr int V = Chunk<T>::kCount, ROWS = block_of(THREADS) / THREADS, N = NV ? NV : 1;
     __shared__ float slots[2][3][16];
     const int t = threadIdx.x % THREADS;
     const long long step = (long long)gridDim.x * ROWS;
-    long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    long long row = (long long)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
     if (row >= p.rows) return;                  // (rows share no barrier where a workgroup has several)
 
     float gamma[N][V], beta[N][V];
-    Chunk<T> held[N], next[N];
-    auto fetch = [&](long long r, Chunk<T> (&to)[N]) __attribute__((always_inline)) {
+    constexpr int DEEP = WHOLE ? 2 : 1;
+    Chunk<T> next[DEEP][N];
+    auto fetch = [&](auto slot, long long r) __attribute__((always_inline)) {
+        constexpr int D = decltype(slot)::value;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) to[i] = load_chunk((const T *)p.x + r * p.x_stride, (t + i * THREADS) * V, p.cols);
+        for (int i = 0; i < NV; ++i) {
+            const int at = (t + i * THREADS) * V;
+            if constexpr (WHOLE) next[D][i] = load_whole((const T *)p.x + r * p.x_stride, r < p.rows, p.cols, at);
+            else next[D][i] = load_chunk((const T *)p.x + r * p.x_stride, at, p.cols);
+        }
     };
-    fetch(row, next);
+    using std::integral_constant;
+    fetch(integral_constant<int, 0>(), row);
+    if constexpr (WHOLE) fetch(integral_constant<int, 1>(), row + step);
     if constexpr (NV > 0 && OUT != kQuantize) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -55,10 +82,11 @@ __global__ __launch_bounds__(block_of(THREADS)) void row_kernel(const RowArgs p)
             load_params((const P *)p.beta, (t + i * THREADS) * V, p.cols, 0.f, beta[i]);
         }
     }
-    for (int turn = 0; row < p.rows; row += step, turn ^= 1) {
+    auto work = [&](auto slot, int turn) __attribute__((always_inline)) {
+        Chunk<T> held[N];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) held[i] = next[i];
-        if (row + step < p.rows) fetch(row + step, next);
+        for (int i = 0; i < NV; ++i) held[i] = next[decltype(slot)::value][i];
+        if (WHOLE || row + step < p.rows) fetch(slot, row + DEEP * step);
         const T *x = (const T *)p.x + row * p.x_stride;
         auto each = [&](auto f) __attribute__((always_inline)) {        // f(column of the chunk's first value, chunk, its number)
             if constexpr (NV > 0) {
@@ -83,7 +111,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void row_kernel(const RowArgs p)
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
                     const float d = (float)c.v[k] - mean;
-                    d2 += at + k < p.cols ? d * d : 0.f;
+                    d2 += WHOLE || at + k < p.cols ? d * d : 0.f;
                 }
             });
             rstd = 1.f / sqrtf(row_reduce<THREADS>(d2, slots[turn][1], Sum()) / (float)p.cols + p.eps);
@@ -100,7 +128,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void row_kernel(const RowArgs p)
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 if constexpr (OUT == kQuantize) to[k] = (float)c.v[k];
-                else to[k] = at + k < p.cols ? ((float)c.v[k] - mean) * rstd * gamma[i][k] + beta[i][k] : 0.f;
+                else to[k] = WHOLE || at + k < p.cols ? ((float)c.v[k] - mean) * rstd * gamma[i][k] + beta[i][k] : 0.f;
             }
         };
         if constexpr (OUT == kReal) {
@@ -134,6 +162,17 @@ __global__ __launch_bounds__(block_of(THREADS)) void row_kernel(const RowArgs p)
                 store_values(q, at, p.cols, out);
             });
         }
+    };
+    if constexpr (WHOLE) {
+        while (row < p.rows) {
+            work(integral_constant<int, 0>(), 0);
+            row += step;
+            if (row >= p.rows) break;
+            work(integral_constant<int, 1>(), 1);
+            row += step;
+        }
+    } else {
+        for (int turn = 0; row < p.rows; row += step, turn ^= 1) work(integral_constant<int, 0>(), turn);
     }
 }
 
@@ -147,15 +186,24 @@ hipError_t launch_rows(const RowArgs &p, hipStream_t st)
         constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
         constexpr int ROWS = block_of(THREADS) / THREADS;
         const long long blocks = (p.rows + ROWS - 1) / ROWS;
-        row_kernel<T, P, OUT, THREADS, NV><<<dim3((unsigned)std::min<long long>(blocks, (THREADS >= 512 && OUT == kReal ? 4 : 16) * compute_units())), dim3(block_of(THREADS)), 0, st>>>(p);
+        const dim3 grid((unsigned)std::min<long long>(blocks, (THREADS >= 512 && OUT == kReal ? 4 : 16) * compute_units())), block(block_of(THREADS));
+        // (16-bit rows: 16384 x 8192 bf16 112 us, so 102, quantised norm 149 and 119, 40000 x 1024 41 and 27; fp32 rows, of twice the chunks, have enough
+        // on their way: 100352 x 512 quantised 40 us, so 42; nor do levels of 1024 threads gain, 4096 x 16384 bf16 42 and 46)
+        if constexpr (V == 8 && NV > 0 && (THREADS < 1024 || OUT == kReal)) {
+            if (whole_rows(p.x, p.x_stride, p.cols, (int)sizeof(T))) {
+                row_kernel<T, P, OUT, THREADS, NV, true><<<grid, block, 0, st>>>(p);
+                return hipGetLastError();
+            }
+        }
+        row_kernel<T, P, OUT, THREADS, NV, false><<<grid, block, 0, st>>>(p);
         return hipGetLastError();
     };
     using std::integral_constant;
     if (chunks <= 64) return go(integral_constant<int, 64>(), integral_constant<int, 1>());
     if (chunks <= 128) return go(integral_constant<int, 64>(), integral_constant<int, 2>());
     if (chunks <= 256) return go(integral_constant<int, 256>(), integral_constant<int, 1>());
-    // Real outputs: a chunk a thread (16384 x 4096 bf16 56 us, with two 67; 16384 x 8192 118 us, with four 169).  Levels take three sums
-    // or maxima over the workgroup, and fewer waves wait for each other (16384 x 4096 quantised norm 63 us, with one chunk 81).
+    // Real outputs: a chunk a thread (16384 x 4096 bf16, one row on its way: 56 us, with two 67; 16384 x 8192 118 us, with four 169).  Levels take three sums
+    // or maxima over the workgroup, and fewer waves wait for each other (16384 x 4096 quantised norm, one row on its way: 63 us, with one chunk 81).
     if constexpr (OUT == kReal) {
         if (chunks <= 512) return go(integral_constant<int, 512>(), integral_constant<int, 1>());
         if (chunks <= 1024) return go(integral_constant<int, 1024>(), integral_constant<int, 1>());
@@ -174,10 +222,9 @@ hipError_t launch_rows(const RowArgs &p, hipStream_t st)
 // Backward.  p = dy gamma, xh = (x - mean) rstd: dx = rstd (p - mean(p) - xh mean(p xh)), dgamma = sum over rows of dy xh,
 // dbeta = sum over rows of dy.  A workgroup takes every gridDim.x-th row and keeps its columns' part of the two sums in
 // registers; a second launch adds the parts in a fixed order.  Memory bounds it: x and dy read, dx written (16384 x 4096 bf16
-// 90 us, 4.5 TB/s; 100000 x 512 f16 71 us, with one row on its way 109).
+// 89 us, 4.5 TB/s; 100000 x 512 f16 71 us, with one row on its way 109).
 // ------------------------------------------------------------------------------------------------
-// WHOLE: rows of whole chunks.  Two rows are then on their way while one is worked on: no load depends on a branch, which would make
-// a wait for one row a wait for both.
+// WHOLE: load_whole takes the rows.  Two are then on their way while one is worked on.
 template <class T, class P, int THREADS, int NV, bool WHOLE>
 __global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const NormBackArgs p)
 {
@@ -185,26 +232,25 @@ __global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const Norm
     __shared__ float slots[2][2][16];
     const int t = threadIdx.x % THREADS;
     const long long step = (long long)gridDim.x * ROWS;
-    long long row = (long long)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    long long row = (long long)blockIdx.x * ROWS + __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
     float gamma[NV][V], sg[NV][V] = {}, sb[NV][V] = {};
     constexpr int DEEP = WHOLE ? 2 : 1;
     Chunk<T> nx[DEEP][NV], nd[DEEP][NV];
     float next_mean[DEEP], next_rstd[DEEP];
     auto fetch = [&](auto slot, long long r) __attribute__((always_inline)) {
         constexpr int D = decltype(slot)::value;
-        if constexpr (WHOLE) r = r < p.rows ? r : row;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int at = (t + i * THREADS) * V;
             if constexpr (WHOLE) {
-                const int c = at < p.cols ? at : 0;
-                __builtin_memcpy(&nx[D][i], (const T *)p.x + r * p.x_stride + c, 16);
-                __builtin_memcpy(&nd[D][i], (const T *)p.dy + r * p.dy_stride + c, 16);
+                nx[D][i] = load_whole((const T *)p.x + r * p.x_stride, r < p.rows, p.cols, at);
+                nd[D][i] = load_whole((const T *)p.dy + r * p.dy_stride, r < p.rows, p.cols, at);
             } else {
                 nx[D][i] = load_chunk((const T *)p.x + r * p.x_stride, at, p.cols);
                 nd[D][i] = load_chunk((const T *)p.dy + r * p.dy_stride, at, p.cols);
             }
         }
+        if constexpr (WHOLE) r = r < p.rows ? r : row;
         next_mean[D] = p.mean[r];
         next_rstd[D] = p.rstd[r];
     };
@@ -220,11 +266,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const Norm
         constexpr int D = decltype(slot)::value;
         Chunk<T> cx[NV], cd[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            cx[i] = nx[D][i], cd[i] = nd[D][i];
-            if constexpr (WHOLE)
-                if ((t + i * THREADS) * V >= p.cols) cd[i] = Chunk<T>{};
-        }
+        for (int i = 0; i < NV; ++i) cx[i] = nx[D][i], cd[i] = nd[D][i];
         const float mean = next_mean[D], rstd = next_rstd[D];
         if (WHOLE || row + step < p.rows) fetch(slot, row + DEEP * step);
         float s1 = 0.f, s2 = 0.f;
@@ -425,7 +467,7 @@ hipError_t back(const NormBackArgs &p, int x_type, hipStream_t st)
         auto go = [&](auto threads, auto nv) {
             constexpr int THREADS = decltype(threads)::value, NV = decltype(nv)::value;
             if constexpr (THREADS < 1024 || NV == 1)        // (what two chunks of 1024 threads hold leaves no registers for a second row)
-                if (p.cols % Chunk<T>::kCount == 0) return norm_back_kernel<T, P, THREADS, NV, true><<<dim3((unsigned)b.blocks), dim3(block_of(THREADS)), 0, st>>>(p);
+                if (whole_rows(p.x, p.x_stride, p.cols, (int)sizeof(T)) && whole_rows(p.dy, p.dy_stride, p.cols, (int)sizeof(T))) return norm_back_kernel<T, P, THREADS, NV, true><<<dim3((unsigned)b.blocks), dim3(block_of(THREADS)), 0, st>>>(p);
             norm_back_kernel<T, P, THREADS, NV, false><<<dim3((unsigned)b.blocks), dim3(block_of(THREADS)), 0, st>>>(p);
         };
         if (b.nv == 0) {
