@@ -207,6 +207,29 @@ def test_norm_backward(xb, dtype, p_dtype, rows, cols):
         assert alone[1] is None and torch.equal(alone[0], got[0])
 
 
+@pytest.mark.parametrize("dtype,p_dtype", PAIRS, ids=str)
+@pytest.mark.parametrize("rows,cols", [(1, 8), (2, 64), (9, 520), (4100, 1024), (5, 2056), (2600, 4096), (3, 8192), (2, 16384)])
+def test_norm_whole_chunks(xb, dtype, p_dtype, rows, cols):
+    """Rows of whole 16-byte chunks at multiples of 16 bytes, with others behind them, up to more than a workgroup takes two of."""
+    x, gamma, beta = norm_inputs(rows, cols, dtype, p_dtype, 16)
+    dy = rand(rows + 78, rows, cols + 8, dtype=dtype)[:, :cols]
+    got = xb.xnor_layer_norm_fwd(x, gamma, beta, EPS)
+    want, bound = ref.norm(x, gamma, beta, EPS, dtype)
+    for t, w, e, name in zip(got, want, bound, ("y", "mean", "rstd")):
+        ref.assert_within(t, w, e, name)
+    _, mean, rstd = got
+    got = xb.xnor_layer_norm_bwd(dy, x, gamma, mean, rstd)
+    want, bound = ref.norm_back(dy, x, gamma, mean, rstd, dtype, p_dtype)
+    for t, w, e, name in zip(got, want, bound, ("dx", "dgamma", "dbeta")):
+        ref.assert_within(t, w, e, name)
+    q, s = xb.xnor_int8_quantize(x)
+    want_q, want_s = xb.xnor_int8_quantize(x[-1:])
+    assert torch.equal(q[-1:], want_q) and torch.equal(s[-1:], want_s)
+    q, s = xb.xnor_layer_norm_fwd_int8(x, gamma, beta, EPS)
+    want_q, want_s = xb.xnor_layer_norm_fwd_int8(x[rows // 2:], gamma, beta, EPS)
+    assert torch.equal(q[rows // 2:], want_q) and torch.equal(s[rows // 2:], want_s)
+
+
 def test_norm_gradient_against_differences(xb):
     rows, cols, h = 4, 37, 1e-4
     x, gamma, beta = norm_inputs(rows, cols, F32, F32)
