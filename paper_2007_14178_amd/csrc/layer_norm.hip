@@ -445,7 +445,7 @@ BackPlan back_plan(int x_type, long long rows, int cols)
     else if (chunks <= 2048) b.threads = 1024, b.nv = chunks <= 1024 ? 1 : 2;
     if (b.nv == 0) {
         b.blocks = (int)std::min(rows, kMaxBlocks);
-        b.parts = (int)std::min<long long>(rows, 64);
+        b.parts = (int)std::max<long long>(1, std::min<long long>(rows, 64));       // (without rows too a caller's workspace is one part)
         return b;
     }
     // Two workgroups a unit, of 256 threads three: their registers, and the parts that they leave, have more run slower

@@ -1,0 +1,37 @@
+"""The dense operators at the edges of what they take: no rows, more rows than one launch's workgroups hold, rows and columns in one piece
+of memory, widths at which another kernel takes over.  Tolerances are the bounds that dense_reference derives."""
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import dense_reference as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module")
+def xb():
+    from paper_2007_14178_amd import binding
+    return binding
+
+
+def rand(seed, *shape, dtype=F32, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * std).to(dtype).cuda()
+
+
+@pytest.mark.parametrize("dtype,cols", [(F32, 33), (F32, 9000), (F16, 16384), (F16, 16392), (BF16, 20000), (BF16, 70001)], ids=str)
+def test_norm_backward_without_rows(xb, dtype, cols):
+    """No rows, short ones or long: gradients of the parameters are zeros, whatever their memory held."""
+    x, none = torch.empty(0, cols, dtype=dtype, device="cuda"), torch.empty(0, device="cuda")
+    gamma = rand(1, cols)
+    dgamma, dbeta = torch.full((cols,), 5.0, device="cuda"), torch.full((cols,), float("nan"), device="cuda")
+    dx, dg, db = xb.xnor_layer_norm_bwd(x, x, gamma, none, none, dgamma=dgamma, dbeta=dbeta)
+    assert dx.shape == (0, cols) and dg is dgamma and db is dbeta
+    assert (dgamma == 0).all() and (dbeta == 0).all()
