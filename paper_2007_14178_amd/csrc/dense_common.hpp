@@ -181,7 +181,7 @@ struct DenseArgs {
     long long first;            // (set by the launchers: the launch's first token)
 };
 
-constexpr long long kMaxBlocks = 1 << 22;      // of a launch, for up to 1024 threads each: fewer than 2^32 threads
+constexpr long long kMaxBlocks = 1 << 22;      // of a launch, for up to 512 threads each: fewer than 2^32 threads
 
 // 16-bit out = a b^T with b as [K][N], and a as [M][K] or [K][M] (a_across): rows at multiples of 16 bytes, N and (a_across) M of 8 values,
 // a stride of b that holds its rows; seam a multiple of 64 values.  Rows of 64 contraction values within 31 bits.

@@ -355,10 +355,14 @@ __global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const Norm
 }
 
 // Rows that no workgroup holds in registers: dx from two readings, the parameters' sums by column.
+constexpr int kLongThreads = 1024;
+constexpr long long kMaxLongBlocks = kMaxBlocks / 2;
+static_assert(kMaxLongBlocks * kLongThreads < 1LL << 32, "a launch has fewer than 2^32 threads");
+
 template <class T, class P>
-__global__ __launch_bounds__(1024) void norm_back_long_kernel(const NormBackArgs p)
+__global__ __launch_bounds__(kLongThreads) void norm_back_long_kernel(const NormBackArgs p)
 {
-    constexpr int V = Chunk<T>::kCount, THREADS = 1024;
+    constexpr int V = Chunk<T>::kCount, THREADS = kLongThreads;
     __shared__ float slots[2][2][16];
     int turn = 0;
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
@@ -444,7 +448,7 @@ BackPlan back_plan(int x_type, long long rows, int cols)
     else if (chunks <= 512) b.threads = 512, b.nv = 1;
     else if (chunks <= 2048) b.threads = 1024, b.nv = chunks <= 1024 ? 1 : 2;
     if (b.nv == 0) {
-        b.blocks = (int)std::min(rows, kMaxBlocks);
+        b.blocks = (int)std::min(rows, kMaxLongBlocks);
         b.parts = (int)std::max<long long>(1, std::min<long long>(rows, 64));       // (without rows too a caller's workspace is one part)
         return b;
     }
@@ -471,7 +475,7 @@ hipError_t back(const NormBackArgs &p, int x_type, hipStream_t st)
             norm_back_kernel<T, P, THREADS, NV, false><<<dim3((unsigned)b.blocks), dim3(block_of(THREADS)), 0, st>>>(p);
         };
         if (b.nv == 0) {
-            norm_back_long_kernel<T, P><<<dim3((unsigned)b.blocks), dim3(1024), 0, st>>>(p);
+            norm_back_long_kernel<T, P><<<dim3((unsigned)b.blocks), dim3(kLongThreads), 0, st>>>(p);
             if (p.partial) norm_back_columns_kernel<T><<<dim3(ceil_div(p.cols, kBlock), parts), dim3(kBlock), 0, st>>>(p, parts);
         } else if (b.threads == 64) {
             b.nv == 1 ? go(integral_constant<int, 64>(), integral_constant<int, 1>()) : go(integral_constant<int, 64>(), integral_constant<int, 2>());

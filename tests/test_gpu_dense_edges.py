@@ -35,3 +35,21 @@ def test_norm_backward_without_rows(xb, dtype, cols):
     dx, dg, db = xb.xnor_layer_norm_bwd(x, x, gamma, none, none, dgamma=dgamma, dbeta=dbeta)
     assert dx.shape == (0, cols) and dg is dgamma and db is dbeta
     assert (dgamma == 0).all() and (dbeta == 0).all()
+
+
+def test_norm_backward_of_millions_of_long_rows(xb):
+    """More long rows than a launch of 1024 threads each has room for (2^22 such workgroups are 2^32 threads): one row for all, so that
+    all of dx's rows are alike."""
+    rows, cols = (1 << 22) + 3, 16392
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < rows * cols * 2 + (8 << 30):
+        pytest.skip("needs 145 GB of device memory")
+    x, dy, gamma = rand(1, 1, cols, dtype=BF16), rand(2, 1, cols, dtype=BF16), rand(3, cols)
+    _, mean, rstd = xb.xnor_layer_norm_fwd(x, None, None, EPS)
+    want, bound = ref.norm_back(dy, x, gamma, mean, rstd, BF16, F32)
+    dx, _, _ = xb.xnor_layer_norm_bwd(dy.expand(rows, cols), x.expand(rows, cols), gamma, mean.repeat(rows), rstd.repeat(rows), want_params=False)
+    ref.assert_within(dx[:1], want[0], bound[0], "dx")
+    for part in dx.split(1 << 18):
+        assert torch.equal(part, dx[:1].expand_as(part))
+    del dx, part
+    torch.cuda.empty_cache()
