@@ -123,12 +123,13 @@ __device__ inline i32x2 read_transposed(const lds_char *from)
 }
 
 // 16 bytes a lane from a buffer straight into LDS, the wave's 1024 from `to` on.  As an instruction of our own beside transposing reads:
-// before each of these the compiler would wait for all such fetches of its builtin.  (Nothing else in these kernels uses m0.)
+// before each of these the compiler would wait for all such fetches of its builtin.  (It reads the place in LDS from m0, one instruction after that is
+// written at the earliest.)
 template <class Rsrc>
 __device__ inline void fetch_16(Rsrc rsrc, int at, int from, lds_char *to)
 {
 #ifdef __HIP_DEVICE_COMPILE__
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"((uint32_t)(uintptr_t)to), "v"(at), "s"(rsrc), "s"(from) : "memory");
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "{m0}"((uint32_t)(uintptr_t)to), "v"(at), "s"(rsrc), "s"(from) : "memory");
 #endif
 }
 
