@@ -670,12 +670,23 @@ def _real(dtype: torch.dtype, name: str) -> int:
     return kind
 
 
+_MOST = 0x7fffffff
+
+
+def _counted(where: str, *sizes: int) -> None:
+    """Refuses what the library's integers do not hold (ctypes would pass it on modulo 2^32)."""
+    if max(sizes) > _MOST:
+        raise XnorError(E_SHAPE, where)
+
+
 def _rows(t: torch.Tensor, dtype, name: str) -> tuple[int, int, int, int]:
     """Rows, columns, pointer and row stride of a matrix whose columns are consecutive (or that has only one)."""
     shape = t.shape
     if len(shape) != 2:
         raise ValueError(f"{name}: need a matrix, got shape {tuple(shape)}")
     rows, cols = shape
+    if rows > _MOST or cols > _MOST:
+        raise XnorError(E_SHAPE, f"{name} of {rows} x {cols}")
     stride = t.stride()
     if not t.is_cuda or t.dtype is not dtype or (stride[1] != 1 and cols != 1):
         raise TypeError(f"{name}: need a GPU matrix of {dtype} with consecutive columns, got {t.dtype} on {t.device}, strides {stride}")
@@ -761,6 +772,7 @@ def xnor_int8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_
 
 @functools.lru_cache(maxsize=256)       # asked on every call
 def xnor_int8_linear_workspace_bytes(M: int, K: int) -> int:
+    _counted("xnor_int8_linear_workspace_bytes", M, K)
     n = ctypes.c_size_t()
     _ok(lib.xnor_int8_linear_workspace_bytes(M, K, ctypes.byref(n)), "xnor_int8_linear_workspace_bytes")
     return n.value
@@ -836,6 +848,7 @@ def xnor_layer_norm_fwd_int8(x: torch.Tensor, gamma: torch.Tensor | None, beta: 
 
 @functools.lru_cache(maxsize=256)
 def xnor_layer_norm_bwd_workspace_bytes(dtype: torch.dtype, rows: int, cols: int) -> int:
+    _counted("xnor_layer_norm_bwd_workspace_bytes", rows, cols)
     n = ctypes.c_size_t()
     _ok(lib.xnor_layer_norm_bwd_workspace_bytes(_real(dtype, "x"), rows, cols, ctypes.byref(n)), "xnor_layer_norm_bwd_workspace_bytes")
     return n.value
@@ -876,6 +889,7 @@ def _gate_weights(wg: torch.Tensor, wu: torch.Tensor, dtype, K: int, where: str)
 
 @functools.lru_cache(maxsize=256)
 def xnor_gated_fwd_workspace_bytes(M: int, F: int, K: int, x_stride: int, w_stride: int) -> int:
+    _counted("xnor_gated_fwd_workspace_bytes", M, F, K)
     n = ctypes.c_size_t()
     _ok(lib.xnor_gated_fwd_workspace_bytes(M, F, K, x_stride, w_stride, ctypes.byref(n)), "xnor_gated_fwd_workspace_bytes")
     return n.value
@@ -905,6 +919,7 @@ def xnor_gated_fwd(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: int
 
 @functools.lru_cache(maxsize=256)
 def xnor_gated_bwd_workspace_bytes(M: int, F: int, K: int) -> int:
+    _counted("xnor_gated_bwd_workspace_bytes", M, F, K)
     n = ctypes.c_size_t()
     _ok(lib.xnor_gated_bwd_workspace_bytes(M, F, K, ctypes.byref(n)), "xnor_gated_bwd_workspace_bytes")
     return n.value

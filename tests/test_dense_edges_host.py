@@ -32,3 +32,68 @@ def test_asm_tells_the_compiler_of_m0():
                 users += 1
                 assert '"{m0}"' in statement, f"{name}: {statement}"
     assert users > 0
+
+
+class FakeMatrix:
+    """What the binding looks at of a tensor on the GPU, without its memory: sizes that this machine does not hold."""
+    is_cuda, device = True, "cuda:0"
+
+    def __init__(self, rows, cols, dtype):
+        self.shape, self.dtype = (rows, cols), dtype
+
+    def stride(self):
+        return (self.shape[1], 1)
+
+    def data_ptr(self):
+        return 0x1000
+
+    def is_contiguous(self):
+        return True
+
+
+class FakeVector(FakeMatrix):
+    def __init__(self, n, dtype=torch.float32):
+        self.shape, self.dtype = (n,), dtype
+
+
+@pytest.mark.parametrize("past", [1 << 31, (1 << 32) + 8, (1 << 33) + 16])
+def test_sizes_past_32_bits_are_refused(xb, monkeypatch, past):
+    """A size beyond what the library counts in is refused as one, never taken modulo 2^32 for a smaller one.  (Nothing is launched: the
+    library's calls are replaced.)"""
+    class Calls:
+        def __getattr__(self, name):
+            return getattr(xb_lib, name) if name in ("xnor_strerror", "xnor_last_hip_error") else lambda *a: pytest.fail(f"{name}{a}")
+    xb_lib = xb.lib
+    monkeypatch.setattr(xb, "lib", Calls())
+    monkeypatch.setattr(xb, "_stream", lambda: 0)
+    f32, f16, i8 = torch.float32, torch.float16, torch.int8
+    M = FakeMatrix
+
+    def refused(call, *args, **kw):
+        with pytest.raises(xb.XnorError) as e:
+            call(*args, **kw)
+        assert e.value.status == xb.E_SHAPE
+    for rows, cols in ((1, past), (past, 1)):
+        n, c = FakeVector(rows), FakeVector(cols)
+        refused(xb.xnor_int8_quantize, M(rows, cols, f32), M(rows, cols, i8), n)
+        refused(xb.xnor_layer_norm_fwd, M(rows, cols, f16), c, c, 1e-5, M(rows, cols, f16), n, n)
+        refused(xb.xnor_layer_norm_fwd_int8, M(rows, cols, f16), c, c, 1e-5, M(rows, cols, i8), n)
+        refused(xb.xnor_layer_norm_bwd, M(rows, cols, f32), M(rows, cols, f32), c, n, n, M(rows, cols, f32), c, c)
+        # tokens, weights or the contraction of that size
+        two = FakeVector(2)
+        refused(xb.xnor_int8_matmul, M(rows, cols, i8), n, M(2, cols, i8), two, out=M(rows, 2, f32))
+        refused(xb.xnor_int8_matmul, M(2, cols, i8), two, M(rows, cols, i8), n, out=M(2, rows, f32))
+        refused(xb.xnor_int8_linear, M(2, cols, f16), M(rows, cols, i8), n, out=M(2, rows, f16))
+        refused(xb.xnor_int8_gated, M(2, cols, i8), two, M(rows, cols, i8), n, M(rows, cols, i8), n, h=M(2, rows, f32))
+        refused(xb.xnor_gated_fwd, M(2, cols, f16), M(rows, cols, f16), M(rows, cols, f16), h=M(2, rows, f16))
+        refused(xb.xnor_gated_bwd, M(2, rows, f16), M(2, cols, f16), M(rows, cols, f16), M(rows, cols, f16), M(2, rows, f16), M(2, rows, f16),
+                dx=M(2, cols, f16), dwg=M(rows, cols, f16), dwu=M(rows, cols, f16))
+    with pytest.raises(xb.XnorError):
+        xb.xnor_int8_linear_workspace_bytes(100, past)
+    with pytest.raises(xb.XnorError):
+        xb.xnor_layer_norm_bwd_workspace_bytes(f32, 100, past)
+    for sizes in ((100, past, 64), (100, 64, past), (past, 64, 64)):
+        with pytest.raises(xb.XnorError):
+            xb.xnor_gated_bwd_workspace_bytes(*sizes)
+        with pytest.raises(xb.XnorError):
+            xb.xnor_gated_fwd_workspace_bytes(*sizes, 64, 64)
