@@ -707,7 +707,7 @@ def _out_rows(t: torch.Tensor | None, like: torch.Tensor, dtype, rows: int, cols
         t = torch.empty(rows, cols, dtype=dtype, device=like.device)        # (0.3 us less than new_empty with a shape)
         return t, t.data_ptr(), cols
     ptr, stride = _same(t, dtype, rows, cols, name)
-    return t, ptr, stride if rows > 1 else max(stride, cols)      # (one row's stride means nothing)
+    return t, ptr, stride if rows > 1 else cols      # (one row's stride means nothing)
 
 
 def _out_int8(q: torch.Tensor | None, like: torch.Tensor, rows: int, cols: int) -> tuple[torch.Tensor, int, int]:

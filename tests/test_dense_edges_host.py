@@ -97,3 +97,44 @@ def test_sizes_past_32_bits_are_refused(xb, monkeypatch, past):
             xb.xnor_gated_bwd_workspace_bytes(*sizes)
         with pytest.raises(xb.XnorError):
             xb.xnor_gated_fwd_workspace_bytes(*sizes, 64, 64)
+
+
+def test_one_row_has_no_stride(xb, monkeypatch):
+    """The stride of a matrix of one row (or none) means nothing: outputs that share one agree whatever theirs are."""
+    class Calls:
+        def __getattr__(self, name):
+            return getattr(xb_lib, name) if name.endswith("_bytes") else lambda *a: calls.append(a) or 0
+    xb_lib, calls = xb.lib, []
+    monkeypatch.setattr(xb, "lib", Calls())
+    monkeypatch.setattr(xb, "_stream", lambda: 0)
+
+    class Apart(FakeMatrix):
+        def __init__(self, rows, cols, stride, dtype=torch.float16):
+            super().__init__(rows, cols, dtype)
+            self.apart = stride
+
+        def stride(self):
+            return (self.apart, 1)
+    K, F = 64, 24
+    w = FakeMatrix(F, K, torch.float16)
+    for M in (0, 1):
+        x = FakeMatrix(M, K, torch.float16)
+        h, g, u = xb.xnor_gated_fwd(x, w, w, h=Apart(M, F, 100), g=Apart(M, F, 48), u=Apart(M, F, 7), want_pre=True)
+        assert calls.pop()[14] >= F
+        assert u.apart == 7 and g.apart == 48
+    one = FakeMatrix(1, K, torch.float16)
+    x, dh = FakeMatrix(5, K, torch.float16), FakeMatrix(5, 1, torch.float16)
+    xb.xnor_gated_bwd(dh, x, one, one, dh, dh, dx=x, dwg=Apart(1, K, 200), dwu=Apart(1, K, 64), workspace=FakeBytes(1 << 20))
+    assert calls.pop()[19] >= K
+    # of two rows the strides count
+    x = FakeMatrix(2, K, torch.float16)
+    with pytest.raises(ValueError):
+        xb.xnor_gated_fwd(x, w, w, h=Apart(2, F, 100), g=Apart(2, F, 48), u=Apart(2, F, 24), want_pre=True)
+
+
+class FakeBytes(FakeVector):
+    def __init__(self, n):
+        super().__init__(n, torch.uint8)
+
+    def numel(self):
+        return self.shape[0]

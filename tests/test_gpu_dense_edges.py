@@ -53,3 +53,23 @@ def test_norm_backward_of_millions_of_long_rows(xb):
         assert torch.equal(part, dx[:1].expand_as(part))
     del dx, part
     torch.cuda.empty_cache()
+
+
+def test_one_row_in_wider_buffers(xb):
+    """One token's g and u, and one hidden unit's weight gradients, each in a buffer of its own width."""
+    K, F = 72, 40
+    x, wg, wu = rand(1, 1, K, dtype=BF16), rand(2, F, K, dtype=BF16, std=0.1), rand(3, F, K, dtype=BF16, std=0.1)
+    held = [torch.full((1, F + spare), 5.0, dtype=BF16, device="cuda") for spare in (8, 3, 60)]
+    got = xb.xnor_gated_fwd(x, wg, wu, h=held[0][:, :F], g=held[1][:, :F], u=held[2][:, :F], want_pre=True)
+    want, bound = ref.gated(x, wg, wu, ref.SILU, BF16)
+    for t, w, e, name in zip(got, want, bound, "hgu"):
+        ref.assert_within(t, w, e, name)
+    assert all((t[:, F:] == 5.0).all() for t in held)
+    x, wg, wu = rand(4, 9, K, dtype=BF16), rand(5, 1, K, dtype=BF16), rand(6, 1, K, dtype=BF16)
+    dh, g, u = (rand(7 + i, 9, 1, dtype=BF16) for i in range(3))
+    held = [torch.full((1, K + spare), 5.0, dtype=BF16, device="cuda") for spare in (8, 33)]
+    got = xb.xnor_gated_bwd(dh, x, wg, wu, g, u, dwg=held[0][:, :K], dwu=held[1][:, :K])
+    want, bound = ref.gated_back(dh, x, wg, wu, g, u, ref.SILU, BF16)
+    for t, w, e, name in zip(got, want, bound, ("dx", "dwg", "dwu")):
+        ref.assert_within(t, w, e, name)
+    assert all((t[:, K:] == 5.0).all() for t in held)
