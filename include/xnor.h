@@ -529,7 +529,8 @@ int xnor_layer_norm_bwd(const void *dy, long long dy_stride, const void *x, int 
  *   g, u     out  [M][F] (one stride), rounded, for the backward pass; or both NULL.  h is formed from g and u before they are rounded.
  * _ws: with a workspace, into which operands whose rows do not all start at multiples of 16 bytes are copied first where that is faster
  * (the same values; XNOR_E_ALIGN if it is not 16-byte aligned; one that is too small, or NULL, is not used).
- * xnor_gated_fwd_workspace_bytes (host only) is 0 where none would be used with these strides.
+ * xnor_gated_fwd_workspace_bytes (host only) is 0 where none would be used for operands that start at multiples of 16 bytes and have these
+ * strides; for operands that start elsewhere it is asked with an odd stride.
  * Gradients, from those of h and the g and u that the forward pass left:
  *     dg = dh * u * act'(g), du = dh * act(g);  dx = dg wg + du wu, dwg = dg^T x, dwu = du^T x
  * dg and du are rounded to the block's type before the products, as the matrix instructions take them.

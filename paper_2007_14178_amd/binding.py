@@ -911,7 +911,8 @@ def xnor_gated_fwd(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: int
         u, up, u_stride = _out_rows(u, x, dtype, M, F, "u")
         if u_stride != gu_stride:
             raise ValueError("xnor_gated_fwd: g and u need the same row stride")
-    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_gated_fwd_workspace_bytes(M, F, K, x_stride, w_stride))
+    apart = x_stride if (x_ptr | g_w | u_w) % 16 == 0 else 1       # (an odd stride stands for operands that start off 16 bytes)
+    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_gated_fwd_workspace_bytes(M, F, K, apart, w_stride))
     _ok(lib.xnor_gated_fwd_ws(x_ptr, kind, x_stride, g_w, u_w, w_stride, act, M, F, K, h_ptr, h_stride, gp, up, gu_stride, ws, ws_bytes, _stream()),
         "xnor_gated_fwd")
     return (h, g, u) if want_pre else h

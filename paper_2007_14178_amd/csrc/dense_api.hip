@@ -15,7 +15,8 @@ int value_size(int type) { return type == XNOR_TYPE_FP32 ? 4 : type == XNOR_TYPE
 
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
-bool stride_fits(long long rows, long long stride) { return stride >= 0 && (rows <= 1 || stride <= (1LL << 60) / rows); }
+constexpr long long kMaxStride = 1LL << 60;
+bool stride_fits(long long rows, long long stride) { return stride >= 0 && (rows <= 1 || stride <= kMaxStride / rows); }
 
 // One matrix operand of a call.
 struct Matrix {
@@ -194,7 +195,9 @@ int xnor_gated_fwd_workspace_bytes(long long M, int F, int K, long long x_stride
 {
     if (!bytes) return XNOR_E_NULL;
     if (M < 0 || M > kMaxRows || F <= 0 || F > kMaxCols || K <= 0 || K > kMaxCols || x_stride < 0 || w_stride < 0) return XNOR_E_SHAPE;
-    *bytes = (x_stride % 8 || w_stride % 8) && gated_fwd_copy_pays(M, F, K) ? gated_fwd_workspace(M, F, K) : 0;
+    DenseArgs d{};
+    d.lda = 2 * std::min(x_stride, kMaxStride), d.ldb = 2 * std::min(w_stride, kMaxStride), d.K = K;
+    *bytes = !dense_direct_supports(d, XNOR_TYPE_F16) && gated_fwd_copy_pays(M, F, K) ? gated_fwd_workspace(M, F, K) : 0;
     return XNOR_OK;
 }
 

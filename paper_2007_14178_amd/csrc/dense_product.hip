@@ -464,7 +464,7 @@ __global__ __launch_bounds__(S::GROUPS * S::WAVES * kWave) __attribute__((amdgpu
 bool direct_supports(const DenseArgs &p, int size)
 {
     auto fits = [&](const void *q, long long ld) {
-        return (reinterpret_cast<uintptr_t>(q) & 15) == 0 && (ld & 15) == 0 && 255 * ld + (long long)p.K * size < 0x7fffffffLL;
+        return (reinterpret_cast<uintptr_t>(q) & 15) == 0 && (ld & 15) == 0 && ld <= (0x7ffffffeLL - (long long)p.K * size) / 255;
     };
     return fits(p.a, p.lda) && fits(p.b, p.ldb) && (!p.b2 || fits(p.b2, p.ldb));
 }

@@ -138,3 +138,33 @@ class FakeBytes(FakeVector):
 
     def numel(self):
         return self.shape[0]
+
+
+def test_gated_workspace_for_operands_off_16_bytes(xb, monkeypatch):
+    """The copies that a workspace allows are worth as much where an operand starts off 16 bytes, or its rows are too far apart for the
+    fetches of whole chunks, as where a stride is odd; the binding asks for one then."""
+    M, F, K = 300, 400, 3008
+    need = xb.xnor_gated_fwd_workspace_bytes(M, F, K, K + 1, K)
+    assert need > 0 and xb.xnor_gated_fwd_workspace_bytes(M, F, K, K, K) == 0
+    assert xb.xnor_gated_fwd_workspace_bytes(M, F, K, 1 << 23, K) == need == xb.xnor_gated_fwd_workspace_bytes(M, F, K, K, 1 << 23)
+    assert xb.xnor_gated_fwd_workspace_bytes(M, F, K, 1 << 60, K) == need
+
+    class Calls:
+        def __getattr__(self, name):
+            return getattr(xb_lib, name) if name.endswith("_bytes") else lambda *a: 0
+    xb_lib, asked = xb.lib, []
+    monkeypatch.setattr(xb, "lib", Calls())
+    monkeypatch.setattr(xb, "_stream", lambda: 0)
+    monkeypatch.setattr(xb, "_workspace", lambda given, like, nbytes: asked.append(nbytes) or (None, None, 0))
+
+    class At(FakeMatrix):
+        def __init__(self, rows, cols, ptr):
+            super().__init__(rows, cols, torch.float16)
+            self.ptr = ptr
+
+        def data_ptr(self):
+            return self.ptr
+    h = At(M, F, 0x1000)
+    for off in ((0, 0, 0), (2, 0, 0), (0, 8, 0), (0, 0, 14), (0, 16, 32)):
+        xb.xnor_gated_fwd(At(M, K, 0x1000 + off[0]), At(F, K, 0x2000 + off[1]), At(F, K, 0x3000 + off[2]), h=h)
+        assert asked.pop() == (need if any(o % 16 for o in off) else 0), off

@@ -73,3 +73,24 @@ def test_one_row_in_wider_buffers(xb):
     for t, w, e, name in zip(got, want, bound, ("dx", "dwg", "dwu")):
         ref.assert_within(t, w, e, name)
     assert all((t[:, K:] == 5.0).all() for t in held)
+
+
+@pytest.mark.parametrize("shifted", ["x", "wg", "wu", "all"])
+def test_gated_forward_off_16_bytes(xb, shifted):
+    """Strides of whole chunks, but operands that start a value behind one: copied, where a workspace allows it, as odd strides are."""
+    M, F, K = 300, 400, 3008
+    need = xb.xnor_gated_fwd_workspace_bytes(M, F, K, K + 1, K)
+    assert need > 0
+
+    def operand(seed, rows, name, **kw):
+        off = 1 if shifted in (name, "all") else 0
+        return rand(seed, rows, K + 8, dtype=F16, **kw)[:, off:off + K]
+    x, wg, wu = operand(1, M, "x"), operand(2, F, "wg", std=0.02), operand(3, F, "wu", std=0.02)
+    want, bound = ref.gated(x, wg, wu, ref.GELU, F16)
+    workspace = torch.full((need,), 77, dtype=torch.uint8, device="cuda")
+    for ws in (None, workspace):
+        got = xb.xnor_gated_fwd(x, wg, wu, ref.GELU, want_pre=True, workspace=ws)
+        for t, w, e, name in zip(got, want, bound, "hgu"):
+            ref.assert_within(t, w, e, name)
+    rows = workspace[:2 * M * K].view(torch.float16).view(M, K)         # x's copy
+    assert torch.equal(rows, x)
