@@ -482,10 +482,13 @@ int xnor_int8_matmul(const int8_t *a, long long a_stride, const float *a_scale, 
 /*
  * A linear layer with 8-bit weights on real tokens: xnor_int8_quantize of x and xnor_int8_matmul with w, the same values.
  *   workspace   16-byte aligned, xnor_int8_linear_workspace_bytes bytes (host only; 0 for up to two tokens of up to 8192 values, eight
- *               of up to 2048 and 16 of up to 1280, which are quantised by the product's own launch: then it may be NULL); its
+ *               of up to 2048 and 16 of up to 1280, which can be quantised by the product's own launch: then it may be NULL); its
  *               contents mean nothing afterwards
+ * That launch quantises such tokens again for every 16 outputs.  In wide layers they are quantised by a launch of their own, the same values in less
+ * time, given a workspace of xnor_int8_linear_layer_workspace_bytes (host only; what xnor_int8_linear_workspace_bytes says where no more is of use).
  */
 int xnor_int8_linear_workspace_bytes(long long M, int K, size_t *bytes);
+int xnor_int8_linear_layer_workspace_bytes(long long M, int N, int K, size_t *bytes);
 int xnor_int8_linear(const void *x, int x_type, long long x_stride, const int8_t *w, long long w_stride, const float *w_scale,
                      const float *bias, long long M, int N, int K, void *out, int out_type, long long out_stride,
                      void *workspace, size_t workspace_bytes, void *stream);

@@ -136,6 +136,7 @@ def _load() -> ctypes.CDLL:
     L.xnor_int8_quantize.argtypes = [vp, ci, ll, ci, ll, vp, ll, vp, vp]
     L.xnor_int8_matmul.argtypes = [vp, ll, vp, vp, ll, vp, vp, ll, ci, ci, vp, ci, ll, vp]
     L.xnor_int8_linear_workspace_bytes.argtypes = [ll, ci, ctypes.POINTER(sz)]
+    L.xnor_int8_linear_layer_workspace_bytes.argtypes = [ll, ci, ci, ctypes.POINTER(sz)]
     L.xnor_int8_linear.argtypes = [vp, ci, ll, vp, ll, vp, vp, ll, ci, ci, vp, ci, ll, vp, sz, vp]
     L.xnor_int8_gated.argtypes = [vp, ll, vp, vp, vp, vp, vp, ll, ci, ll, ci, ci, vp, ci, ll, vp]
     L.xnor_layer_norm_fwd.argtypes = [vp, ci, ll, ci, ll, vp, vp, ci, ctypes.c_float, vp, ll, vp, vp, vp]
@@ -147,7 +148,8 @@ def _load() -> ctypes.CDLL:
     L.xnor_gated_fwd_ws.argtypes = [vp, ci, ll, vp, vp, ll, ci, ll, ci, ci, vp, ll, vp, vp, ll, vp, sz, vp]
     L.xnor_gated_bwd_workspace_bytes.argtypes = [ll, ci, ci, ctypes.POINTER(sz)]
     L.xnor_gated_bwd.argtypes = [vp, ll, vp, ci, ll, vp, vp, ll, vp, vp, ll, ci, ll, ci, ci, vp, ll, vp, vp, ll, vp, sz, vp]
-    for name in ("xnor_int8_quantize", "xnor_int8_matmul", "xnor_int8_linear_workspace_bytes", "xnor_int8_linear", "xnor_int8_gated",
+    for name in ("xnor_int8_quantize", "xnor_int8_matmul", "xnor_int8_linear_workspace_bytes",
+                 "xnor_int8_linear_layer_workspace_bytes", "xnor_int8_linear", "xnor_int8_gated",
                  "xnor_layer_norm_fwd", "xnor_layer_norm_fwd_int8", "xnor_layer_norm_bwd_workspace_bytes", "xnor_layer_norm_bwd",
                  "xnor_gated_fwd", "xnor_gated_fwd_workspace_bytes", "xnor_gated_fwd_ws", "xnor_gated_bwd_workspace_bytes", "xnor_gated_bwd",
                  "xnor_out_dim", "xnor_packed_words", "xnor_binarize_pack", "xnor_scale_K",
@@ -770,18 +772,27 @@ def xnor_int8_matmul(a: torch.Tensor, a_scale: torch.Tensor, b: torch.Tensor, b_
     return out
 
 
-@functools.lru_cache(maxsize=256)       # asked on every call
+@functools.lru_cache(maxsize=256)
 def xnor_int8_linear_workspace_bytes(M: int, K: int) -> int:
-    _counted("xnor_int8_linear_workspace_bytes", M, K)
     n = ctypes.c_size_t()
+    _counted("xnor_int8_linear_workspace_bytes", M, K)
     _ok(lib.xnor_int8_linear_workspace_bytes(M, K, ctypes.byref(n)), "xnor_int8_linear_workspace_bytes")
+    return n.value
+
+
+@functools.lru_cache(maxsize=256)       # asked on every call
+def xnor_int8_linear_layer_workspace_bytes(M: int, N: int, K: int) -> int:
+    """What is of use to a layer of N outputs: in wide layers a few tokens are quantised once, not by every part of the product."""
+    n = ctypes.c_size_t()
+    _counted("xnor_int8_linear_layer_workspace_bytes", M, N, K)
+    _ok(lib.xnor_int8_linear_layer_workspace_bytes(M, N, K, ctypes.byref(n)), "xnor_int8_linear_layer_workspace_bytes")
     return n.value
 
 
 def xnor_int8_linear(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bias: torch.Tensor | None = None, out: torch.Tensor | None = None,
                      out_dtype: torch.dtype | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Linear layer with 8-bit weights w [N][K] on real tokens x [M][K], quantised on the way.  ``out_dtype`` (of a new
-    out): x's by default; ``workspace``: uint8, xnor_int8_linear_workspace_bytes, a new one by default."""
+    out): x's by default; ``workspace``: uint8, xnor_int8_linear_layer_workspace_bytes, a new one by default."""
     dtype = x.dtype
     x_kind = kind = _real(dtype, "x")
     M, K, x_ptr, x_stride = _rows(x, dtype, "x")
@@ -791,7 +802,7 @@ def xnor_int8_linear(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, bi
         dtype = out.dtype if out is not None else out_dtype
         kind = _real(dtype, "out")
     out, o_ptr, o_stride = _out_rows(out, x, dtype, M, N, "out")
-    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int8_linear_workspace_bytes(M, K))
+    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int8_linear_layer_workspace_bytes(M, N, K))
     _ok(lib.xnor_int8_linear(x_ptr, x_kind, x_stride, w_ptr, w_stride, _dev(w_scale, torch.float32, (N,), "w_scale"),
                              _dev(bias, torch.float32, (N,), "bias") if bias is not None else None, M, N, K, o_ptr, kind, o_stride,
                              ws, ws_bytes, _stream()), "xnor_int8_linear")

@@ -71,6 +71,7 @@ int norm_forward(const void *x, int x_type, long long rows, int cols, long long 
 }
 
 size_t q_stride_of(int K) { return ((size_t)K + 127) / 128 * 128; }       // whole cache lines
+size_t linear_workspace(long long M, int K) { return (size_t)M * (q_stride_of(K) + sizeof(float)); }
 
 }  // namespace
 
@@ -108,7 +109,15 @@ int xnor_int8_linear_workspace_bytes(long long M, int K, size_t *bytes)
 {
     if (!bytes) return XNOR_E_NULL;
     if (M < 0 || M > kMaxRows || K <= 0 || K > kMaxInt8Cols) return XNOR_E_SHAPE;
-    *bytes = dense_few_real_supports(M, K) ? 0 : (size_t)M * q_stride_of(K) + (size_t)M * sizeof(float);
+    *bytes = dense_few_real_supports(M, K) ? 0 : linear_workspace(M, K);
+    return XNOR_OK;
+}
+
+int xnor_int8_linear_layer_workspace_bytes(long long M, int N, int K, size_t *bytes)
+{
+    if (const int rc = xnor_int8_linear_workspace_bytes(M, K, bytes)) return rc;
+    if (N <= 0 || N > kMaxCols) return XNOR_E_SHAPE;
+    if (!dense_few_real_pays(M, N)) *bytes = linear_workspace(M, K);
     return XNOR_OK;
 }
 
@@ -125,7 +134,8 @@ int xnor_int8_linear(const void *x, int x_type, long long x_stride, const int8_t
     if (const int rc = check(all)) return rc;
     if (!aligned(bias, 4)) return XNOR_E_ALIGN;
     if (workspace_bytes < need) return XNOR_E_WORKSPACE;
-    if (M > 0 && need == 0) {
+    const bool alone = need > 0 || (workspace && workspace_bytes >= linear_workspace(M, K) && !dense_few_real_pays(M, N));
+    if (M > 0 && !alone) {
         DenseArgs d{};
         d.a = x, d.lda = x_stride * xs, d.b = w, d.ldb = w_stride, d.b_scale = w_scale, d.bias = bias;
         d.M = M, d.N = N, d.K = K, d.out = out, d.ldo = out_stride;

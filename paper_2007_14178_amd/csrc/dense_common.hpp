@@ -191,8 +191,9 @@ bool dense_direct_supports(const DenseArgs &p, int type);
 hipError_t launch_dense_gated(const DenseArgs &p, int type, hipStream_t st);                 // 16-bit
 hipError_t launch_dense_int8(const DenseArgs &p, int out_type, hipStream_t st);
 hipError_t launch_dense_int8_gated(const DenseArgs &p, int out_type, hipStream_t st);
-// The 8-bit product of real tokens, a and lda theirs, quantised in the kernel; where it takes them.
+// The 8-bit product of real tokens, a and lda theirs, quantised in the kernel; where it takes them, and where it is not slower for that.
 bool dense_few_real_supports(long long M, int K);
+bool dense_few_real_pays(long long M, int N);
 hipError_t launch_dense_few_real(const DenseArgs &p, int x_type, int out_type, hipStream_t st);
 
 struct RowArgs {

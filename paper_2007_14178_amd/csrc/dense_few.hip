@@ -11,9 +11,8 @@ namespace xnor {
 namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * kWave;
-// Real tokens that are quantised in the product's launch, by every workgroup for itself: one or two by all its waves together, shorter ones by a
-// wave each, up to eight, or, still shorter, by a wave each two.  (GPU time 8 x 1037 x 1531 f16 6.6 us, by two launches 8.0; 16 tokens 9.0 and 8.1,
-// but two launches take the host 4.4 us more, which is what passes of this size take; 16 x 2048 x 8192 13.2 and 10.2.)
+// Real tokens that can be quantised in the product's launch, by every workgroup for itself: one or two by all its waves together, shorter ones by a
+// wave each, up to eight, or, still shorter, by a wave each two.
 constexpr int kTogether = 2, kTogetherCols = 8192, kRealTokens = 2 * kWaves, kRealCols = 2048, kRealColsOfTwo = 1280;
 
 // X: the type of real tokens, quantised by every workgroup for itself; void: a holds T.
@@ -219,6 +218,20 @@ template hipError_t launch_few<bf16_t, bf16_t, kGated>(const DenseArgs &, hipStr
 bool dense_few_real_supports(long long M, int K)
 {
     return M <= kTogether ? K <= kTogetherCols : M <= kWaves ? K <= kRealCols : M <= kRealTokens && K <= kRealColsOfTwo;
+}
+
+// Two workgroups fit on a unit, and those of a second round quantise all tokens once more behind the first: then a launch of its own for the
+// tokens is the faster form, for one token from the third round on.  With more than eight tokens already a second workgroup on a unit costs more than
+// the host's 4 us for another launch, which passes of this size take.  GPU time in us by one launch and by two, f16 (the host's call 7 and 11):
+//     tokens x inner    N = 4096         8192           10240          16384          49152
+//     1 x 4096          7.5  9.0     10.4  12.4     14.3  15.5     17.7  18.4     45.6  43.6
+//     3 x 1280          6.0  6.8      7.3   7.6     10.8   9.2     12.1  10.5     30.6  21.4
+//     8 x 2048          7.0  7.9      9.2   9.4     12.3  11.5     15.7  13.6     36.6  28.1
+//    16 x 256           7.5  5.7      9.4   5.9     13.4   6.8     16.1   7.7     42.4  14.5
+//    16 x 1280          8.9  7.4     11.5   8.6     16.6  10.4     19.9  11.9     50.9  24.8
+bool dense_few_real_pays(long long M, int N)
+{
+    return ceil_div(N, 16) <= (M == 1 ? 4 : M <= kWaves ? 2 : 1) * kPlanUnits;
 }
 
 template <class X>

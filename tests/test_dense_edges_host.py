@@ -1,4 +1,5 @@
 """Edges of the dense operators that show on the host: workspaces of empty inputs, sizes past 32 bits, rows whose stride means nothing."""
+import ctypes
 import os
 import re
 
@@ -168,3 +169,19 @@ def test_gated_workspace_for_operands_off_16_bytes(xb, monkeypatch):
     for off in ((0, 0, 0), (2, 0, 0), (0, 8, 0), (0, 0, 14), (0, 16, 32)):
         xb.xnor_gated_fwd(At(M, K, 0x1000 + off[0]), At(F, K, 0x2000 + off[1]), At(F, K, 0x3000 + off[2]), h=h)
         assert asked.pop() == (need if any(o % 16 for o in off) else 0), off
+
+
+def test_linear_workspace_by_the_layers_width(xb):
+    """A few tokens are quantised by the product's own launch in narrow layers only, and a workspace for a launch of theirs in wide ones."""
+    ask, least = xb.xnor_int8_linear_layer_workspace_bytes, xb.xnor_int8_linear_workspace_bytes
+    for M, K, narrow in ((1, 4096, 16384), (2, 8192, 8192), (3, 2048, 8192), (8, 256, 8192), (9, 1280, 4096), (16, 1, 4096)):
+        assert least(M, K) == 0 and ask(M, narrow, K) == 0 and ask(M, 1, K) == 0
+        assert ask(M, narrow + 1, K) == ask(M, 50000, K) == M * ((K + 127) // 128 * 128 + 4)
+    # where the product's launch does not take them the width makes no difference
+    for M, K in ((1, 8193), (3, 2049), (9, 1281), (17, 64), (1000, 4096)):
+        assert ask(M, 1, K) == ask(M, 50000, K) == least(M, K) > 0
+    assert ask(0, 64, 64) == ask(0, 50000, 64) == 0
+    n = ctypes.c_size_t()
+    assert xb.lib.xnor_int8_linear_layer_workspace_bytes(4, 64, 64, None) == xb.E_NULL
+    for M, N, K in ((-1, 64, 64), (4, 0, 64), (4, 64, 0), (4, 64, 1 << 17), (4, (1 << 26) + 1, 64)):
+        assert xb.lib.xnor_int8_linear_layer_workspace_bytes(M, N, K, ctypes.byref(n)) == xb.E_SHAPE

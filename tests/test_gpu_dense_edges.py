@@ -94,3 +94,27 @@ def test_gated_forward_off_16_bytes(xb, shifted):
             ref.assert_within(t, w, e, name)
     rows = workspace[:2 * M * K].view(torch.float16).view(M, K)         # x's copy
     assert torch.equal(rows, x)
+
+
+@pytest.mark.parametrize("M,K", [(1, 300), (2, 1037), (3, 2000), (8, 256), (9, 1280), (16, 77)])
+def test_int8_linear_wide(xb, M, K):
+    """A few tokens on wide layers: with the workspace they are quantised once, without one by every part of the product, and on both
+    sides of the width where that changes the values are the same."""
+    x, bias = rand(M, M, K, dtype=BF16), rand(9, 20000)
+    w, sw = xb.xnor_int8_quantize(rand(2, 20000, K))
+    q, s = ref.quantize(x)
+    for N in (4096, 4097, 8192, 8193, 16385, 20000):
+        out = xb.xnor_int8_linear(x, w[:N], sw[:N].contiguous(), bias[:N].contiguous())
+        want, bound = ref.int8_matmul(q, s, w[:N], sw[:N], bias[:N], BF16)
+        ref.assert_within(out, want, bound, f"N {N}")
+        need = xb.xnor_int8_linear_layer_workspace_bytes(M, N, K)
+        for nbytes in (16, max(16, need)):
+            workspace = torch.full((nbytes,), 99, dtype=torch.uint8, device="cuda")
+            again = xb.xnor_int8_linear(x, w[:N], sw[:N].contiguous(), bias[:N].contiguous(), workspace=workspace)
+            assert torch.equal(out, again)
+            if nbytes == need:
+                assert torch.equal(workspace[:need - 4 * M].view(torch.int8).view(M, -1)[:, :K].cpu(), q)
+            else:
+                assert (workspace == 99).all()
+    x[0, K // 2] = float("nan")
+    assert xb.xnor_int8_linear(x, w, sw)[0].isnan().all() and not xb.xnor_int8_linear(x, w, sw)[1:].isnan().any()
