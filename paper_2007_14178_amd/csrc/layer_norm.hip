@@ -45,6 +45,17 @@ inline bool whole_rows(const void *x, long long stride, int cols, int value_byte
     return (((uintptr_t)x | (uintptr_t)(stride * value_bytes) | (uintptr_t)cols * value_bytes) & 15) == 0;
 }
 
+// v rounded to T from fp32.  The compiler folds the last multiply-add of some values into the conversion to f16, which rounds once where the others
+// round twice; it chooses anew in each copy of the code that takes the rows in turns, and a row's output would depend on its place among the rows.
+template <class T>
+__device__ inline T rounded(float v)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    if constexpr (std::is_same<T, f16_t>::value) asm("" : "+v"(v));
+#endif
+    return (T)v;
+}
+
 constexpr int block_of(int threads) { return threads < kBlock ? kBlock : threads; }
 
 // Rows by THREADS threads each, NV chunks of 16 bytes of a row in a thread's registers, and with them the parameters of its
@@ -138,7 +149,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void row_kernel(const RowArgs p)
                 values(at, c, i, v);
                 T out[V];
 #pragma unroll
-                for (int k = 0; k < V; ++k) out[k] = (T)v[k];
+                for (int k = 0; k < V; ++k) out[k] = rounded<T>(v[k]);
                 store_values(y, at, p.cols, out);
             });
         } else {
@@ -306,7 +317,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void norm_back_kernel(const Norm
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const float xh = ((float)cx[i].v[k] - mean) * rstd;
-                out[k] = (T)(rstd * ((float)cd[i].v[k] * gamma[i][k] - s1 - xh * s2));
+                out[k] = rounded<T>(rstd * ((float)cd[i].v[k] * gamma[i][k] - s1 - xh * s2));
             }
             store_values(dx, at, p.cols, out);
         }
@@ -389,7 +400,7 @@ __global__ __launch_bounds__(kLongThreads) void norm_back_long_kernel(const Norm
             load_params((const P *)p.gamma, at, p.cols, 1.f, gamma);
             T out[V];
 #pragma unroll
-            for (int k = 0; k < V; ++k) out[k] = (T)(rstd * ((float)cd.v[k] * gamma[k] - s1 - ((float)cx.v[k] - mean) * rstd * s2));
+            for (int k = 0; k < V; ++k) out[k] = rounded<T>(rstd * ((float)cd.v[k] * gamma[k] - s1 - ((float)cx.v[k] - mean) * rstd * s2));
             store_values(dx, at, p.cols, out);
         }
     }

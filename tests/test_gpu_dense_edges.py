@@ -118,3 +118,47 @@ def test_int8_linear_wide(xb, M, K):
                 assert (workspace == 99).all()
     x[0, K // 2] = float("nan")
     assert xb.xnor_int8_linear(x, w, sw)[0].isnan().all() and not xb.xnor_int8_linear(x, w, sw)[1:].isnan().any()
+
+
+def repeated(seed, rows, cols, dtype, std=1.0, period=61):
+    """`period` rows over and over (61 shares no factor with a tile, a grid or a workgroup's rows)."""
+    return rand(seed, period, cols, dtype=dtype, std=std).repeat((rows + period - 1) // period, 1)[:rows]
+
+
+def assert_repeats(outputs, what, period=61):
+    for i, t in enumerate(outputs):
+        assert torch.equal(t[:-period], t[period:]), f"{what}: output {i} differs in {int((t[:-period] != t[period:]).sum())} of {t.numel()} values"
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16], ids=str)
+@pytest.mark.parametrize("rows,cols", [(40003, 512), (35001, 264), (35001, 263), (12501, 2048), (9001, 4096), (9002, 8192), (3001, 16384), (3001, 1111), (1001, 40000)])
+def test_rows_do_not_depend_on_their_place(xb, dtype, rows, cols):
+    """The same row gives the same bits wherever it stands among the others."""
+    x, dy = repeated(1, rows, cols, dtype), repeated(2, rows, cols, dtype)
+    assert_repeats(xb.xnor_int8_quantize(x), "quantise")
+    for p_dtype in {F32, dtype}:
+        gamma, beta = (1.0 + rand(5, cols, std=0.2)).to(p_dtype), rand(6, cols, dtype=p_dtype)
+        assert_repeats(xb.xnor_layer_norm_fwd_int8(x, gamma, beta, EPS), "quantised norm")
+        y, mean, rstd = xb.xnor_layer_norm_fwd(x, gamma, beta, EPS)
+        assert_repeats((y, mean, rstd), "norm")
+        assert_repeats(xb.xnor_layer_norm_bwd(dy, x, gamma, mean, rstd)[:1], "norm backward")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=str)
+@pytest.mark.parametrize("M,F,K", [(64, 200, 256), (500, 333, 328), (500, 333, 331), (1300, 900, 1000), (4100, 4096, 1104), (128, 640, 4096)])
+def test_tokens_do_not_depend_on_their_place(xb, dtype, M, F, K):
+    """The same token gives the same bits wherever it stands, in a product's tile or in another one."""
+    period = 61 if M > 64 else 13
+    a, sa = xb.xnor_int8_quantize(repeated(1, M, K, F32, period=period))
+    (wg, sg), (wu, su) = xb.xnor_int8_quantize(rand(2, F, K, std=K ** -0.5)), xb.xnor_int8_quantize(rand(3, F, K, std=K ** -0.5))
+    bias = rand(4, F)
+    for out_dtype in (F32, dtype):
+        assert_repeats([xb.xnor_int8_matmul(a, sa, wg, sg, bias, out_dtype=out_dtype)], "8-bit product", period)
+        for kind in (ref.SILU, ref.GELU, ref.RELU):
+            assert_repeats([xb.xnor_int8_gated(a, sa, wg, sg, wu, su, kind, out_dtype=out_dtype)], "8-bit gated", period)
+    x = repeated(5, M, K, dtype, period=period)
+    w = [rand(6 + i, F, K, dtype=dtype, std=K ** -0.5) for i in range(2)]
+    dh, g, u = (repeated(8 + i, M, F, dtype, period=period) for i in range(3))
+    for kind in (ref.SILU, ref.GELU, ref.RELU):
+        assert_repeats(xb.xnor_gated_fwd(x, *w, kind, want_pre=True), "gated", period)
+        assert_repeats(xb.xnor_gated_bwd(dh, x, *w, g, u, kind)[:1], "gated backward, dx", period)
