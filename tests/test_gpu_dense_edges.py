@@ -162,3 +162,57 @@ def test_tokens_do_not_depend_on_their_place(xb, dtype, M, F, K):
     for kind in (ref.SILU, ref.GELU, ref.RELU):
         assert_repeats(xb.xnor_gated_fwd(x, *w, kind, want_pre=True), "gated", period)
         assert_repeats(xb.xnor_gated_bwd(dh, x, *w, g, u, kind)[:1], "gated backward, dx", period)
+
+
+def sampled(rows):
+    """Rows of the first turns of a grid of 1024, 4096 and 16384 rows, and of each turn after, on both sides of where it begins."""
+    at = {0, 1, 2, rows // 2, rows - 3, rows - 2, rows - 1}
+    for grid in (1024, 4096, 16384):
+        for turn in range(1, 10):
+            at |= {turn * grid - 1, turn * grid, turn * grid + 1, turn * grid + 3}
+    return torch.tensor(sorted(r for r in at if 0 <= r < rows))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=str)
+@pytest.mark.parametrize("rows,cols", [(40003, 512), (35001, 264), (12501, 2048), (9001, 4096), (9002, 8192), (2501, 8192), (2501, 16384)])
+def test_rows_in_turns(xb, dtype, rows, cols):
+    """More rows of whole 16-byte chunks than a launch holds at a time: each workgroup takes several, with two on their way, up to an odd
+    number of turns and a last one that some workgroups have no row for.  Rows differ in size by powers of two, so that one row's
+    sums or maximum in another's place show."""
+    x = rand(cols, 61, cols, dtype=dtype).repeat((rows + 60) // 61, 1)[:rows]          # (61 shares no factor with a grid)
+    x = x * torch.exp2((torch.arange(rows, device="cuda") % 7 - 3).float())[:, None].to(dtype) + (torch.arange(rows, device="cuda") % 5)[:, None].to(dtype)
+    gamma, beta = 1.0 + rand(5, cols, std=0.2), rand(6, cols)
+    r = sampled(rows)
+    some = x[r.cuda()]
+    q, s = xb.xnor_int8_quantize(x)
+    q0, s0 = ref.quantize(some)
+    assert torch.equal(q[r.cuda()].cpu(), q0) and torch.equal(s[r.cuda()].cpu(), s0)
+    got = xb.xnor_layer_norm_fwd(x, gamma, beta, EPS)
+    want, bound = ref.norm(some, gamma, beta, EPS, dtype)
+    for t, w, e, name in zip(got, want, bound, ("y", "mean", "rstd")):
+        ref.assert_within(t[r.cuda()], w, e, name)
+    q, s = xb.xnor_layer_norm_fwd_int8(x, gamma, beta, EPS)
+    (y, _, _), (e, _, _) = ref.norm(some, gamma, beta, EPS, None)
+    top, e_top = y.abs().amax(1), e.amax(1)
+    ref.assert_within(s[r.cuda()], top / 127, e_top / 127 + 2 * ref.U * top / 127, "scale")
+    level = s[r.cuda()].cpu().double()[:, None]
+    ref.assert_within(q[r.cuda()].cpu().double() * level, y, 0.5 * level + e + 127 * 4 * ref.U * level, "levels")
+
+
+@pytest.mark.parametrize("kind", [ref.SILU, ref.GELU])
+@pytest.mark.parametrize("M,F,K", [(4090, 4081, 1104), (4096, 4096, 2000), (8150, 2040, 1168)])
+def test_large_int8_gated_ends_inside_a_step(xb, kind, M, F, K):
+    """Tiles of 256 x 256 on rows at multiples of 16 bytes, with a contraction that is no multiple of 128."""
+    a, wg, wu = (torch.randint(-128, 128, (n, K + 16), generator=torch.Generator().manual_seed(K + i), dtype=torch.int32).to(torch.int8).cuda()[:, :K]
+                 for i, n in enumerate((M, F, F)))
+    sa, sg, su = rand(1, M).abs() * 0.01 + 1e-3, rand(2, F).abs() * 1e-3 + 1e-4, rand(3, F).abs() * 1e-3 + 1e-4
+
+    def some(n):
+        return torch.tensor(sorted({0, 1, 127, 128, 255, 256, 257, n // 2, n // 256 * 256 - 1, n - 2, n - 1}))
+    for dtype in (F32, BF16):
+        held = torch.full((M, F + 3), 5.0, dtype=dtype, device="cuda")
+        h = xb.xnor_int8_gated(a, sa, wg, sg, wu, su, kind, h=held[:, :F])
+        for r, c in ((some(M), torch.arange(F)), (torch.arange(M), some(F))):
+            want, bound = ref.int8_gated(a[r], sa[r], wg[c], sg[c], wu[c], su[c], kind, dtype)
+            ref.assert_within(h[r.cuda()][:, c.cuda()], want, bound, str(dtype))
+        assert (held[:, F:] == 5.0).all()
