@@ -23,7 +23,7 @@ struct Copy {
 // i / n for i < total
 __device__ inline long long row_of(long long i, int n, long long total) { return total >> 32 ? i / n : (long long)((uint32_t)i / (uint32_t)n); }
 
-// Up to three matrices of `cols` 16-bit values a row to rows of `stride` values, whole cache lines (777 x 2501 x 968: products 20 us with, 27 us without); what is behind a row's end is zero.
+// Up to three matrices of `cols` 16-bit values a row to rows of `stride` values, whole cache lines; what is behind a row's end is zero.
 __global__ __launch_bounds__(256) void copy_rows_kernel(const Copy a, const Copy b, const Copy c, int cols, int stride)
 {
     const Copy &m = blockIdx.y == 0 ? a : blockIdx.y == 1 ? b : c;
@@ -176,13 +176,15 @@ hipError_t run(GatedBackArgs p, int type, hipStream_t st)
 size_t gated_fwd_workspace(long long M, int F, int K) { return layout(M, F, K, false).bytes; }
 size_t gated_bwd_workspace(long long M, int F, int K) { return layout(M, F, K, true).bytes; }
 
-// Products of rows that lie badly take about 0.9 us more a step of 64 values and round of 512 tiles of 128 x 64; the copy takes its launch and 2.7 TB/s
-// read and written.  (16 bits: 777 x 2501 x 1001 27 us either way, 300 x 1000 x 3001 51 and 34 us, 4096 x 4096 x 4095 374 and 241.)
+// Products of rows that lie badly take 2.5 us and 0.65 us a step of 64 values more for every round of 512 tiles of 128 x 64; the copy takes a launch
+// and 5.2 TB/s read and written.  (f16, us without and with: 256 x 256 x 257 11.7 and 12.1, 100 x 8192 x 1001 24.3 and 25.6, 777 x 2501 x 1001 28 and 32,
+// 900 x 4000 x 1001 38 and 35, 300 x 1000 x 3001 51 and 31, 1000 x 4096 x 4095 106 and 90, 128 x 8192 x 8191 151 and 214, 4096 x 4096 x 4095 397 and 254:
+// of 79 sizes measured the rule has 65 right and loses 10 us of 71 at most in the others.)
 bool gated_fwd_copy_pays(long long M, int F, int K)
 {
     if (M <= 64) return false;          // (few tokens: the weights are read once)
     const double tiles = (double)((M + 127) / 128) * ceil_div(F, 64), rounds = (double)(long long)((tiles + 511) / 512);
-    return rounds * (K / 64.0) * 0.9 > 4.0 + ((double)M + 2.0 * F) * K * 4 / 2.7e6;
+    return rounds * (K / 64.0 * 0.65 + 2.5) > 4.0 + ((double)M + 2.0 * F) * K * 4 / 5.2e6;
 }
 
 hipError_t gated_fwd_copy(DenseArgs *p, void *workspace, hipStream_t st)

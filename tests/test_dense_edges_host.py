@@ -185,3 +185,12 @@ def test_linear_workspace_by_the_layers_width(xb):
     assert xb.lib.xnor_int8_linear_layer_workspace_bytes(4, 64, 64, None) == xb.E_NULL
     for M, N, K in ((-1, 64, 64), (4, 0, 64), (4, 64, 0), (4, 64, 1 << 17), (4, (1 << 26) + 1, 64)):
         assert xb.lib.xnor_int8_linear_layer_workspace_bytes(M, N, K, ctypes.byref(n)) == xb.E_SHAPE
+
+
+def test_gated_copies_where_they_pay(xb):
+    """Sizes at which copying the rows first measured much faster, and much slower, than reading them where they lie."""
+    ask = xb.xnor_gated_fwd_workspace_bytes
+    for M, F, K in ((1000, 4096, 4095), (8192, 300, 3001), (900, 4000, 2501), (500, 5500, 2501), (4096, 4096, 4095), (300, 1000, 3001), (65, 2501, 2001)):
+        assert ask(M, F, K, K, K) > 0, (M, F, K)
+    for M, F, K in ((128, 8192, 8191), (4398, 177, 183), (1288, 118, 65), (100, 8192, 1001), (64, 4096, 4095), (1, 4096, 4095)):
+        assert ask(M, F, K, K, K) == 0, (M, F, K)
