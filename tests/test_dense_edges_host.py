@@ -194,3 +194,23 @@ def test_gated_copies_where_they_pay(xb):
         assert ask(M, F, K, K, K) > 0, (M, F, K)
     for M, F, K in ((128, 8192, 8191), (4398, 177, 183), (1288, 118, 65), (100, 8192, 1001), (64, 4096, 4095), (1, 4096, 4095)):
         assert ask(M, F, K, K, K) == 0, (M, F, K)
+
+
+def test_fit_of_erfc():
+    """The coefficients in the source against erfc in 64 bits: the fit itself, and what fp32 leaves of it with an exact exponential."""
+    np, special = pytest.importorskip("numpy"), pytest.importorskip("scipy.special")
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2007_14178_amd", "csrc")
+    body = open(os.path.join(csrc, "dense_common.hpp")).read().split("float erfc_short(float z)")[1].split("\n}")[0]
+    p = [float(body.split("float p = ")[1].split("f;")[0])] + [float(sign + c) for sign, c in re.findall(r"p = p \* t ([+-]) ([0-9.]+)f;", body)]
+    assert len(p) == 8
+    z = np.linspace(0.0, 14.0, 100001)
+    t = 1.0 / (1.0 + 0.5 * z)
+    assert np.abs(np.polyval(p, t) - np.log(special.erfcx(z) / t)).max() < 7e-7
+    z = np.linspace(0.0, 9.0, 300001).astype(np.float32)
+    t = np.float32(1.0) / (np.float32(1.0) + np.float32(0.5) * z)
+    v = np.full_like(t, np.float32(p[0]))
+    for c in p[1:]:
+        v = v * t + np.float32(c)
+    v = (v - z * z) * np.float32(1.44269504)
+    off = np.abs(t.astype(np.float64) * np.exp2(v.astype(np.float64)) / special.erfc(z.astype(np.float64)) - 1.0)
+    assert off[z <= 2].max() < 1.2e-6 and off[z <= 5].max() < 3.6e-6 and off.max() < 1.25e-5
