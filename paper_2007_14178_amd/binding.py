@@ -659,6 +659,7 @@ def xnor_conv2d_fwd_chain(Ipk: torch.Tensor, Wpk: torch.Tensor | None, K: torch.
 
 
 # ---- dense layers: 8-bit products, layer norm, the gated feed-forward block -------------------------------------------
+# (Plain calls, as all of this module: autograd records none of them, whatever their tensors require; gradients are the _bwd calls'.)
 
 TYPE_FP32, TYPE_F16, TYPE_BF16 = 0, 1, 2
 ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2

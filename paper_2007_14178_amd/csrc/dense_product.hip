@@ -100,8 +100,10 @@ __global__ __launch_bounds__(256, 2) void dense_tile_kernel(const DenseArgs p, i
 // What a phase has read is refilled in the next one with the rows of STEPS steps further on (16 bytes a lane, two instructions
 // a wave and part), 4 STEPS - 1 phases before they are read; at a phase's end the 4 STEPS - 2 youngest fetches may be under way.
 //
-// Bound by the matrix instructions and by what the card's power lets them clock at: 16384 x 8192 x 8192 8 bits 804-870 us, 2.53-2.73 POP/s,
-// no bank conflicts, the matrix pipes busy 59 % of the cycles (8192 x 8192 x 8192); gated f16 4096 x 4096 x 8192 410-440 us, 1.25-1.34 PFLOP/s.
+// Bound by the clock that the card's power leaves the matrix instructions, and by the phases' ends: 8192 x 8192 x 8192 on 8 bits takes 398 us (2.76
+// POP/s) at 1.9 GHz, with the matrix pipes busy 68 % of the cycles and no bank conflicts; a third of its waves' cycles are waits and barriers, and two waves
+// a SIMD do not always cover for each other.  16384 x 8192 x 8192 811 us over and over on the same operands, 880-965 us right after other work (2.71 and
+// 2.28-2.50 POP/s); gated 4096 x 4096 x 8192 f16 430 us, bf16 417 us, 1.28 and 1.32 PFLOP/s.
 // Instructions of 32 x 32 were slower: two accumulators' chains a wave depend on themselves, and their reads meet in the banks.
 // ------------------------------------------------------------------------------------------------
 constexpr int kFetches = 2;

@@ -3,8 +3,8 @@
 //   dg = dh u act'(g)   du = dh act(g)   dx = dg wg + du wu   dwg = dg^T x   dwu = du^T x
 // One pass forms [dg du] by token; the two products read it and the block's own operands as they lie, across their rows where the
 // contraction goes across.  dg and du are rounded to the block's type, which the matrix instructions take; everything
-// else is summed in fp32 and rounded once.  The products are nearly all of it (bf16, 8192 x 4096 x 8192: forming dg and du 150 us, 4.5 TB/s,
-// and the products 776-860 and 832-910 us, 1.1 TFLOP each); below a few hundred tokens it is the number of launches.
+// else is summed in fp32 and rounded once.  The products are nearly all of it (bf16, 8192 x 4096 x 8192: forming dg and du 136-150 us, 4.5-4.9
+// TB/s, and the products 753-882 and 832-927 us, 1.1 TFLOP each); below a few hundred tokens it is the number of launches.
 #include <algorithm>
 
 #include "dense_common.hpp"
