@@ -1,5 +1,6 @@
-"""The dense operators at the edges of what they take: no rows, more rows than one launch's workgroups hold, rows and columns in one piece
-of memory, widths at which another kernel takes over.  Tolerances are the bounds that dense_reference derives."""
+"""The dense operators at the edges of what they take: no rows, more rows than a launch's workgroups hold at a time, operands off 16 bytes and
+outputs in wider buffers, widths at which another kernel takes over, equal rows in different places.  Tolerances are the bounds that
+dense_reference derives."""
 import os
 import sys
 
