@@ -1,51 +1,13 @@
 // Host side of the dense layers' part of the C ABI: argument validation, then the launchers.
 #include <algorithm>
 
-#include "dense_common.hpp"
+#include "dense_check.hpp"
 
 namespace {
 
 using namespace xnor;
 
-constexpr long long kMaxRows = 0x7fffffffLL;
-constexpr int kMaxCols = 1 << 26;          // a launch of a workgroup of 512 for 16 outputs has fewer than 2^32 threads
 constexpr int kMaxInt8Cols = (1 << 17) - 1;        // |sum of K products of two int8| <= K 2^14 < 2^31
-
-int value_size(int type) { return type == XNOR_TYPE_FP32 ? 4 : type == XNOR_TYPE_F16 || type == XNOR_TYPE_BF16 ? 2 : 0; }
-
-bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-constexpr long long kMaxStride = 1LL << 60;
-bool stride_fits(long long rows, long long stride) { return stride >= 0 && (rows <= 1 || stride <= kMaxStride / rows); }
-
-// One matrix operand of a call.
-struct Matrix {
-    const void *p;
-    long long rows;
-    int cols;
-    long long stride;
-    int size;           // of a value
-    bool output;
-};
-
-// Status of a call's operands, in the order pointers, sizes, alignment.
-template <int COUNT>
-int check(const Matrix (&m)[COUNT])
-{
-    for (const Matrix &x : m)
-        if (x.rows > 0 && !x.p) return XNOR_E_NULL;
-    for (const Matrix &x : m) {
-        if (x.rows < 0 || x.rows > kMaxRows || x.cols <= 0 || x.cols > kMaxCols) return XNOR_E_SHAPE;
-        if (!stride_fits(x.rows, x.stride) || (x.output && x.stride < x.cols)) return XNOR_E_SHAPE;
-    }
-    for (const Matrix &x : m)
-        if (!aligned(x.p, x.size)) return XNOR_E_ALIGN;
-    return XNOR_OK;
-}
-
-Matrix vec(const void *p, long long n, int size, bool output = false) { return {p, n, 1, 1, size, output}; }
-
-bool known_act(int act) { return act == XNOR_ACT_SILU || act == XNOR_ACT_GELU || act == XNOR_ACT_RELU; }
 
 int norm_types(int x_type, int p_type, int *xs, int *ps)
 {
