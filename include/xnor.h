@@ -562,6 +562,112 @@ int xnor_int8_gated(const int8_t *a, long long a_stride, const float *a_scale, c
                     int h_type, long long h_stride, void *stream);
 
 /*
+ * Weights of 4 bits, with a scale (and a zero point) for each row and group of columns: a value stands for (level - zero) * scale, its level
+ * one of 0 .. 15.  What a matrix [rows][cols] consists of:
+ *   q           [rows] rows of 4 * ceil(cols / 8) bytes, q_stride bytes apart (a multiple of 4, at least those bytes; rows at multiples of 16
+ *               bytes are read faster).  Eight consecutive values are a little-endian 32-bit word: of these value 2 j stands in bits 4 j .. 4 j + 3
+ *               and value 2 j + 1 in bits 16 + 4 j .. 19 + 4 j.  Levels behind the last column may be anything.
+ *   scale       [groups][rows] (one group after the other), scale_type any; groups = ceil(cols / group)
+ *   zero        uint8 [groups][rows], each 0 .. 15, or NULL: 8 everywhere
+ *   group       columns that share a scale: 32, 64 or 128
+ * A stack of matrices (experts) holds them one after the other: matrix e's rows start at q + e * rows * q_stride, its scales at e * groups * rows.
+ */
+typedef struct {
+    const uint8_t *q;
+    long long q_stride;
+    const void *scale;
+    const uint8_t *zero;
+    int rows, cols, group, scale_type;
+} xnor_int4;
+
+/*
+ * Real weights to 4 bits, by row and group.  Without zero points (zero NULL) scale = top / 7 with top the group's largest magnitude, level =
+ * rint(w / scale) + 8; with them scale = (high - low) / 15, high and low the group's largest and smallest value and 0 among them, zero =
+ * rint(-low / scale), level = rint(w / scale) + zero; levels and zeros within 0 .. 15.  All in fp32, from the scale as it is stored.  A group whose
+ * scale comes out as 0 holds levels that stand for 0; one with a NaN, an infinity or a scale that scale_type does not hold has the scale
+ * NaN, so that what is computed from it is NaN.
+ *   w       in   [rows][cols], w_type any
+ *   q, scale, zero   out, as above, scale_type any; levels behind the last column are 0
+ * _pack: levels that are there already, uint8 [rows][cols] (of each the low four bits), into q.
+ * _dequantize: the values that a matrix stands for, out [rows][cols], out_type any.
+ */
+int xnor_int4_quantize(const void *w, int w_type, long long rows, int cols, long long w_stride, int group, uint8_t *q, long long q_stride,
+                       void *scale, int scale_type, uint8_t *zero, void *stream);
+int xnor_int4_pack(const uint8_t *levels, long long rows, int cols, long long levels_stride, uint8_t *q, long long q_stride, void *stream);
+int xnor_int4_dequantize(const xnor_int4 *w, void *out, int out_type, long long out_stride, void *stream);
+
+/*
+ * Products with such weights on real tokens:
+ *     linear   y = x w^T + bias                                     w [N][K]
+ *     gated    h = act(x wg^T) * (x wu^T)                           wg, wu [F][K], of one group, scale_type and q_stride, both with zeros or none
+ *   x      in   [M][K], type XNOR_TYPE_F16 or _BF16
+ *   bias   in   fp32 [N] or NULL
+ *   out    out  [M][rows of the weights], out_type any
+ * Sums are fp32.  For few tokens (and without a workspace) the products are of levels less their zero point, which the tokens' type holds
+ * exactly, and a group's sum is multiplied by its scale; for many a weight is rounded to the tokens' type first, as the matrix instructions take it.
+ *   workspace  16-byte aligned, xnor_int4_*_workspace_bytes bytes (host only), or NULL or smaller: then not used; its contents mean nothing
+ *              afterwards
+ */
+int xnor_int4_linear_workspace_bytes(long long M, int N, int K, size_t *bytes);
+int xnor_int4_linear(const void *x, int type, long long x_stride, const xnor_int4 *w, const float *bias, long long M, void *out, int out_type,
+                     long long out_stride, void *workspace, size_t workspace_bytes, void *stream);
+int xnor_int4_gated_workspace_bytes(long long M, int F, int K, size_t *bytes);
+int xnor_int4_gated(const void *x, int type, long long x_stride, const xnor_int4 *wg, const xnor_int4 *wu, int act, long long M, void *h, int h_type,
+                    long long h_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Routing of tokens to experts.
+ *   logits   in   [T][E], type any, E <= 1024
+ *   bias     in   fp32 [E] or NULL: added to the scores for the choice, not to the weights
+ * Scores p are the softmax of a token's logits, or each one's sigmoid; c = p + bias.  The experts are in `groups` groups of E / groups
+ * consecutive ones, a group's score the sum of its `group_top` (1 or 2) largest c; of a token's groups the groups_kept best stay, of their experts the
+ * k (1 .. 32) with the largest c are chosen, the largest first; equals go by the lower index.  All of that is formed in 64 bits.
+ *   experts  out  int32 [T][k]
+ *   weights  out  fp32 [T][k]: the chosen experts' p, divided by their sum if `renorm`, times `factor`
+ * An expert whose logit is -inf or whose c is -inf or NaN is never chosen.  Where there are fewer than k to choose, the rest of a token's
+ * experts is -1, of weight 0.  A token with a NaN among its logits (softmax: or +inf) has the experts -1 and weights NaN.  Weights whose sum is 0
+ * (scores too small for 64 bits) are 0.
+ * XNOR_E_UNSUPPORTED for another score; XNOR_E_SHAPE where groups does not divide E, 1 <= groups_kept <= groups or the other ranges do not
+ * hold, or k exceeds the experts of the groups kept, or T * k >= 2^31.
+ *
+ * _lists: of each expert the pairs (token t, slot s) that have it, as t k + s, ascending.
+ *   experts  in   int32 [T][k], values outside 0 .. E-1 stand for none; one expert may stand several times in a row
+ *   offsets  out  int32 [E + 1]: expert e's pairs are order[offsets[e]] .. order[offsets[e + 1] - 1]
+ *   order    out  int32 [T k]; behind offsets[E]: -1
+ *   workspace  16-byte aligned, xnor_route_lists_workspace_bytes bytes (host only; 0 for up to 1024 pairs: then it may be NULL)
+ *
+ * _bwd: the logits' gradient from the weights' (none flows through the choice, so none to the bias).  With dw' = factor * dweights and, if renorm,
+ * dw'' = (dw' - sum_s dw' p / S) / S with S the sum of the token's chosen p, in place of dw':  sigmoid: dlogit_e = dw' p (1 - p) for the chosen;
+ * softmax: dlogit_e = p_e (dw'_e - sum_s dw' p), dw'_e = 0 for others.  Slots without an expert count nothing; one expert in several slots gets the
+ * sum of theirs.  Tokens without any expert have gradients of 0, those of logits of -inf are 0.
+ *   dweights in   fp32 [T][k]           dlogits  out  [T][E], the logits' type
+ */
+typedef enum { XNOR_SCORE_SOFTMAX = 0, XNOR_SCORE_SIGMOID = 1 } xnor_score;
+int xnor_route_fwd(const void *logits, int type, long long T, int E, long long logits_stride, const float *bias, int score, int groups,
+                   int groups_kept, int group_top, int k, int renorm, float factor, int32_t *experts, float *weights, void *stream);
+int xnor_route_lists_workspace_bytes(long long T, int k, int E, size_t *bytes);
+int xnor_route_lists(const int32_t *experts, long long T, int k, int E, int32_t *offsets, int32_t *order, void *workspace, size_t workspace_bytes,
+                     void *stream);
+int xnor_route_bwd(const float *dweights, const void *logits, int type, long long T, int E, long long logits_stride, const int32_t *experts, int k,
+                   int score, int renorm, float factor, void *dlogits, long long dlogits_stride, void *stream);
+
+/*
+ * The chosen experts' gated blocks on 4-bit weights:
+ *     out[t] = sum_s weights[t][s] * ((act(x[t] wg_e^T) * (x[t] wu_e^T)) wd_e^T),  e = experts[t][s]
+ * slots in ascending order, in fp32; the gated blocks' outputs are rounded to the tokens' type, as the matrix instructions take them.  Slots whose
+ * expert is outside 0 .. E-1 add weight * 0 (so that the weights NaN of a token that could not be routed are seen).
+ *   x        in   [T][K], type XNOR_TYPE_F16 or _BF16
+ *   experts, weights   in   int32, fp32 [T][k], k <= 32, T k < 2^31
+ *   wg, wu   in   stacks of E matrices [F][K], as for xnor_int4_gated       wd  in  a stack of E matrices [N][F]; E <= 1024
+ *   out      out  [T][N], out_type any
+ *   workspace  16-byte aligned, xnor_int4_experts_workspace_bytes bytes (host only); its contents mean nothing afterwards
+ */
+int xnor_int4_experts_workspace_bytes(long long T, int k, int E, int K, int F, int N, size_t *bytes);
+int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, const int32_t *experts, const float *weights, int k, int E,
+                      const xnor_int4 *wg, const xnor_int4 *wu, const xnor_int4 *wd, int act, void *out, int out_type, long long out_stride,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Measurement probes (no part of the forward pass): what the GPU at hand sustains on the resources
  * the kernels above are priced against, for reading a roofline fraction against a measured
  * ceiling beside the published one.  Each enqueues one kernel on `stream` and returns; the caller

@@ -11,6 +11,7 @@ import ctypes
 import functools
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -40,6 +41,11 @@ class XnorError(RuntimeError):
 class CShape(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int) for k in
                 ("N", "C", "H", "W", "F", "kh", "kw", "sh", "sw", "ph", "pw")]
+
+
+class CInt4(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_stride", ctypes.c_longlong), ("scale", ctypes.c_void_p), ("zero", ctypes.c_void_p),
+                *((k, ctypes.c_int) for k in ("rows", "cols", "group", "scale_type"))]
 
 
 @dataclass(frozen=True)
@@ -97,6 +103,21 @@ def _load() -> ctypes.CDLL:
     L.xnor_prepare.argtypes = [vp, vp, sp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.xnor_conv2d_fwd.argtypes = [vp, vp, vp, vp, sp, vp, vp, vp, sz, vp]
     L.xnor_conv2d_fwd_algo.argtypes = [vp, vp, vp, vp, sp, vp, vp, vp, sz, ci, vp]
+    ll, cf = ctypes.c_longlong, ctypes.c_float
+    wp = ctypes.POINTER(CInt4)
+    L.xnor_int4_quantize.argtypes = [vp, ci, ll, ci, ll, ci, vp, ll, vp, ci, vp, vp]
+    L.xnor_int4_pack.argtypes = [vp, ll, ci, ll, vp, ll, vp]
+    L.xnor_int4_dequantize.argtypes = [wp, vp, ci, ll, vp]
+    L.xnor_int4_linear_workspace_bytes.argtypes = [ll, ci, ci, ctypes.POINTER(sz)]
+    L.xnor_int4_linear.argtypes = [vp, ci, ll, wp, vp, ll, vp, ci, ll, vp, sz, vp]
+    L.xnor_int4_gated_workspace_bytes.argtypes = [ll, ci, ci, ctypes.POINTER(sz)]
+    L.xnor_int4_gated.argtypes = [vp, ci, ll, wp, wp, ci, ll, vp, ci, ll, vp, sz, vp]
+    L.xnor_route_fwd.argtypes = [vp, ci, ll, ci, ll, vp, ci, ci, ci, ci, ci, ci, cf, vp, vp, vp]
+    L.xnor_route_lists_workspace_bytes.argtypes = [ll, ci, ci, ctypes.POINTER(sz)]
+    L.xnor_route_lists.argtypes = [vp, ll, ci, ci, vp, vp, vp, sz, vp]
+    L.xnor_route_bwd.argtypes = [vp, vp, ci, ll, ci, ll, vp, ci, ci, ci, cf, vp, ll, vp]
+    L.xnor_int4_experts_workspace_bytes.argtypes = [ll, ci, ci, ci, ci, ci, ctypes.POINTER(sz)]
+    L.xnor_int4_experts.argtypes = [vp, ci, ll, ll, vp, vp, ci, ci, wp, wp, wp, ci, vp, ci, ll, vp, sz, vp]
     L.xnor_conv2d_fwd_static.argtypes = [vp, vp, vp, vp, sp, vp, vp, vp]
     L.xnor_filter_expand.argtypes = [vp, sp, vp, sz, vp]
     dp = ctypes.POINTER(ctypes.c_double)
@@ -960,3 +981,244 @@ def xnor_gated_bwd(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torc
     _ok(lib.xnor_gated_bwd(d_ptr, d_stride, x_ptr, kind, x_stride, g_w, u_w, w_stride, g_ptr, u_ptr, gu_stride, act, M, F, K, dx_ptr, dx_stride,
                            dg_ptr, du_ptr, dw_stride, ws, ws_bytes, _stream()), "xnor_gated_bwd")
     return dx, dwg, dwu
+
+
+# ---- weights of 4 bits, routing to experts, the experts' gated blocks -----------------------------------------------------
+
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+
+
+class Int4(NamedTuple):
+    """A matrix of 4-bit weights, or a stack of them: q uint8 [rows][4 ceil(cols / 8)] (the library's order of levels: xnor_int4_pack), scale
+    [groups][rows] (fp32, f16, bf16), zero uint8 [groups][rows] or None for 8 everywhere; a stack's have one dimension more in front.  ``group``:
+    columns that share a scale, 32, 64 or 128."""
+    q: torch.Tensor
+    scale: torch.Tensor
+    zero: torch.Tensor | None
+    cols: int
+    group: int
+
+    @property
+    def rows(self) -> int:
+        return self.q.shape[-2]
+
+
+def _int4(w: Int4, name: str, cols: int | None = None, count: int | None = None) -> CInt4:
+    """The matrix (``count``: stack) as the library takes it, checked."""
+    q, scale, zero, K, group = w
+    many = () if count is None else (count,)
+    if group not in (32, 64, 128):
+        raise XnorError(E_UNSUPPORTED, f"{name}: group of {group}")
+    if cols is not None and K != cols:
+        raise ValueError(f"{name}: {K} columns, expected {cols}")
+    if q.dim() != 2 + len(many) or q.shape[:-2] != many:
+        raise ValueError(f"{name}.q: shape {tuple(q.shape)}, expected {(*many, 'rows', 'bytes')}")
+    N, held = q.shape[-2:]
+    if K < 1 or K > _MOST or N > _MOST:
+        raise XnorError(E_SHAPE, f"{name} of {N} x {K}")
+    if held != (K + 7) // 8 * 4:
+        raise ValueError(f"{name}.q: rows of {held} bytes, {K} columns take {(K + 7) // 8 * 4}")
+    stride = q.stride()
+    apart = stride[-2] if N > 1 else stride[0] if count is not None and count > 1 else held       # (one row's stride means nothing)
+    if not q.is_cuda or q.dtype is not torch.uint8 or stride[-1] != 1 or (count is not None and count > 1 and stride[0] != N * apart):
+        raise TypeError(f"{name}.q: need GPU rows of torch.uint8, a stack's at one distance, got {q.dtype} on {q.device}, strides {stride}")
+    kind = _real(scale.dtype, f"{name}.scale")
+    shape = (*many, (K + group - 1) // group, N)
+    return CInt4(q.data_ptr(), apart, _dev(scale, scale.dtype, shape, f"{name}.scale"),
+                 _dev(zero, torch.uint8, shape, f"{name}.zero") if zero is not None else None, N, K, group, kind)
+
+
+def _int4_rows(like: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
+    """Memory for rows of levels, at multiples of 64 bytes."""
+    held = (cols + 7) // 8 * 4
+    stride = (held + 63) // 64 * 64
+    return torch.empty_strided((rows, held), (stride, 1), dtype=torch.uint8, device=like.device)
+
+
+def xnor_int4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, scale_dtype: torch.dtype | None = None) -> Int4:
+    """Weights [rows][cols] (fp32, f16, bf16) to 4 bits by row and group of columns; ``zeros``: with a zero point for each group,
+    ``scale_dtype``: w's by default."""
+    kind = _real(w.dtype, "w")
+    if group not in (32, 64, 128):
+        raise XnorError(E_UNSUPPORTED, f"xnor_int4_quantize: group of {group}")
+    rows, cols, ptr, stride = _rows(w, w.dtype, "w")
+    q = _int4_rows(w, rows, cols)
+    groups = (cols + group - 1) // group
+    scale = torch.empty(groups, rows, dtype=scale_dtype or w.dtype, device=w.device)
+    zero = torch.empty(groups, rows, dtype=torch.uint8, device=w.device) if zeros else None
+    _ok(lib.xnor_int4_quantize(ptr, kind, rows, cols, stride, group, q.data_ptr(), q.stride(0), scale.data_ptr(), _real(scale.dtype, "scale"),
+                               zero.data_ptr() if zeros else None, _stream()), "xnor_int4_quantize")
+    return Int4(q, scale, zero, cols, group)
+
+
+def xnor_int4_pack(levels: torch.Tensor, q: torch.Tensor | None = None) -> torch.Tensor:
+    """Levels that are there already, uint8 [rows][cols] of 0 .. 15, in the library's order: q uint8 [rows][4 ceil(cols / 8)]."""
+    rows, cols, ptr, stride = _rows(levels, torch.uint8, "levels")
+    if q is None:
+        q = _int4_rows(levels, rows, cols)
+    q_ptr, q_stride = _same(q, torch.uint8, rows, (cols + 7) // 8 * 4, "q")
+    _ok(lib.xnor_int4_pack(ptr, rows, cols, stride, q_ptr, q_stride if rows > 1 else (cols + 7) // 8 * 4, _stream()), "xnor_int4_pack")
+    return q
+
+
+def xnor_int4_dequantize(w: Int4, out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """The values [rows][cols] that a matrix of 4-bit weights stands for."""
+    c = _int4(w, "w")
+    dtype = out.dtype if out is not None else out_dtype
+    kind = _real(dtype, "out")
+    out, o_ptr, o_stride = _out_rows(out, w.q, dtype, w.rows, w.cols, "out")
+    _ok(lib.xnor_int4_dequantize(ctypes.byref(c), o_ptr, kind, o_stride, _stream()), "xnor_int4_dequantize")
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def xnor_int4_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    _counted("xnor_int4_linear_workspace_bytes", M, N, K)
+    n = ctypes.c_size_t()
+    _ok(lib.xnor_int4_linear_workspace_bytes(M, N, K, ctypes.byref(n)), "xnor_int4_linear_workspace_bytes")
+    return n.value
+
+
+def xnor_int4_linear(x: torch.Tensor, w: Int4, bias: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                     out_dtype: torch.dtype | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Linear layer with 4-bit weights w [N][K] on tokens x [M][K] in f16 or bf16.  ``out_dtype`` (of a new out): x's by default;
+    ``workspace``: uint8, xnor_int4_linear_workspace_bytes, a new one by default."""
+    dtype = x.dtype
+    x_kind = kind = _real(dtype, "x")
+    M, K, x_ptr, x_stride = _rows(x, dtype, "x")
+    c = _int4(w, "w", K)
+    N = c.rows
+    if out is not None or out_dtype is not None:
+        dtype = out.dtype if out is not None else out_dtype
+        kind = _real(dtype, "out")
+    out, o_ptr, o_stride = _out_rows(out, x, dtype, M, N, "out")
+    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int4_linear_workspace_bytes(M, N, K))
+    _ok(lib.xnor_int4_linear(x_ptr, x_kind, x_stride, ctypes.byref(c), _dev(bias, torch.float32, (N,), "bias") if bias is not None else None, M,
+                             o_ptr, kind, o_stride, ws, ws_bytes, _stream()), "xnor_int4_linear")
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def xnor_int4_gated_workspace_bytes(M: int, F: int, K: int) -> int:
+    _counted("xnor_int4_gated_workspace_bytes", M, F, K)
+    n = ctypes.c_size_t()
+    _ok(lib.xnor_int4_gated_workspace_bytes(M, F, K, ctypes.byref(n)), "xnor_int4_gated_workspace_bytes")
+    return n.value
+
+
+def xnor_int4_gated(x: torch.Tensor, wg: Int4, wu: Int4, act: int = ACT_SILU, h: torch.Tensor | None = None,
+                    out_dtype: torch.dtype | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Gated block h = act(x wg^T) * (x wu^T) on 4-bit weights wg, wu [F][K] and tokens x [M][K] in f16 or bf16.  ``out_dtype`` (of a new h): x's
+    by default; ``workspace``: uint8, xnor_int4_gated_workspace_bytes, a new one by default."""
+    dtype = x.dtype
+    x_kind = kind = _real(dtype, "x")
+    M, K, x_ptr, x_stride = _rows(x, dtype, "x")
+    cg, cu = _int4(wg, "wg", K), _int4(wu, "wu", K)
+    F = cg.rows
+    if h is not None or out_dtype is not None:
+        dtype = h.dtype if h is not None else out_dtype
+        kind = _real(dtype, "h")
+    h, h_ptr, h_stride = _out_rows(h, x, dtype, M, F, "h")
+    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int4_gated_workspace_bytes(M, F, K))
+    _ok(lib.xnor_int4_gated(x_ptr, x_kind, x_stride, ctypes.byref(cg), ctypes.byref(cu), act, M, h_ptr, kind, h_stride, ws, ws_bytes, _stream()),
+        "xnor_int4_gated")
+    return h
+
+
+def _slots(t: torch.Tensor | None, like: torch.Tensor, dtype, T: int, k: int, name: str) -> tuple[torch.Tensor, int]:
+    """A contiguous output of one value a token and slot."""
+    if t is None:
+        t = torch.empty(T, k, dtype=dtype, device=like.device)
+        return t, t.data_ptr()
+    return t, _dev(t, dtype, (T, k), name)
+
+
+def xnor_route_fwd(logits: torch.Tensor, k: int, bias: torch.Tensor | None = None, score: int = SCORE_SOFTMAX, groups: int = 1, groups_kept: int = 1,
+                   group_top: int = 1, renorm: bool = True, factor: float = 1.0, experts: torch.Tensor | None = None,
+                   weights: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Chooses k experts for each token by logits [T][E] (fp32, f16, bf16): returns (experts int32 [T][k], weights fp32 [T][k]), the best first.
+    ``bias`` fp32 [E] is added to the scores for the choice alone; of ``groups`` groups of consecutive experts the ``groups_kept`` with the largest sums of
+    their ``group_top`` best stay; ``renorm``: weights are divided by their sum; ``factor`` multiplies them."""
+    kind = _real(logits.dtype, "logits")
+    T, E, ptr, stride = _rows(logits, logits.dtype, "logits")
+    _counted("xnor_route_fwd", k, groups, groups_kept, group_top, T * max(k, 0))
+    if not 0 < k <= 32:
+        raise XnorError(E_SHAPE, f"xnor_route_fwd: {k} experts a token")
+    experts, e_ptr = _slots(experts, logits, torch.int32, T, k, "experts")
+    weights, w_ptr = _slots(weights, logits, torch.float32, T, k, "weights")
+    _ok(lib.xnor_route_fwd(ptr, kind, T, E, stride, _dev(bias, torch.float32, (E,), "bias") if bias is not None else None, score, groups, groups_kept,
+                           group_top, k, bool(renorm), factor, e_ptr, w_ptr, _stream()), "xnor_route_fwd")
+    return experts, weights
+
+
+@functools.lru_cache(maxsize=256)
+def xnor_route_lists_workspace_bytes(T: int, k: int, E: int) -> int:
+    _counted("xnor_route_lists_workspace_bytes", T, k, E)
+    n = ctypes.c_size_t()
+    _ok(lib.xnor_route_lists_workspace_bytes(T, k, E, ctypes.byref(n)), "xnor_route_lists_workspace_bytes")
+    return n.value
+
+
+def xnor_route_lists(experts: torch.Tensor, E: int, offsets: torch.Tensor | None = None, order: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Of each of E experts the pairs (token t, slot s) of experts [T][k] that have it, as t k + s: returns (offsets int32 [E + 1], order
+    int32 [T k]); expert e's are order[offsets[e]:offsets[e + 1]], ascending; behind the last expert's stands -1."""
+    if experts.dim() != 2:
+        raise ValueError(f"experts: need a matrix, got shape {tuple(experts.shape)}")
+    T, k = experts.shape
+    e_ptr = _dev(experts, torch.int32, (T, k), "experts")
+    need = xnor_route_lists_workspace_bytes(T, k, E)
+    offsets, f_ptr = _out_vector(offsets, experts, torch.int32, E + 1, "offsets")
+    order, o_ptr = _out_vector(order, experts, torch.int32, T * k, "order")
+    workspace, ws, ws_bytes = _workspace(workspace, experts, need)
+    _ok(lib.xnor_route_lists(e_ptr, T, k, E, f_ptr, o_ptr, ws, ws_bytes, _stream()), "xnor_route_lists")
+    return offsets, order
+
+
+def xnor_route_bwd(dweights: torch.Tensor, logits: torch.Tensor, experts: torch.Tensor, score: int = SCORE_SOFTMAX, renorm: bool = True,
+                   factor: float = 1.0, dlogits: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient of xnor_route_fwd's weights: dlogits [T][E], in the logits' type, from dweights fp32 [T][k] and the experts that it chose."""
+    dtype = logits.dtype
+    kind = _real(dtype, "logits")
+    T, E, ptr, stride = _rows(logits, dtype, "logits")
+    if experts.dim() != 2:
+        raise ValueError(f"experts: need a matrix, got shape {tuple(experts.shape)}")
+    k = experts.shape[1]
+    _counted("xnor_route_bwd", k, T * k)
+    dlogits, d_ptr, d_stride = _out_rows(dlogits, logits, dtype, T, E, "dlogits")
+    _ok(lib.xnor_route_bwd(_dev(dweights, torch.float32, (T, k), "dweights"), ptr, kind, T, E, stride, _dev(experts, torch.int32, (T, k), "experts"), k,
+                           score, bool(renorm), factor, d_ptr, d_stride, _stream()), "xnor_route_bwd")
+    return dlogits
+
+
+@functools.lru_cache(maxsize=256)
+def xnor_int4_experts_workspace_bytes(T: int, k: int, E: int, K: int, F: int, N: int) -> int:
+    _counted("xnor_int4_experts_workspace_bytes", T, k, E, K, F, N)
+    n = ctypes.c_size_t()
+    _ok(lib.xnor_int4_experts_workspace_bytes(T, k, E, K, F, N, ctypes.byref(n)), "xnor_int4_experts_workspace_bytes")
+    return n.value
+
+
+def xnor_int4_experts(x: torch.Tensor, experts: torch.Tensor, weights: torch.Tensor, wg: Int4, wu: Int4, wd: Int4, act: int = ACT_SILU,
+                      out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """out[t] = the sum over token t's experts e (experts, weights [T][k], as xnor_route_fwd leaves them) of weight * (act(x wg_e^T) * (x wu_e^T)) wd_e^T,
+    on stacks of 4-bit weights wg, wu [E][F][K], wd [E][N][F], for tokens x [T][K] in f16 or bf16.  ``out_dtype`` (of a new out): x's by default;
+    ``workspace``: uint8, xnor_int4_experts_workspace_bytes, a new one by default."""
+    dtype = x.dtype
+    x_kind = kind = _real(dtype, "x")
+    T, K, x_ptr, x_stride = _rows(x, dtype, "x")
+    if experts.dim() != 2 or experts.shape[0] != T:
+        raise ValueError(f"experts: shape {tuple(experts.shape)}, expected {(T, 'k')}")
+    k, E = experts.shape[1], wg.q.shape[0]
+    cg, cu = _int4(wg, "wg", K, E), _int4(wu, "wu", K, E)
+    cd = _int4(wd, "wd", cg.rows, E)
+    N = cd.rows
+    if out is not None or out_dtype is not None:
+        dtype = out.dtype if out is not None else out_dtype
+        kind = _real(dtype, "out")
+    out, o_ptr, o_stride = _out_rows(out, x, dtype, T, N, "out")
+    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int4_experts_workspace_bytes(T, k, E, K, cg.rows, N))
+    _ok(lib.xnor_int4_experts(x_ptr, x_kind, x_stride, T, _dev(experts, torch.int32, (T, k), "experts"), _dev(weights, torch.float32, (T, k), "weights"), k,
+                              E, ctypes.byref(cg), ctypes.byref(cu), ctypes.byref(cd), act, o_ptr, kind, o_stride, ws, ws_bytes, _stream()),
+        "xnor_int4_experts")
+    return out

@@ -1,0 +1,262 @@
+// Host side of routing and of the products with 4-bit weights in the C ABI: argument validation, then the launchers.
+#include <algorithm>
+
+#include "dense_check.hpp"
+#include "experts_common.hpp"
+
+namespace {
+
+using namespace xnor;
+
+bool known_group(int g) { return g == 32 || g == 64 || g == 128; }
+int row_bytes(int cols) { return (int)(((long long)cols + 7) / 8 * 4); }
+
+// Status of a matrix of 4-bit weights or of a stack of `count`.
+int check_int4(const xnor_int4 *w, int count)
+{
+    if (!w) return XNOR_E_NULL;
+    if (!value_size(w->scale_type) || !known_group(w->group)) return XNOR_E_UNSUPPORTED;
+    if (w->rows <= 0 || w->rows > kMaxCols || w->cols <= 0 || w->cols > kMaxCols) return XNOR_E_SHAPE;
+    if (!w->q || !w->scale) return XNOR_E_NULL;
+    if (w->q_stride < row_bytes(w->cols) || !stride_fits((long long)w->rows * count, w->q_stride)) return XNOR_E_SHAPE;
+    if (!aligned(w->q, 4) || w->q_stride % 4 || !aligned(w->scale, value_size(w->scale_type))) return XNOR_E_ALIGN;
+    return XNOR_OK;
+}
+
+// The gated block's two matrices.
+int check_pair(const xnor_int4 *wg, const xnor_int4 *wu, int count)
+{
+    int rc = check_int4(wg, count);
+    if (rc || (rc = check_int4(wu, count))) return rc;
+    if (wg->rows != wu->rows || wg->cols != wu->cols || wg->group != wu->group || wg->q_stride != wu->q_stride) return XNOR_E_SHAPE;
+    return wg->scale_type != wu->scale_type || !wg->zero != !wu->zero ? XNOR_E_UNSUPPORTED : XNOR_OK;
+}
+
+Int4Args args_of(const void *x, long long ldx, const xnor_int4 *w, const xnor_int4 *w2, long long M, void *out, int out_type, long long ldo)
+{
+    Int4Args a{};
+    a.x = x, a.ldx = ldx, a.w = {w->q, w->scale, w->zero}, a.ldq = w->q_stride, a.scale_type = w->scale_type, a.group = w->group;
+    if (w2) a.w2 = {w2->q, w2->scale, w2->zero};
+    a.M = M, a.N = w->rows, a.K = w->cols, a.out = out, a.out_type = out_type, a.ldo = ldo;
+    return a;
+}
+
+// Sizes of a call of xnor_int4_experts, and its workspace's parts, each at a multiple of 256 bytes.
+int check_experts(long long T, int k, int E)
+{
+    if (T < 0 || T > kMaxRows || k <= 0 || k > kMaxChosen || E <= 0 || E > kMaxExperts || T * k > kMaxRows) return XNOR_E_SHAPE;
+    return XNOR_OK;
+}
+struct ExpertParts {
+    size_t offsets, order, lists, hidden, pairs, bytes;
+};
+ExpertParts expert_parts(long long T, int k, int E, int F, int N)
+{
+    const long long pairs = T * k;
+    ExpertParts to{};
+    size_t at = 0;
+    auto part = [&](size_t bytes) {
+        const size_t from = at;
+        at += (bytes + 255) / 256 * 256;
+        return from;
+    };
+    to.offsets = part((size_t)(E + 1) * 4);
+    to.order = part((size_t)pairs * 4);
+    to.lists = part(route_lists_workspace(pairs, E));
+    to.hidden = part((size_t)pairs * F * 2);
+    to.pairs = part((size_t)pairs * N * 4);
+    to.bytes = at;
+    return to;
+}
+
+int check_route(long long T, int E, int k)
+{
+    if (T < 0 || T > kMaxRows || E <= 0 || E > kMaxExperts || k <= 0 || k > kMaxChosen || T * k > kMaxRows) return XNOR_E_SHAPE;
+    return XNOR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int xnor_int4_quantize(const void *w, int w_type, long long rows, int cols, long long w_stride, int group, uint8_t *q, long long q_stride,
+                       void *scale, int scale_type, uint8_t *zero, void *stream)
+{
+    const int ws = value_size(w_type), ss = value_size(scale_type);
+    if (!ws || !ss || !known_group(group)) return XNOR_E_UNSUPPORTED;
+    const Matrix all[] = {{w, rows, cols, w_stride, ws, false}, {q, rows, cols, std::max<long long>(q_stride, cols), 4, false}, vec(scale, rows, ss)};
+    if (const int rc = check(all)) return rc;
+    if (q_stride < row_bytes(cols) || !stride_fits(rows, q_stride)) return XNOR_E_SHAPE;
+    if (q_stride % 4) return XNOR_E_ALIGN;
+    Int4Make a{};
+    a.from = w, a.rows = rows, a.cols = cols, a.stride = w_stride, a.group = group, a.q = q, a.q_stride = q_stride, a.scale = scale, a.zero = zero;
+    a.scale_type = scale_type;
+    return hip_status(launch_int4_quantize(a, w_type, (hipStream_t)stream));
+}
+
+int xnor_int4_pack(const uint8_t *levels, long long rows, int cols, long long levels_stride, uint8_t *q, long long q_stride, void *stream)
+{
+    const Matrix all[] = {{levels, rows, cols, levels_stride, 1, false}, {q, rows, cols, std::max<long long>(q_stride, cols), 4, false}};
+    if (const int rc = check(all)) return rc;
+    if (q_stride < row_bytes(cols) || !stride_fits(rows, q_stride)) return XNOR_E_SHAPE;
+    if (q_stride % 4) return XNOR_E_ALIGN;
+    Int4Make a{};
+    a.from = levels, a.rows = rows, a.cols = cols, a.stride = levels_stride, a.q = q, a.q_stride = q_stride;
+    return hip_status(launch_int4_pack(a, (hipStream_t)stream));
+}
+
+int xnor_int4_dequantize(const xnor_int4 *w, void *out, int out_type, long long out_stride, void *stream)
+{
+    if (const int rc = check_int4(w, 1)) return rc;
+    const int os = value_size(out_type);
+    if (!os) return XNOR_E_UNSUPPORTED;
+    const Matrix all[] = {{out, w->rows, w->cols, out_stride, os, true}};
+    if (const int rc = check(all)) return rc;
+    Int4Make a{};
+    a.rows = w->rows, a.cols = w->cols, a.group = w->group, a.q = const_cast<uint8_t *>(w->q), a.q_stride = w->q_stride;
+    a.scale = const_cast<void *>(w->scale), a.zero = const_cast<uint8_t *>(w->zero), a.scale_type = w->scale_type;
+    a.out = out, a.out_type = out_type, a.stride = out_stride;
+    return hip_status(launch_int4_dequantize(a, (hipStream_t)stream));
+}
+
+int xnor_int4_linear_workspace_bytes(long long M, int N, int K, size_t *bytes)
+{
+    if (!bytes) return XNOR_E_NULL;
+    if (M < 0 || M > kMaxRows || N <= 0 || N > kMaxCols || K <= 0 || K > kMaxCols) return XNOR_E_SHAPE;
+    *bytes = 0;
+    return XNOR_OK;
+}
+
+int xnor_int4_linear(const void *x, int type, long long x_stride, const xnor_int4 *w, const float *bias, long long M, void *out, int out_type,
+                     long long out_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int os = value_size(out_type);
+    if (value_size(type) != 2 || !os) return XNOR_E_UNSUPPORTED;
+    if (const int rc = check_int4(w, 1)) return rc;
+    const Matrix all[] = {{x, M, w->cols, x_stride, 2, false}, {out, M, w->rows, out_stride, os, true}};
+    if (const int rc = check(all)) return rc;
+    if (!aligned(bias, 4) || !aligned(workspace, 16)) return XNOR_E_ALIGN;
+    Int4Args a = args_of(x, 2 * x_stride, w, nullptr, M, out, out_type, out_stride);
+    a.bias = bias;
+    return hip_status(launch_int4_few(a, type, false, (hipStream_t)stream));
+}
+
+int xnor_int4_gated_workspace_bytes(long long M, int F, int K, size_t *bytes) { return xnor_int4_linear_workspace_bytes(M, F, K, bytes); }
+
+int xnor_int4_gated(const void *x, int type, long long x_stride, const xnor_int4 *wg, const xnor_int4 *wu, int act, long long M, void *h, int h_type,
+                    long long h_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int hs = value_size(h_type);
+    if (value_size(type) != 2 || !hs || !known_act(act)) return XNOR_E_UNSUPPORTED;
+    if (const int rc = check_pair(wg, wu, 1)) return rc;
+    const Matrix all[] = {{x, M, wg->cols, x_stride, 2, false}, {h, M, wg->rows, h_stride, hs, true}};
+    if (const int rc = check(all)) return rc;
+    if (!aligned(workspace, 16)) return XNOR_E_ALIGN;
+    Int4Args a = args_of(x, 2 * x_stride, wg, wu, M, h, h_type, h_stride);
+    a.act = act;
+    return hip_status(launch_int4_few(a, type, true, (hipStream_t)stream));
+}
+
+int xnor_route_fwd(const void *logits, int type, long long T, int E, long long logits_stride, const float *bias, int score, int groups,
+                   int groups_kept, int group_top, int k, int renorm, float factor, int32_t *experts, float *weights, void *stream)
+{
+    const int size = value_size(type);
+    if (!size || (score != XNOR_SCORE_SOFTMAX && score != XNOR_SCORE_SIGMOID)) return XNOR_E_UNSUPPORTED;
+    if (const int rc = check_route(T, E, k)) return rc;
+    if (groups < 1 || groups > E || E % groups || groups_kept < 1 || groups_kept > groups || group_top < 1 || group_top > 2) return XNOR_E_SHAPE;
+    if (k > E / groups * groups_kept) return XNOR_E_SHAPE;
+    const Matrix all[] = {{logits, T, E, logits_stride, size, false}, {experts, T, k, k, 4, true}, {weights, T, k, k, 4, true}};
+    if (const int rc = check(all)) return rc;
+    if (!aligned(bias, 4)) return XNOR_E_ALIGN;
+    RouteArgs a{};
+    a.logits = logits, a.T = T, a.stride = logits_stride, a.E = E, a.bias = bias, a.score = score, a.groups = groups, a.kept = groups_kept;
+    a.top = group_top, a.k = k, a.renorm = renorm != 0, a.factor = factor, a.experts = experts, a.weights = weights;
+    return hip_status(launch_route(a, type, (hipStream_t)stream));
+}
+
+int xnor_route_lists_workspace_bytes(long long T, int k, int E, size_t *bytes)
+{
+    if (!bytes) return XNOR_E_NULL;
+    if (const int rc = check_route(T, E, k)) return rc;
+    *bytes = route_lists_workspace(T * k, E);
+    return XNOR_OK;
+}
+
+int xnor_route_lists(const int32_t *experts, long long T, int k, int E, int32_t *offsets, int32_t *order, void *workspace, size_t workspace_bytes,
+                     void *stream)
+{
+    if (const int rc = check_route(T, E, k)) return rc;
+    const size_t need = route_lists_workspace(T * k, E);
+    const Matrix all[] = {{experts, T, k, k, 4, false}, vec(offsets, E + 1, 4), {order, T, k, k, 4, true}, vec(workspace, need ? 1 : 0, 16)};
+    if (const int rc = check(all)) return rc;
+    if (workspace_bytes < need) return XNOR_E_WORKSPACE;
+    ListArgs a{};
+    a.experts = experts, a.pairs = T * k, a.E = E, a.offsets = offsets, a.order = order, a.counts = (int32_t *)workspace;
+    return hip_status(launch_route_lists(a, (hipStream_t)stream));
+}
+
+int xnor_route_bwd(const float *dweights, const void *logits, int type, long long T, int E, long long logits_stride, const int32_t *experts, int k,
+                   int score, int renorm, float factor, void *dlogits, long long dlogits_stride, void *stream)
+{
+    const int size = value_size(type);
+    if (!size || (score != XNOR_SCORE_SOFTMAX && score != XNOR_SCORE_SIGMOID)) return XNOR_E_UNSUPPORTED;
+    if (const int rc = check_route(T, E, k)) return rc;
+    const Matrix all[] = {{dweights, T, k, k, 4, false}, {logits, T, E, logits_stride, size, false}, {experts, T, k, k, 4, false},
+                          {dlogits, T, E, dlogits_stride, size, true}};
+    if (const int rc = check(all)) return rc;
+    RouteArgs a{};
+    a.logits = logits, a.T = T, a.stride = logits_stride, a.E = E, a.score = score, a.k = k, a.renorm = renorm != 0, a.factor = factor;
+    a.experts = const_cast<int32_t *>(experts), a.dweights = dweights, a.dlogits = dlogits, a.dstride = dlogits_stride;
+    return T > 0 ? hip_status(launch_route_bwd(a, type, (hipStream_t)stream)) : XNOR_OK;
+}
+
+int xnor_int4_experts_workspace_bytes(long long T, int k, int E, int K, int F, int N, size_t *bytes)
+{
+    if (!bytes) return XNOR_E_NULL;
+    if (const int rc = check_experts(T, k, E)) return rc;
+    if (K <= 0 || K > kMaxCols || F <= 0 || F > kMaxCols || N <= 0 || N > kMaxCols) return XNOR_E_SHAPE;
+    *bytes = T > 0 ? expert_parts(T, k, E, F, N).bytes : 0;
+    return XNOR_OK;
+}
+
+int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, const int32_t *experts, const float *weights, int k, int E,
+                      const xnor_int4 *wg, const xnor_int4 *wu, const xnor_int4 *wd, int act, void *out, int out_type, long long out_stride,
+                      void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int os = value_size(out_type);
+    if (value_size(type) != 2 || !os || !known_act(act)) return XNOR_E_UNSUPPORTED;
+    if (const int rc = check_experts(T, k, E)) return rc;
+    int rc = check_pair(wg, wu, E);
+    if (rc || (rc = check_int4(wd, E))) return rc;
+    const int K = wg->cols, F = wg->rows, N = wd->rows;
+    if (wd->cols != F) return XNOR_E_SHAPE;
+    const Matrix all[] = {{x, T, K, x_stride, 2, false}, {experts, T, k, k, 4, false}, {weights, T, k, k, 4, false}, {out, T, N, out_stride, os, true},
+                          vec(workspace, T > 0 ? 1 : 0, 16)};
+    if ((rc = check(all))) return rc;
+    if (T == 0) return XNOR_OK;
+    const ExpertParts at = expert_parts(T, k, E, F, N);
+    if (workspace_bytes < at.bytes) return XNOR_E_WORKSPACE;
+    char *const held = (char *)workspace;
+    const hipStream_t st = (hipStream_t)stream;
+
+    ListArgs l{};
+    l.experts = experts, l.pairs = T * k, l.E = E, l.offsets = (int32_t *)(held + at.offsets), l.order = (int32_t *)(held + at.order);
+    l.counts = (int32_t *)(held + at.lists);
+    hipError_t e = launch_route_lists(l, st);
+    if (e != hipSuccess) return hip_status(e);
+    // hidden: rows by sorted position; pairs: rows by token and slot
+    Int4Args a = args_of(x, 2 * x_stride, wg, wu, T * k, held + at.hidden, type, F);
+    a.act = act, a.offsets = l.offsets, a.order_x = l.order, a.E = E, a.chosen = k;
+    e = launch_int4_few(a, type, true, st);
+    if (e != hipSuccess) return hip_status(e);
+    Int4Args b = args_of(held + at.hidden, 2LL * F, wd, nullptr, T * k, held + at.pairs, XNOR_TYPE_FP32, N);
+    b.offsets = l.offsets, b.order_out = l.order, b.E = E, b.chosen = k;
+    e = launch_int4_few(b, type, false, st);
+    if (e != hipSuccess) return hip_status(e);
+    CombineArgs c{};
+    c.pairs = (const float *)(held + at.pairs), c.experts = experts, c.weights = weights, c.T = T, c.ldo = out_stride, c.k = k, c.E = E, c.N = N;
+    c.out = out, c.out_type = out_type;
+    return hip_status(launch_combine(c, st));
+}
+
+}  // extern "C"

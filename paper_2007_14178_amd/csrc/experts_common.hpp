@@ -1,0 +1,100 @@
+// What routing to experts and the products with 4-bit weights share.
+#pragma once
+
+#include "dense_common.hpp"
+
+namespace xnor {
+
+constexpr int kMaxExperts = 1024, kMaxChosen = 32;
+
+struct RouteArgs {
+    const void *logits;
+    long long T, stride;
+    int E;
+    const float *bias;
+    int score, groups, kept, top, k, renorm;
+    float factor;
+    int32_t *experts;
+    float *weights;
+    const float *dweights;          // backward
+    void *dlogits;
+    long long dstride;
+};
+hipError_t launch_route(const RouteArgs &p, int type, hipStream_t st);
+hipError_t launch_route_bwd(const RouteArgs &p, int type, hipStream_t st);
+
+struct ListArgs {
+    const int32_t *experts;
+    long long pairs;
+    int E;
+    int32_t *offsets, *order, *counts;      // counts: workspace
+};
+size_t route_lists_workspace(long long pairs, int E);
+hipError_t launch_route_lists(const ListArgs &p, hipStream_t st);
+
+// A matrix of 4-bit weights, or a stack of them, as the kernels see it.
+struct Int4View {
+    const uint8_t *q;
+    const void *scale;
+    const uint8_t *zero;
+};
+struct Int4Args {
+    const void *x;              // [M][K], or the experts' tokens: sorted position i's row is order[i] / chosen, or i (order_x NULL)
+    long long ldx;              // bytes
+    Int4View w, w2;             // w2: the gated block's second matrix
+    long long ldq;              // bytes
+    int scale_type, group;
+    long long M;
+    int N, K, act;
+    const float *bias;
+    void *out;                  // row m; experts: row i, or order_out[i]
+    long long ldo;              // values
+    int out_type;
+    const int32_t *offsets;     // experts' sorted positions, NULL: one matrix for all of x's rows
+    const int32_t *order_x, *order_out;
+    int E, chosen;
+    long long first;            // (set by the launchers: the launch's first tile of tokens)
+};
+// GATED: w and w2 with the activation.
+hipError_t launch_int4_few(const Int4Args &p, int type, bool gated, hipStream_t st);
+
+struct Int4Make {
+    const void *from;           // weights, levels, or (dequantize) nothing
+    long long rows, stride;
+    int cols, group;
+    uint8_t *q;
+    long long q_stride;
+    void *scale;
+    uint8_t *zero;
+    int scale_type;
+    void *out;
+    int out_type;
+};
+hipError_t launch_int4_quantize(const Int4Make &p, int w_type, hipStream_t st);
+hipError_t launch_int4_pack(const Int4Make &p, hipStream_t st);
+hipError_t launch_int4_dequantize(const Int4Make &p, hipStream_t st);
+
+// out[t] = sum over slots of weights[t][s] * pairs[t k + s], of slots without an expert weights * 0.
+struct CombineArgs {
+    const float *pairs;
+    const int32_t *experts;
+    const float *weights;
+    long long T, ldo;
+    int k, E, N;
+    void *out;
+    int out_type;
+};
+hipError_t launch_combine(const CombineArgs &p, hipStream_t st);
+
+__device__ inline float load_real(const void *p, long long at, int type)
+{
+    return type == XNOR_TYPE_FP32 ? ((const float *)p)[at] : type == XNOR_TYPE_F16 ? (float)((const f16_t *)p)[at] : (float)((const bf16_t *)p)[at];
+}
+__device__ inline void store_real(void *p, long long at, int type, float v)
+{
+    if (type == XNOR_TYPE_FP32) ((float *)p)[at] = v;
+    else if (type == XNOR_TYPE_F16) ((f16_t *)p)[at] = (f16_t)v;
+    else ((bf16_t *)p)[at] = (bf16_t)v;
+}
+
+}  // namespace xnor

@@ -1,0 +1,144 @@
+// Levels of 4 bits on their way to the matrix instructions, and how the products with them finish.
+#pragma once
+
+#include "dense_tile.hpp"
+#include "experts_common.hpp"
+
+namespace xnor {
+
+// Eight values of a word as the operand's four registers: register j holds the values 2 j and 2 j + 1, as f16 or bf16.
+template <class T> struct Levels;
+
+// f16 has ten bits behind the point: a level in the lowest four of 1024's is 1024 + level, in the next four of 64's 64 + level, and a packed
+// addition leaves level - zero, exactly: 9 instructions for eight values.
+template <> struct Levels<f16_t> {
+    static constexpr bool kOffset = false;
+    struct Zero {
+        uint32_t far, near;             // -(1024 + zero), -(64 + zero), twice
+    };
+    static __device__ Zero zero(uint32_t z)
+    {
+        const uint32_t zz = z | z << 16;
+        return {0xe400e400u | zz, 0xd400d400u | zz << 4};
+    }
+    static __device__ i32x4 offset(const Zero &) { return i32x4{}; }        // (not called)
+    static __device__ uint32_t add(uint32_t a, uint32_t b)
+    {
+        typedef f16_t f16x2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, a) + __builtin_bit_cast(f16x2, b));
+    }
+    template <bool EXACT>
+    static __device__ i32x4 operand(uint32_t w, const Zero &z)
+    {
+        const uint32_t v = w >> 8;
+        return i32x4{(int)add((w & 0x000f000fu) | 0x64006400u, z.far), (int)add((w & 0x00f000f0u) | 0x54005400u, z.near),
+                     (int)add((v & 0x000f000fu) | 0x64006400u, z.far), (int)add((v & 0x00f000f0u) | 0x54005400u, z.near)};
+    }
+};
+
+// bf16 has seven, and no packed addition: a level in the upper four of 16's is 16 + level, at 8 instructions for eight values, and a second matrix
+// instruction adds -(16 + zero) times the same tokens in fp32.  That costs up to 5 bits of the 24 in sums of a group and makes NaN of a token's
+// infinity (and infinities of sums near the largest value): sums that are not finite are formed again (EXACT), from levels less zeros times
+// 2^-16, which their group's scale gets back.
+template <> struct Levels<bf16_t> {
+    static constexpr bool kOffset = true;
+    struct Zero {
+        uint32_t minus;                 // -(16 + zero), twice
+        float z;
+    };
+    static __device__ Zero zero(uint32_t z) { return {0xc180c180u | (z | z << 16) << 3, (float)z}; }
+    static __device__ i32x4 offset(const Zero &z) { return i32x4{(int)z.minus, (int)z.minus, (int)z.minus, (int)z.minus}; }
+    template <bool EXACT>
+    static __device__ i32x4 operand(uint32_t w, const Zero &z)
+    {
+        if constexpr (EXACT) {
+            i32x4 to;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float low = ((float)(w >> 4 * j & 15u) - z.z) * 0x1p-16f, high = ((float)(w >> (16 + 4 * j) & 15u) - z.z) * 0x1p-16f;
+                to[j] = (int)(__float_as_uint(low) >> 16 | (__float_as_uint(high) & 0xffff0000u));      // (small integers: no bits are lost)
+            }
+            return to;
+        }
+        return i32x4{(int)((w << 3 & 0x00780078u) | 0x41804180u), (int)((w >> 1 & 0x00780078u) | 0x41804180u),
+                     (int)((w >> 5 & 0x00780078u) | 0x41804180u), (int)((w >> 9 & 0x00780078u) | 0x41804180u)};
+    }
+};
+
+// Scales of rows n .. n + 3 in group g, 0 behind the last row.
+__device__ inline void load_scales(const Int4View &w, int type, long long g, int n, int N, float (&to)[4])
+{
+    const long long at = g * N;
+    if (type == XNOR_TYPE_FP32) load_params((const float *)w.scale + at, n, N, 0.f, to);
+    else if (type == XNOR_TYPE_F16) load_params((const f16_t *)w.scale + at, n, N, 0.f, to);
+    else load_params((const bf16_t *)w.scale + at, n, N, 0.f, to);
+}
+
+// The gated block's outputs from its sums.  16-bit ones by the short forms of the activations.
+__device__ inline float gate(int act, bool half, float g)
+{
+    if (half)
+        return act == XNOR_ACT_SILU ? act_value<XNOR_ACT_SILU, true>(g) : act == XNOR_ACT_GELU ? act_value<XNOR_ACT_GELU, true>(g) : act_value<XNOR_ACT_RELU, true>(g);
+    return act == XNOR_ACT_SILU ? act_value<XNOR_ACT_SILU, false>(g) : act == XNOR_ACT_GELU ? act_value<XNOR_ACT_GELU, false>(g) : act_value<XNOR_ACT_RELU, false>(g);
+}
+
+// Outputs n .. n + 3 of row m, as far as the row goes, rounded once.
+__device__ inline void store_outputs(const Int4Args &p, long long m, int n, const float (&v)[4])
+{
+    const long long at = m * p.ldo;
+    if (p.out_type == XNOR_TYPE_FP32) {
+        store_values((float *)p.out + at, n, p.N, v);
+    } else if (p.out_type == XNOR_TYPE_F16) {
+        const f16_t to[4] = {(f16_t)v[0], (f16_t)v[1], (f16_t)v[2], (f16_t)v[3]};
+        store_values((f16_t *)p.out + at, n, p.N, to);
+    } else {
+        const bf16_t to[4] = {(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
+        store_values((bf16_t *)p.out + at, n, p.N, to);
+    }
+}
+
+// Experts: the expert and its positions of the slot-th tile of `tile` tokens, tiles counted over the experts in turn.  False: there are fewer.
+// All lanes of a wave ask together.
+struct ExpertTile {
+    int expert, first, count;       // count: of the expert's positions from `first` on, at most a tile
+};
+__device__ inline bool expert_tile(const int32_t *offsets, int E, int tile, long long slot, ExpertTile *to)
+{
+    const int lane = threadIdx.x & 63, each = (E + 63) >> 6, from = lane * each;
+    int mine = 0;
+    for (int i = 0; i < each; ++i) {
+        const int e = from + i;
+        if (e < E) mine += (offsets[e + 1] - offsets[e] + tile - 1) / tile;
+    }
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int v = __shfl_up(upto, d);
+        if (lane >= d) upto += v;
+    }
+    const unsigned long long found = __ballot(upto > slot);
+    if (!found) return false;
+    const int owner = __builtin_ctzll(found);
+    int left = (int)(slot - __shfl(upto - mine, owner));
+    for (int e = owner * each; e < E; ++e) {
+        const int first = offsets[e], count = offsets[e + 1] - first, tiles = (count + tile - 1) / tile;
+        if (left < tiles) {
+            to->expert = __builtin_amdgcn_readfirstlane(e);
+            to->first = __builtin_amdgcn_readfirstlane(first + left * tile);
+            to->count = __builtin_amdgcn_readfirstlane(min(tile, count - left * tile));
+            return true;
+        }
+        left -= tiles;
+    }
+    return false;
+}
+
+// Matrix e of a stack.
+__device__ inline Int4View of_stack(const Int4View &w, const Int4Args &p, int e)
+{
+    const long long groups = (p.K + p.group - 1) / p.group, values = e * groups * p.N;
+    const int size = p.scale_type == XNOR_TYPE_FP32 ? 4 : 2;
+    return {w.q + (long long)e * p.N * p.ldq, (const char *)w.scale + values * size, w.zero ? w.zero + values : nullptr};
+}
+
+}  // namespace xnor
