@@ -138,7 +138,7 @@ int xnor_int4_linear(const void *x, int type, long long x_stride, const xnor_int
     if (!aligned(bias, 4) || !aligned(workspace, 16)) return XNOR_E_ALIGN;
     Int4Args a = args_of(x, 2 * x_stride, w, nullptr, M, out, out_type, out_stride);
     a.bias = bias;
-    return hip_status(launch_int4_few(a, type, false, (hipStream_t)stream));
+    return hip_status(launch_int4(a, type, false, (hipStream_t)stream));
 }
 
 int xnor_int4_gated_workspace_bytes(long long M, int F, int K, size_t *bytes) { return xnor_int4_linear_workspace_bytes(M, F, K, bytes); }
@@ -154,7 +154,7 @@ int xnor_int4_gated(const void *x, int type, long long x_stride, const xnor_int4
     if (!aligned(workspace, 16)) return XNOR_E_ALIGN;
     Int4Args a = args_of(x, 2 * x_stride, wg, wu, M, h, h_type, h_stride);
     a.act = act;
-    return hip_status(launch_int4_few(a, type, true, (hipStream_t)stream));
+    return hip_status(launch_int4(a, type, true, (hipStream_t)stream));
 }
 
 int xnor_route_fwd(const void *logits, int type, long long T, int E, long long logits_stride, const float *bias, int score, int groups,
@@ -247,11 +247,11 @@ int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, 
     // hidden: rows by sorted position; pairs: rows by token and slot
     Int4Args a = args_of(x, 2 * x_stride, wg, wu, T * k, held + at.hidden, type, F);
     a.act = act, a.offsets = l.offsets, a.order_x = l.order, a.E = E, a.chosen = k;
-    e = launch_int4_few(a, type, true, st);
+    e = launch_int4(a, type, true, st);
     if (e != hipSuccess) return hip_status(e);
     Int4Args b = args_of(held + at.hidden, 2LL * F, wd, nullptr, T * k, held + at.pairs, XNOR_TYPE_FP32, N);
     b.offsets = l.offsets, b.order_out = l.order, b.E = E, b.chosen = k;
-    e = launch_int4_few(b, type, false, st);
+    e = launch_int4(b, type, false, st);
     if (e != hipSuccess) return hip_status(e);
     CombineArgs c{};
     c.pairs = (const float *)(held + at.pairs), c.experts = experts, c.weights = weights, c.T = T, c.ldo = out_stride, c.k = k, c.E = E, c.N = N;

@@ -57,6 +57,9 @@ struct Int4Args {
 };
 // GATED: w and w2 with the activation.
 hipError_t launch_int4_few(const Int4Args &p, int type, bool gated, hipStream_t st);
+hipError_t launch_int4_tiles(const Int4Args &p, int type, bool gated, hipStream_t st);
+// By the number of tokens (experts: of an expert, were all liked alike).
+hipError_t launch_int4(const Int4Args &p, int type, bool gated, hipStream_t st);
 
 struct Int4Make {
     const void *from;           // weights, levels, or (dequantize) nothing

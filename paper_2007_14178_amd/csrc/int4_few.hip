@@ -214,4 +214,10 @@ hipError_t launch_int4_few(const Int4Args &p, int type, bool gated, hipStream_t 
     return gated ? few_by_tokens<bf16_t, true>(p, st) : few_by_tokens<bf16_t, false>(p, st);
 }
 
+hipError_t launch_int4(const Int4Args &p, int type, bool gated, hipStream_t st)
+{
+    const long long each = p.offsets ? p.M / p.E : p.M;
+    return each > 64 ? launch_int4_tiles(p, type, gated, st) : launch_int4_few(p, type, gated, st);
+}
+
 }  // namespace xnor
