@@ -239,6 +239,16 @@ int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, 
     char *const held = (char *)workspace;
     const hipStream_t st = (hipStream_t)stream;
 
+    if (int4_pairs_pay(T * k, E)) {
+        // hidden: rows by pair
+        Int4Args a = args_of(x, 2 * x_stride, wg, wu, T * k, held + at.hidden, type, F);
+        a.act = act, a.pairs = experts, a.E = E, a.chosen = k;
+        const hipError_t e = launch_int4(a, type, true, st);
+        if (e != hipSuccess) return hip_status(e);
+        Int4Args b = args_of(held + at.hidden, 2LL * F, wd, nullptr, T, out, out_type, out_stride);
+        b.pairs = experts, b.E = E, b.chosen = k;
+        return hip_status(launch_int4_down(b, weights, type, st));
+    }
     ListArgs l{};
     l.experts = experts, l.pairs = T * k, l.E = E, l.offsets = (int32_t *)(held + at.offsets), l.order = (int32_t *)(held + at.order);
     l.counts = (int32_t *)(held + at.lists);

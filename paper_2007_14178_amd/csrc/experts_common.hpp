@@ -52,9 +52,14 @@ struct Int4Args {
     int out_type;
     const int32_t *offsets;     // experts' sorted positions, NULL: one matrix for all of x's rows
     const int32_t *order_x, *order_out;
+    const int32_t *pairs;       // experts' pairs, each by itself (offsets NULL): row m is that of expert pairs[m], x's row m / chosen
     int E, chosen;
     long long first;            // (set by the launchers: the launch's first tile of tokens)
 };
+// Whether so few pairs are better taken each by itself, without lists.
+inline bool int4_pairs_pay(long long pairs, int E) { return pairs <= 64 && pairs <= E; }
+// A token's chosen experts' second products and their sum in one launch: x holds the rows of the pairs, weights their shares, M the tokens.
+hipError_t launch_int4_down(const Int4Args &p, const float *weights, int type, hipStream_t st);
 // GATED: w and w2 with the activation.
 hipError_t launch_int4_few(const Int4Args &p, int type, bool gated, hipStream_t st);
 hipError_t launch_int4_tiles(const Int4Args &p, int type, bool gated, hipStream_t st);

@@ -6,6 +6,19 @@
 
 namespace xnor {
 
+// (a & mask) | set as one instruction: of its operands only one can be a scalar, so that the compiler, which keeps both constants in scalars, makes two.
+template <uint32_t MASK, uint32_t SET>
+__device__ inline uint32_t and_or(uint32_t a)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    uint32_t to;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(to) : "v"(a), "s"(MASK), "v"(SET));
+    return to;
+#else
+    return (a & MASK) | SET;
+#endif
+}
+
 // Eight values of a word as the operand's four registers: register j holds the values 2 j and 2 j + 1, as f16 or bf16.
 template <class T> struct Levels;
 
@@ -31,8 +44,8 @@ template <> struct Levels<f16_t> {
     static __device__ i32x4 operand(uint32_t w, const Zero &z)
     {
         const uint32_t v = w >> 8;
-        return i32x4{(int)add((w & 0x000f000fu) | 0x64006400u, z.far), (int)add((w & 0x00f000f0u) | 0x54005400u, z.near),
-                     (int)add((v & 0x000f000fu) | 0x64006400u, z.far), (int)add((v & 0x00f000f0u) | 0x54005400u, z.near)};
+        return i32x4{(int)add(and_or<0x000f000fu, 0x64006400u>(w), z.far), (int)add(and_or<0x00f000f0u, 0x54005400u>(w), z.near),
+                     (int)add(and_or<0x000f000fu, 0x64006400u>(v), z.far), (int)add(and_or<0x00f000f0u, 0x54005400u>(v), z.near)};
     }
 };
 
@@ -60,8 +73,8 @@ template <> struct Levels<bf16_t> {
             }
             return to;
         }
-        return i32x4{(int)((w << 3 & 0x00780078u) | 0x41804180u), (int)((w >> 1 & 0x00780078u) | 0x41804180u),
-                     (int)((w >> 5 & 0x00780078u) | 0x41804180u), (int)((w >> 9 & 0x00780078u) | 0x41804180u)};
+        return i32x4{(int)and_or<0x00780078u, 0x41804180u>(w << 3), (int)and_or<0x00780078u, 0x41804180u>(w >> 1),
+                     (int)and_or<0x00780078u, 0x41804180u>(w >> 5), (int)and_or<0x00780078u, 0x41804180u>(w >> 9)};
     }
 };
 
@@ -106,10 +119,8 @@ __device__ inline bool expert_tile(const int32_t *offsets, int E, int tile, long
 {
     const int lane = threadIdx.x & 63, each = (E + 63) >> 6, from = lane * each;
     int mine = 0;
-    for (int i = 0; i < each; ++i) {
-        const int e = from + i;
-        if (e < E) mine += (offsets[e + 1] - offsets[e] + tile - 1) / tile;
-    }
+    for (int i = 0; i < each; ++i)
+        if (from + i < E) mine += (offsets[from + i + 1] - offsets[from + i] + tile - 1) / tile;
     int upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -119,18 +130,17 @@ __device__ inline bool expert_tile(const int32_t *offsets, int E, int tile, long
     const unsigned long long found = __ballot(upto > slot);
     if (!found) return false;
     const int owner = __builtin_ctzll(found);
-    int left = (int)(slot - __shfl(upto - mine, owner));
-    for (int e = owner * each; e < E; ++e) {
-        const int first = offsets[e], count = offsets[e + 1] - first, tiles = (count + tile - 1) / tile;
-        if (left < tiles) {
-            to->expert = __builtin_amdgcn_readfirstlane(e);
-            to->first = __builtin_amdgcn_readfirstlane(first + left * tile);
-            to->count = __builtin_amdgcn_readfirstlane(min(tile, count - left * tile));
-            return true;
-        }
-        left -= tiles;
+    // (all lanes look among their own; the owner's finding counts)
+    long long left = slot - (upto - mine);
+    int e = min(from, E - 1), first = offsets[e], count = offsets[e + 1] - first;
+    for (int i = 1; i < each && from + i < E && left >= (count + tile - 1) / tile; ++i) {
+        left -= (count + tile - 1) / tile;
+        e = from + i, first = offsets[e], count = offsets[e + 1] - first;
     }
-    return false;
+    to->expert = __builtin_amdgcn_readlane(e, owner);
+    to->first = __builtin_amdgcn_readlane(first + (int)left * tile, owner);
+    to->count = __builtin_amdgcn_readlane(min(tile, count - (int)left * tile), owner);
+    return true;
 }
 
 // Matrix e of a stack.

@@ -3,7 +3,8 @@
 // A workgroup has 16 rows of the weights (of each matrix in the gated block), its eight waves an eighth of the contraction each, whose sums are added
 // in LDS.  A step is 128 values, 64 bytes of a row: lane (r, g) loads 16 bytes, row r's values 32 g .. 32 g + 31, and two exchanges across the wave
 // turn the four words of the four lanes of a row about, so that instruction i takes the values 32 i .. 32 i + 31, which have one scale.
-// A group's sum is multiplied by its scale in fp32: the weights are never rounded.
+// A group's sum is multiplied by its scale in fp32: the weights are never rounded.  Some steps' loads are on their way together, behind no branch; their
+// scales and zero points come with one load each, and reach the lanes that need them through LDS.
 #include <algorithm>
 
 #include "int4_common.hpp"
@@ -12,6 +13,7 @@ namespace xnor {
 namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * kWave, kValues = 128;
+constexpr int kMostGroups = 16;         // whose scales a wave holds at a time
 
 // d[i] of the 16 lanes g to d[g] of the 16 lanes i.
 __device__ inline void turn_about(uint32_t (&d)[4])
@@ -30,106 +32,157 @@ __device__ inline void turn_about(uint32_t (&d)[4])
 #endif
 }
 
-// TT: tiles of 16 tokens.  GROUPS: of a step.
-template <class T, bool GATED, int TT, int GROUPS>
-__global__ __launch_bounds__(kThreads) void int4_few_kernel(const Int4Args p)
+// A wave's scales and zero points of some groups: fp32 [kMostGroups][16], a byte each.
+struct Held {
+    float scale[kMostGroups * 16];
+    uint32_t zero[kMostGroups * 4];
+};
+
+// What a wave multiplies.
+template <class T, int MATS, int TT>
+struct Span {
+    Int4View view[MATS];
+    const uint32_t *w[MATS];        // the lane's row
+    const T *x[TT];                 // the lane's token (or another's, where there is none)
+    int n0, N, K, groups, scale_type;
+    Held *held;                     // [MATS]
+};
+
+// U steps from s on.  WHOLE: all of their values are there.
+template <class T, int MATS, int TT, int GROUPS, int U, bool WHOLE, bool EXACT>
+__device__ inline void some_steps(const Span<T, MATS, TT> &p, int s, f32x4 (&acc)[MATS][TT])
 {
-    // U: steps whose weights are on their way together
-    constexpr int MATS = GATED ? 2 : 1, U = GATED || TT == 4 || GROUPS == 4 ? 2 : 4;
     typedef Mat<T> Mul;
     typedef Levels<T> Level;
-    __shared__ f32x4 sums[kWaves][MATS][TT][kWave];
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16;
-
-    Int4View view[MATS];
-    view[0] = p.w;
-    if constexpr (GATED) view[1] = p.w2;
-    long long m0 = (p.first + blockIdx.y) * (16 * TT);
-    int count = (int)min(p.M - m0, 16LL * TT);
-    if (p.offsets) {
-        ExpertTile tile;
-        if (!expert_tile(p.offsets, p.E, 16 * TT, p.first + blockIdx.y, &tile)) return;
-        m0 = tile.first, count = tile.count;
+    static_assert(U * GROUPS <= kMostGroups, "");
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    // scales and zero points of group lane / 4's rows 4 (lane & 3) .. + 3
+    const int rows = p.n0 + (lane & 3) * 4;
+    const long long group = min(s * GROUPS + min(lane >> 2, U * GROUPS - 1), p.groups - 1), at = group * p.N;
+    float scale[MATS][4];
+    uint32_t zero[MATS];
+    uint32_t held[MATS][U][4];
+    i32x4 vx[U][4][TT];
+    uint32_t raw[MATS][4];
+    if (p.N >= 16) {
 #pragma unroll
-        for (int k = 0; k < MATS; ++k) view[k] = of_stack(view[k], p, tile.expert);
+        for (int k = 0; k < MATS; ++k) {
+            if (p.scale_type == XNOR_TYPE_FP32) __builtin_memcpy(raw[k], (const float *)p.view[k].scale + at + rows, 16);
+            else __builtin_memcpy(raw[k], (const f16_t *)p.view[k].scale + at + rows, 8);
+            zero[k] = 0x08080808u;
+            if (p.view[k].zero) __builtin_memcpy(&zero[k], p.view[k].zero + at + rows, 4);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < MATS; ++k) {
+            load_scales(p.view[k], p.scale_type, group, rows, p.N, scale[k]);
+            zero[k] = p.view[k].zero ? 0u : 0x08080808u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (p.view[k].zero && rows + i < p.N) zero[k] |= (uint32_t)p.view[k].zero[at + rows + i] << 8 * i;
+        }
     }
-
-    const int steps = (p.K + kValues - 1) / kValues, share = (steps + kWaves - 1) / kWaves, words = (p.K + 7) / 8;
-    const int from = wave * share, to = min(steps, from + share);
-    const int groups = (p.K + p.group - 1) / p.group;
-    const int row = min(n0 + r, p.N - 1);
-    const uint32_t *w[MATS];
 #pragma unroll
-    for (int k = 0; k < MATS; ++k) w[k] = (const uint32_t *)(view[k].q + row * p.ldq);
-    const T *x[TT];
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int j = 0; j < TT; ++j) {
-        const long long m = m0 + min(j * 16 + r, count - 1);
-        x[j] = (const T *)((const char *)p.x + (p.order_x ? p.order_x[m] / p.chosen : m) * p.ldx);
-    }
-
-    auto accumulate = [&](f32x4 (&acc)[MATS][TT], auto exact) __attribute__((always_inline)) {
-        constexpr bool EXACT = decltype(exact)::value;
+        for (int k = 0; k < MATS; ++k) {
+            if constexpr (WHOLE) {
+                __builtin_memcpy(held[k][u], p.w[k] + (s + u) * (kValues / 8) + g * 4, 16);
+            } else {
+                // (words behind the last one: any levels, as the tokens' values are zeros there)
 #pragma unroll
-        for (int k = 0; k < MATS; ++k)
+                for (int i = 0; i < 4; ++i) held[k][u][i] = p.w[k][min((s + u) * (kValues / 8) + g * 4 + i, (p.K - 1) / 8)];
+            }
+        }
+    auto load_x = [&](int u) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < TT; ++j) acc[k][j] = f32x4{};
-        for (int s = from; s < to; s += U) {
-            uint32_t held[MATS][U][4];
-            float scale[MATS][U][GROUPS][4];
-            uint32_t zero[MATS][U][GROUPS];
+        for (int j = 0; j < TT; ++j) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int i = 0; i < 4; ++i) {
+                const int from = (s + u) * kValues + i * 32 + g * 8;
+                if constexpr (WHOLE) {
+                    __builtin_memcpy(&vx[u][i][j], p.x[j] + from, 16);
+                } else {
+                    T v[8];
 #pragma unroll
-                for (int k = 0; k < MATS; ++k) {
-                    if (s + u >= to) continue;
-                    const Chunk<uint32_t> c = load_chunk(w[k], (s + u) * (kValues / 8) + g * 4, words);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) held[k][u][i] = c.v[i];
-#pragma unroll
-                    for (int i = 0; i < GROUPS; ++i) {
-                        const long long at = min((s + u) * GROUPS + i, groups - 1);
-                        load_scales(view[k], p.scale_type, at, n0 + g * 4, p.N, scale[k][u][i]);
-                        zero[k][u][i] = view[k].zero ? view[k].zero[at * p.N + row] & 15u : 8u;
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] = p.x[j][min(from + e, p.K - 1)];
+                        v[e] = from + e < p.K ? v[e] : T(0);
                     }
-                }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (s + u >= to) continue;
-                i32x4 vx[4][TT];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < TT; ++j) vx[i][j] = __builtin_bit_cast(i32x4, load_chunk(x[j], (s + u) * kValues + i * 32 + g * 8, p.K));
-#pragma unroll
-                for (int k = 0; k < MATS; ++k) {
-                    turn_about(held[k][u]);
-#pragma unroll
-                    for (int i = 0; i < GROUPS; ++i) {
-                        const typename Level::Zero z = Level::zero(zero[k][u][i]);
-                        f32x4 part[TT] = {};
-#pragma unroll
-                        for (int q = i * (4 / GROUPS); q < (i + 1) * (4 / GROUPS); ++q) {
-                            const i32x4 levels = Level::template operand<EXACT>(held[k][u][q], z);
-#pragma unroll
-                            for (int j = 0; j < TT; ++j) {
-                                part[j] = Mul::mul(levels, vx[q][j], part[j]);
-                                if constexpr (Level::kOffset && !EXACT) part[j] = Mul::mul(Level::offset(z), vx[q][j], part[j]);
-                            }
-                        }
-#pragma unroll
-                        for (int j = 0; j < TT; ++j)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[k][j][e] += (EXACT && Level::kOffset ? scale[k][u][i][e] * 0x1p16f : scale[k][u][i][e]) * part[j][e];
-                    }
+                    vx[u][i][j] = __builtin_bit_cast(i32x4, v);
                 }
             }
         }
     };
-    f32x4 acc[MATS][TT];
-    accumulate(acc, std::false_type{});
-    if constexpr (Level::kOffset) {
+    if constexpr (TT < 4)
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_x(u);
+#pragma unroll
+    for (int k = 0; k < MATS; ++k) {
+        if (p.N >= 16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t half = raw[k][i / 2] >> 16 * (i & 1) & 0xffffu;
+                scale[k][i] = p.scale_type == XNOR_TYPE_FP32 ? __uint_as_float(raw[k][i])
+                              : p.scale_type == XNOR_TYPE_F16 ? (float)__builtin_bit_cast(f16_t, (uint16_t)half) : __uint_as_float(half << 16);
+            }
+        }
+        if ((lane >> 2) < U * GROUPS) {
+            *(f32x4 *)&p.held[k].scale[lane * 4] = f32x4{scale[k][0], scale[k][1], scale[k][2], scale[k][3]};
+            p.held[k].zero[lane] = zero[k];
+        }
+    }
+    // (a wave's own: its LDS instructions come in order)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if constexpr (TT == 4) load_x(u);
+#pragma unroll
+        for (int k = 0; k < MATS; ++k) {
+            turn_about(held[k][u]);
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i) {
+                const int of = u * GROUPS + i;
+                const typename Level::Zero z = Level::zero(((const uint8_t *)p.held[k].zero)[of * 16 + r] & 15u);
+                const f32x4 by = *(const f32x4 *)&p.held[k].scale[of * 16 + g * 4];
+                f32x4 part[TT] = {};
+#pragma unroll
+                for (int q = i * (4 / GROUPS); q < (i + 1) * (4 / GROUPS); ++q) {
+                    const i32x4 levels = Level::template operand<EXACT>(held[k][u][q], z);
+#pragma unroll
+                    for (int j = 0; j < TT; ++j) {
+                        part[j] = Mul::mul(levels, vx[u][q][j], part[j]);
+                        if constexpr (Level::kOffset && !EXACT) part[j] = Mul::mul(Level::offset(z), vx[u][q][j], part[j]);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < TT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[k][j][e] += (EXACT && Level::kOffset ? by[e] * 0x1p16f : by[e]) * part[j][e];
+            }
+            __builtin_amdgcn_sched_barrier(0);          // (all groups' operands at a time would not fit the registers)
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Steps from .. to - 1.
+// U: steps whose loads are on their way together.
+template <class T, int MATS, int TT, int GROUPS, int U>
+__device__ inline void accumulate(const Span<T, MATS, TT> &p, int from, int to, f32x4 (&acc)[MATS][TT])
+{
+#pragma unroll
+    for (int k = 0; k < MATS; ++k)
+#pragma unroll
+        for (int j = 0; j < TT; ++j) acc[k][j] = f32x4{};
+    const int whole = min(to, p.K / kValues);
+    int s = from;
+    for (; s + U <= whole; s += U) some_steps<T, MATS, TT, GROUPS, U, true, false>(p, s, acc);
+    for (; s < whole; ++s) some_steps<T, MATS, TT, GROUPS, 1, true, false>(p, s, acc);
+    for (; s < to; ++s) some_steps<T, MATS, TT, GROUPS, 1, false, false>(p, s, acc);
+    if constexpr (Levels<T>::kOffset) {
         auto is_odd = [](float v) { return !(fabsf(v) <= 3.402823466e38f); };
         bool odd = false;
 #pragma unroll
@@ -139,8 +192,8 @@ __global__ __launch_bounds__(kThreads) void int4_few_kernel(const Int4Args p)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) odd |= is_odd(acc[k][j][e]);
         if (__any(odd)) {
-            f32x4 exact[MATS][TT];
-            accumulate(exact, std::true_type{});
+            f32x4 exact[MATS][TT] = {};
+            for (s = from; s < to; ++s) some_steps<T, MATS, TT, GROUPS, 1, false, true>(p, s, exact);
 #pragma unroll
             for (int k = 0; k < MATS; ++k)
 #pragma unroll
@@ -150,6 +203,53 @@ __global__ __launch_bounds__(kThreads) void int4_few_kernel(const Int4Args p)
                         if (is_odd(acc[k][j][e])) acc[k][j][e] = exact[k][j][e];
         }
     }
+}
+
+// The first of a workgroup's 16 rows: the last workgroup's are the matrix's last ones, some of them another's too, which come out alike.
+__device__ inline int first_row(int block, int N) { return max(0, min(block * 16, N - 16)); }
+
+// TT: tiles of 16 tokens.  GROUPS: of a step.
+template <class T, bool GATED, int TT, int GROUPS>
+__global__ __launch_bounds__(kThreads, TT == 1 ? 4 : 2) void int4_few_kernel(const Int4Args p)
+{
+    constexpr int MATS = GATED ? 2 : 1;
+    __shared__ f32x4 sums[kWaves][MATS][TT][kWave];
+    __shared__ Held held[kWaves][MATS];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = lane & 15, g = lane >> 4;
+    const int n0 = first_row(blockIdx.x, p.N);
+
+    Span<T, MATS, TT> span;
+    span.view[0] = p.w;
+    if constexpr (GATED) span.view[1] = p.w2;
+    long long m0 = (p.first + blockIdx.y) * (16 * TT);
+    int count = (int)min(p.M - m0, 16LL * TT);
+    int expert = -1;
+    if (p.pairs) {
+        m0 = p.first + blockIdx.y, count = 1;
+        expert = p.pairs[m0];
+        if (expert < 0 || expert >= p.E) return;
+    } else if (p.offsets) {
+        ExpertTile tile;
+        if (!expert_tile(p.offsets, p.E, 16 * TT, p.first + blockIdx.y, &tile)) return;
+        m0 = tile.first, count = tile.count, expert = tile.expert;
+    }
+    const int row = min(n0 + r, p.N - 1);
+#pragma unroll
+    for (int k = 0; k < MATS; ++k) {
+        if (expert >= 0) span.view[k] = of_stack(span.view[k], p, expert);
+        span.w[k] = (const uint32_t *)(span.view[k].q + row * p.ldq);
+    }
+#pragma unroll
+    for (int j = 0; j < TT; ++j) {
+        const long long m = m0 + min(j * 16 + r, count - 1);
+        const long long from = p.pairs ? m / p.chosen : p.order_x ? p.order_x[m] / p.chosen : m;
+        span.x[j] = (const T *)((const char *)p.x + from * p.ldx);
+    }
+    span.n0 = n0, span.N = p.N, span.K = p.K, span.groups = (p.K + p.group - 1) / p.group, span.scale_type = p.scale_type, span.held = held[wave];
+
+    const int steps = (p.K + kValues - 1) / kValues, share = (steps + kWaves - 1) / kWaves;
+    f32x4 acc[MATS][TT];
+    accumulate<T, MATS, TT, GROUPS, (GATED || TT > 1 ? 2 : 4)>(span, wave * share, min(steps, wave * share + share), acc);
 #pragma unroll
     for (int k = 0; k < MATS; ++k)
 #pragma unroll
@@ -183,7 +283,7 @@ hipError_t few(const Int4Args &p, hipStream_t st)
 {
     constexpr long long kMost = 32768;          // tiles of tokens in a launch
     const int TM = 16 * TT;
-    const long long tiles = p.offsets ? std::min<long long>(p.E, p.M) + p.M / TM : (p.M + TM - 1) / TM;
+    const long long tiles = p.pairs ? p.M : p.offsets ? std::min<long long>(p.E, p.M) + p.M / TM : (p.M + TM - 1) / TM;
     const long long each = std::max<long long>(1, std::min<long long>(kMost, kMaxBlocks / ceil_div(p.N, 16)));
     for (long long m = 0; m < tiles; m += each) {
         Int4Args q = p;
@@ -201,8 +301,77 @@ hipError_t few(const Int4Args &p, hipStream_t st)
 template <class T, bool GATED>
 hipError_t few_by_tokens(const Int4Args &p, hipStream_t st)
 {
-    const long long each = p.offsets ? (p.M + p.E - 1) / p.E : p.M;
+    const long long each = p.pairs ? 1 : p.offsets ? (p.M + p.E - 1) / p.E : p.M;
     return each <= 16 ? few<T, GATED, 1>(p, st) : each <= 32 ? few<T, GATED, 2>(p, st) : few<T, GATED, 4>(p, st);
+}
+
+// ---- a token's experts' second products and their sum -------------------------------------------------------------------
+// A workgroup has 16 rows of every chosen expert's matrix for one token; a wave has a share of the contraction of one of them, or of several in turn.
+// Sums are multiplied by their slot's weight before they are added, slots in order within a wave, then the waves'.
+
+constexpr int kDownWaves = 16;
+
+template <class T, int GROUPS>
+__global__ __launch_bounds__(kDownWaves * kWave) void int4_down_kernel(const Int4Args p, const float *weights, int shares)
+{
+    __shared__ f32x4 sums[kDownWaves][4];
+    __shared__ Held held[kDownWaves];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = lane & 15, g = lane >> 4;
+    const int n0 = first_row(blockIdx.x, p.N), row = min(n0 + r, p.N - 1);
+    const long long token = p.first + blockIdx.y;
+    const int steps = (p.K + kValues - 1) / kValues, share = (steps + shares - 1) / shares;
+    f32x4 sum = {};
+    float none = 0.f;           // of slots without an expert: weight * 0
+    for (int item = wave; item < p.chosen * shares; item += kDownWaves) {
+        const int slot = item / shares, part = item % shares;
+        const long long m = token * p.chosen + slot;
+        const int expert = __builtin_amdgcn_readfirstlane(p.pairs[m]);
+        const float weight = weights[m];
+        if (expert < 0 || expert >= p.E) {
+            none += weight * 0.f;
+            continue;
+        }
+        Span<T, 1, 1> span;
+        span.view[0] = of_stack(p.w, p, expert);
+        span.w[0] = (const uint32_t *)(span.view[0].q + row * p.ldq);
+        span.x[0] = (const T *)((const char *)p.x + m * p.ldx);
+        span.n0 = n0, span.N = p.N, span.K = p.K, span.groups = (p.K + p.group - 1) / p.group, span.scale_type = p.scale_type, span.held = &held[wave];
+        f32x4 acc[1][1];
+        accumulate<T, 1, 1, GROUPS, 2>(span, min(part * share, steps), min(steps, part * share + share), acc);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += weight * acc[0][0][e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += none;
+    if (r == 0) sums[wave][g] = sum;
+    __syncthreads();
+    const int n = n0 + t * 4;
+    if (t >= 4 || n >= p.N) return;
+    float out[4] = {};
+#pragma unroll
+    for (int w = 0; w < kDownWaves; ++w)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] += sums[w][t][e];
+    store_outputs(p, token, n, out);
+}
+
+template <class T>
+hipError_t down(const Int4Args &p, const float *weights, hipStream_t st)
+{
+    const int shares = std::max(1, kDownWaves / p.chosen);
+    constexpr long long kMost = 32768;
+    const long long each = std::max<long long>(1, std::min<long long>(kMost, kMaxBlocks / 2 / ceil_div(p.N, 16)));
+    for (long long m = 0; m < p.M; m += each) {
+        Int4Args q = p;
+        q.first = m;
+        const dim3 grid((unsigned)ceil_div(p.N, 16), (unsigned)std::min(each, p.M - m)), block(kDownWaves * kWave);
+        if (p.group == 128) int4_down_kernel<T, 1><<<grid, block, 0, st>>>(q, weights, shares);
+        else if (p.group == 64) int4_down_kernel<T, 2><<<grid, block, 0, st>>>(q, weights, shares);
+        else int4_down_kernel<T, 4><<<grid, block, 0, st>>>(q, weights, shares);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
@@ -214,10 +383,15 @@ hipError_t launch_int4_few(const Int4Args &p, int type, bool gated, hipStream_t 
     return gated ? few_by_tokens<bf16_t, true>(p, st) : few_by_tokens<bf16_t, false>(p, st);
 }
 
+hipError_t launch_int4_down(const Int4Args &p, const float *weights, int type, hipStream_t st)
+{
+    return type == XNOR_TYPE_F16 ? down<f16_t>(p, weights, st) : down<bf16_t>(p, weights, st);
+}
+
 hipError_t launch_int4(const Int4Args &p, int type, bool gated, hipStream_t st)
 {
     const long long each = p.offsets ? p.M / p.E : p.M;
-    return each > 64 ? launch_int4_tiles(p, type, gated, st) : launch_int4_few(p, type, gated, st);
+    return each > 64 && !p.pairs ? launch_int4_tiles(p, type, gated, st) : launch_int4_few(p, type, gated, st);
 }
 
 }  // namespace xnor
