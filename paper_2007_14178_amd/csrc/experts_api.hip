@@ -48,7 +48,8 @@ int check_experts(long long T, int k, int E)
     return XNOR_OK;
 }
 struct ExpertParts {
-    size_t offsets, order, lists, hidden, pairs, bytes;
+    size_t offsets, order, lists, tiles, hidden, pairs, bytes;
+    int tile;
 };
 ExpertParts expert_parts(long long T, int k, int E, int F, int N)
 {
@@ -63,6 +64,8 @@ ExpertParts expert_parts(long long T, int k, int E, int F, int N)
     to.offsets = part((size_t)(E + 1) * 4);
     to.order = part((size_t)pairs * 4);
     to.lists = part(route_lists_workspace(pairs, E));
+    to.tile = int4_expert_tile(pairs, E);
+    to.tiles = part((size_t)(1 + most_tiles(pairs, E, std::min(to.tile, kInt4Few))) * sizeof(ExpertTile));
     to.hidden = part((size_t)pairs * F * 2);
     to.pairs = part((size_t)pairs * N * 4);
     to.bytes = at;
@@ -234,7 +237,7 @@ int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, 
                           vec(workspace, T > 0 ? 1 : 0, 16)};
     if ((rc = check(all))) return rc;
     if (T == 0) return XNOR_OK;
-    const ExpertParts at = expert_parts(T, k, E, F, N);
+    ExpertParts at = expert_parts(T, k, E, F, N);
     if (workspace_bytes < at.bytes) return XNOR_E_WORKSPACE;
     char *const held = (char *)workspace;
     const hipStream_t st = (hipStream_t)stream;
@@ -251,17 +254,17 @@ int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, 
     }
     ListArgs l{};
     l.experts = experts, l.pairs = T * k, l.E = E, l.offsets = (int32_t *)(held + at.offsets), l.order = (int32_t *)(held + at.order);
-    l.counts = (int32_t *)(held + at.lists);
-    hipError_t e = launch_route_lists(l, st);
-    if (e != hipSuccess) return hip_status(e);
+    l.counts = (int32_t *)(held + at.lists), l.tiles = (ExpertTile *)(held + at.tiles);
     // hidden: rows by sorted position; pairs: rows by token and slot
     Int4Args a = args_of(x, 2 * x_stride, wg, wu, T * k, held + at.hidden, type, F);
-    a.act = act, a.offsets = l.offsets, a.order_x = l.order, a.E = E, a.chosen = k;
-    e = launch_int4(a, type, true, st);
-    if (e != hipSuccess) return hip_status(e);
+    a.act = act, a.tiles = l.tiles, a.order_x = l.order, a.E = E, a.chosen = k;
     Int4Args b = args_of(held + at.hidden, 2LL * F, wd, nullptr, T * k, held + at.pairs, XNOR_TYPE_FP32, N);
-    b.offsets = l.offsets, b.order_out = l.order, b.E = E, b.chosen = k;
-    e = launch_int4(b, type, false, st);
+    b.tiles = l.tiles, b.order_out = l.order, b.E = E, b.chosen = k;
+    if (!int4_tiles_support(a) || !int4_tiles_support(b)) at.tile = std::min(at.tile, kInt4Few);
+    l.tile = a.tile = b.tile = at.tile;
+    hipError_t e = launch_route_lists(l, st);
+    if (e == hipSuccess) e = launch_int4(a, type, true, st);
+    if (e == hipSuccess) e = launch_int4(b, type, false, st);
     if (e != hipSuccess) return hip_status(e);
     CombineArgs c{};
     c.pairs = (const float *)(held + at.pairs), c.experts = experts, c.weights = weights, c.T = T, c.ldo = out_stride, c.k = k, c.E = E, c.N = N;

@@ -1,6 +1,8 @@
 // What routing to experts and the products with 4-bit weights share.
 #pragma once
 
+#include <algorithm>
+
 #include "dense_common.hpp"
 
 namespace xnor {
@@ -28,7 +30,14 @@ struct ListArgs {
     long long pairs;
     int E;
     int32_t *offsets, *order, *counts;      // counts: workspace
+    int tile;                               // > 0: the lists cut into tiles of so many pairs,
+    struct ExpertTile *tiles;               // one after the other; tiles[0].count is their number
 };
+// A tile of an expert's sorted positions.
+struct ExpertTile {
+    int expert, first, count, unused;
+};
+inline long long most_tiles(long long pairs, int E, int tile) { return std::min<long long>(E, pairs) + pairs / tile; }
 size_t route_lists_workspace(long long pairs, int E);
 hipError_t launch_route_lists(const ListArgs &p, hipStream_t st);
 
@@ -50,21 +59,26 @@ struct Int4Args {
     void *out;                  // row m; experts: row i, or order_out[i]
     long long ldo;              // values
     int out_type;
-    const int32_t *offsets;     // experts' sorted positions, NULL: one matrix for all of x's rows
+    const ExpertTile *tiles;    // of experts' sorted positions, NULL: one matrix for all of x's rows
+    int tile;                   // their tokens
     const int32_t *order_x, *order_out;
-    const int32_t *pairs;       // experts' pairs, each by itself (offsets NULL): row m is that of expert pairs[m], x's row m / chosen
+    const int32_t *pairs;       // experts' pairs, each by itself (tiles NULL): row m is that of expert pairs[m], x's row m / chosen
     int E, chosen;
     long long first;            // (set by the launchers: the launch's first tile of tokens)
 };
+// Tiles of more tokens than this go to the kernel for many.
+constexpr int kInt4Few = 64;
 // Whether so few pairs are better taken each by itself, without lists.
 inline bool int4_pairs_pay(long long pairs, int E) { return pairs <= 64 && pairs <= E; }
 // A token's chosen experts' second products and their sum in one launch: x holds the rows of the pairs, weights their shares, M the tokens.
 hipError_t launch_int4_down(const Int4Args &p, const float *weights, int type, hipStream_t st);
 // GATED: w and w2 with the activation.
 hipError_t launch_int4_few(const Int4Args &p, int type, bool gated, hipStream_t st);
+bool int4_tiles_support(const Int4Args &p);
 hipError_t launch_int4_tiles(const Int4Args &p, int type, bool gated, hipStream_t st);
-// By the number of tokens (experts: of an expert, were all liked alike).
+// By the number of tokens (experts: by the tiles that they were cut into).
 hipError_t launch_int4(const Int4Args &p, int type, bool gated, hipStream_t st);
+int int4_expert_tile(long long pairs, int E);
 
 struct Int4Make {
     const void *from;           // weights, levels, or (dequantize) nothing

@@ -110,39 +110,6 @@ __device__ inline void store_outputs(const Int4Args &p, long long m, int n, cons
     }
 }
 
-// Experts: the expert and its positions of the slot-th tile of `tile` tokens, tiles counted over the experts in turn.  False: there are fewer.
-// All lanes of a wave ask together.
-struct ExpertTile {
-    int expert, first, count;       // count: of the expert's positions from `first` on, at most a tile
-};
-__device__ inline bool expert_tile(const int32_t *offsets, int E, int tile, long long slot, ExpertTile *to)
-{
-    const int lane = threadIdx.x & 63, each = (E + 63) >> 6, from = lane * each;
-    int mine = 0;
-    for (int i = 0; i < each; ++i)
-        if (from + i < E) mine += (offsets[from + i + 1] - offsets[from + i] + tile - 1) / tile;
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int v = __shfl_up(upto, d);
-        if (lane >= d) upto += v;
-    }
-    const unsigned long long found = __ballot(upto > slot);
-    if (!found) return false;
-    const int owner = __builtin_ctzll(found);
-    // (all lanes look among their own; the owner's finding counts)
-    long long left = slot - (upto - mine);
-    int e = min(from, E - 1), first = offsets[e], count = offsets[e + 1] - first;
-    for (int i = 1; i < each && from + i < E && left >= (count + tile - 1) / tile; ++i) {
-        left -= (count + tile - 1) / tile;
-        e = from + i, first = offsets[e], count = offsets[e + 1] - first;
-    }
-    to->expert = __builtin_amdgcn_readlane(e, owner);
-    to->first = __builtin_amdgcn_readlane(first + (int)left * tile, owner);
-    to->count = __builtin_amdgcn_readlane(min(tile, count - (int)left * tile), owner);
-    return true;
-}
-
 // Matrix e of a stack.
 __device__ inline Int4View of_stack(const Int4View &w, const Int4Args &p, int e)
 {

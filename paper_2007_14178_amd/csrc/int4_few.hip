@@ -228,9 +228,9 @@ __global__ __launch_bounds__(kThreads, TT == 1 ? 4 : 2) void int4_few_kernel(con
         m0 = p.first + blockIdx.y, count = 1;
         expert = p.pairs[m0];
         if (expert < 0 || expert >= p.E) return;
-    } else if (p.offsets) {
-        ExpertTile tile;
-        if (!expert_tile(p.offsets, p.E, 16 * TT, p.first + blockIdx.y, &tile)) return;
+    } else if (p.tiles) {
+        if (p.first + blockIdx.y >= p.tiles[0].count) return;
+        const ExpertTile tile = p.tiles[1 + p.first + blockIdx.y];
         m0 = tile.first, count = tile.count, expert = tile.expert;
     }
     const int row = min(n0 + r, p.N - 1);
@@ -283,7 +283,7 @@ hipError_t few(const Int4Args &p, hipStream_t st)
 {
     constexpr long long kMost = 32768;          // tiles of tokens in a launch
     const int TM = 16 * TT;
-    const long long tiles = p.pairs ? p.M : p.offsets ? std::min<long long>(p.E, p.M) + p.M / TM : (p.M + TM - 1) / TM;
+    const long long tiles = p.pairs ? p.M : p.tiles ? most_tiles(p.M, p.E, TM) : (p.M + TM - 1) / TM;
     const long long each = std::max<long long>(1, std::min<long long>(kMost, kMaxBlocks / ceil_div(p.N, 16)));
     for (long long m = 0; m < tiles; m += each) {
         Int4Args q = p;
@@ -301,7 +301,7 @@ hipError_t few(const Int4Args &p, hipStream_t st)
 template <class T, bool GATED>
 hipError_t few_by_tokens(const Int4Args &p, hipStream_t st)
 {
-    const long long each = p.pairs ? 1 : p.offsets ? (p.M + p.E - 1) / p.E : p.M;
+    const long long each = p.pairs ? 1 : p.tiles ? p.tile : p.M;
     return each <= 16 ? few<T, GATED, 1>(p, st) : each <= 32 ? few<T, GATED, 2>(p, st) : few<T, GATED, 4>(p, st);
 }
 
@@ -390,8 +390,8 @@ hipError_t launch_int4_down(const Int4Args &p, const float *weights, int type, h
 
 hipError_t launch_int4(const Int4Args &p, int type, bool gated, hipStream_t st)
 {
-    const long long each = p.offsets ? p.M / p.E : p.M;
-    return each > 64 && !p.pairs ? launch_int4_tiles(p, type, gated, st) : launch_int4_few(p, type, gated, st);
+    const bool many = p.tiles ? p.tile > kInt4Few : !p.pairs && p.M > kInt4Few && int4_tiles_support(p);
+    return many ? launch_int4_tiles(p, type, gated, st) : launch_int4_few(p, type, gated, st);
 }
 
 }  // namespace xnor

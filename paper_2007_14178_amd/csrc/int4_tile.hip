@@ -10,7 +10,7 @@
 namespace xnor {
 namespace {
 
-constexpr int kThreads = 256, kRows = 128, kDeep = 64;       // values of a step
+constexpr int kRows = 128, kDeep = 64;       // rows of the weights a tile, values of a step
 
 // The values of a word: level * scale - zero * scale.
 template <class T>
@@ -25,15 +25,35 @@ __device__ inline i32x4 values_of(uint32_t w, float scale, float minus)
     return __builtin_bit_cast(i32x4, to);
 }
 
-template <class T, bool GATED>
-__global__ __launch_bounds__(kThreads, 2) void int4_tile_kernel(const Int4Args p, int tiles_n, long long tiles)
+// Loads from a buffer: a lane's offset and a scalar one.  (The host's pass does not know the builtins.)
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+__device__ inline auto buffer(const void *p, int size) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, size, 0x00027000); }
+#ifdef __HIP_DEVICE_COMPILE__
+template <class R> __device__ inline i32x4 load_16(R r, int at, int from) { return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, from, 0)); }
+template <class R> __device__ inline i32x2 load_8(R r, int at, int from) { return __builtin_bit_cast(i32x2, __builtin_amdgcn_raw_buffer_load_b64(r, at, from, 0)); }
+template <class R> __device__ inline uint32_t load_4(R r, int at, int from) { return __builtin_amdgcn_raw_buffer_load_b32(r, at, from, 0); }
+template <class R> __device__ inline uint16_t load_2(R r, int at, int from) { return __builtin_amdgcn_raw_buffer_load_b16(r, at, from, 0); }
+template <class R> __device__ inline uint8_t load_1(R r, int at, int from) { return __builtin_amdgcn_raw_buffer_load_b8(r, at, from, 0); }
+#else
+template <class R> __device__ inline i32x4 load_16(R, int, int) { return {}; }
+template <class R> __device__ inline i32x2 load_8(R, int, int) { return {}; }
+template <class R> __device__ inline uint32_t load_4(R, int, int) { return 0; }
+template <class R> __device__ inline uint16_t load_2(R, int, int) { return 0; }
+template <class R> __device__ inline uint8_t load_1(R, int, int) { return 0; }
+#endif
+
+// WIDE: scales of 32 bits.
+template <class T, bool GATED, bool WIDE, int TM>
+__global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, int tiles_n, long long tiles)
 {
     constexpr int TN = GATED ? 64 : 128;        // outputs n of a tile
+    constexpr int kThreads = 2 * TM, A = 4, B = 512 / kThreads;         // chunks of the tokens and word pairs of the weights that a thread stages
     typedef Mat<T> Mul;
-    __shared__ __align__(16) char lds[2][2 * kRows * kStep];
+    __shared__ __align__(16) char lds[2][(TM + kRows) * kStep];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     // Workgroups go round the eight XCDs by their index: each takes a run of consecutive tiles, groups of eight tiles of tokens for a tile of the
-    // weights' rows, so that what its units work on at a time shares both in its L2.
+    // weights' rows, so that what its units work on at a time shares both in its L2.  (Experts: of the tiles that there are.)
+    if (p.tiles) tiles = min(tiles, (p.tiles[0].count - p.first) * tiles_n);
     const long long eighth = (tiles + 7) >> 3, index = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= eighth || index >= tiles) return;
     const int rows = (int)(tiles / tiles_n), group8 = (int)(index / (8 * tiles_n)), in = (int)(index - (long long)group8 * 8 * tiles_n);
@@ -41,110 +61,161 @@ __global__ __launch_bounds__(kThreads, 2) void int4_tile_kernel(const Int4Args p
     const int tn = __builtin_amdgcn_readfirstlane(in / high), tm = __builtin_amdgcn_readfirstlane(group8 * 8 + in % high);
     const int n0 = tn * TN;
     Int4View view[2] = {p.w, GATED ? p.w2 : p.w};
-    long long m0 = (p.first + tm) * kRows;
-    int count = (int)min(p.M - m0, (long long)kRows);
-    if (p.offsets) {
-        ExpertTile tile;
-        if (!expert_tile(p.offsets, p.E, kRows, p.first + tm, &tile)) return;
+    long long m0 = (p.first + tm) * TM;
+    int count = (int)min(p.M - m0, (long long)TM);
+    if (p.tiles) {
+        const ExpertTile tile = p.tiles[1 + p.first + tm];
         m0 = tile.first, count = tile.count;
         view[0] = of_stack(view[0], p, tile.expert), view[1] = of_stack(view[1], p, tile.expert);
     }
 
-    // Tokens: chunk `chunk` of rows t / 8 + 32 i.  Weights: word pair `pair` (16 values) of rows t / 4 + 64 i.
+    // Tokens: chunk `chunk` of rows t / 8 + TM / 4 i.  Weights: word pair `pair` (16 values) of rows t / 4 + TM / 2 i.  All through buffers, a lane's offsets staying as
+    // they are and a step's a scalar.
     const int chunk = t & 7, pair = t & 3;
-    const T *a[4];
+    const long long from_x = p.order_x ? 0 : m0 * p.ldx;
+    const auto x = buffer((const char *)p.x + from_x, 0x7fffffff);
+    int a[A];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const long long m = m0 + min((t >> 3) + 32 * i, count - 1);
-        a[i] = (const T *)((const char *)p.x + (p.order_x ? p.order_x[m] / p.chosen : m) * p.ldx);
-    }
-    const uint32_t *b[2];
-    int row[2];
-    const Int4View *of[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = (t >> 2) + 64 * i;
-        row[i] = min(n0 + (GATED ? (r >> 5) * 16 + (r & 15) : r), p.N - 1);
-        of[i] = &view[GATED ? r >> 4 & 1 : 0];
-        b[i] = (const uint32_t *)(of[i]->q + row[i] * p.ldq);
+    for (int i = 0; i < A; ++i) {
+        const int m = min((t >> 3) + TM / 4 * i, count - 1);
+        a[i] = (int)((p.order_x ? p.order_x[m0 + m] / p.chosen : m) * p.ldx) + chunk * 16;
     }
     const int words = (p.K + 7) / 8, groups = (p.K + p.group - 1) / p.group, shift = __builtin_ctz(p.group);
-    const int steps = (p.K + kDeep - 1) / kDeep;
+    const bool has_zero = view[0].zero != nullptr, half = p.scale_type == XNOR_TYPE_F16;
+    constexpr int kScale = WIDE ? 4 : 2;
+    // (a lane's matrix: in the gated block that of its row's 16; a wave's rows t / 4 are 16 of one)
+    const bool second = GATED && (wave & 1);
+    const Int4View &mine = second ? view[1] : view[0];
+    const auto q = buffer(mine.q + (long long)n0 * p.ldq, 0x7fffffff);
+    const auto scales = buffer(mine.scale, 0x7fffffff);
+    const auto zeros = buffer(has_zero ? (const void *)mine.zero : mine.scale, 0x7fffffff);        // (loaded in any case: a branch would part the step)
+    int b[B], of_scale[B], of_zero[B];
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+        const int r = (t >> 2) + TM / 2 * i, row = min(GATED ? (r >> 5) * 16 + (r & 15) : r, p.N - 1 - n0);
+        const int value = n0 + row + (shift == 5 ? (pair >> 1) * p.N : 0);
+        b[i] = row * (int)p.ldq + pair * 8, of_scale[i] = value * kScale, of_zero[i] = has_zero ? value : 0;
+    }
+    // Steps in the order that they are taken: one that the contraction ends inside comes first.
+    const int whole = p.K / kDeep, part = p.K % kDeep ? 1 : 0, steps = whole + part;
 
-    Chunk<T> va[4];
-    uint32_t vb[2][2];
-    float scale[2], minus[2];
-    auto fetch = [&](int s, auto whole) __attribute__((always_inline)) {
-        const int at = s * kDeep + chunk * 8;
+    // Two steps' rows are on their way.
+    struct Rows {
+        i32x4 a[A];
+        i32x2 b[B];
+        uint32_t scale[B], zero[B];        // as they are loaded: a conversion beside the loads would wait for them
+    };
+    Rows held[2];
+    auto fetch = [&](int s, Rows &to, auto ends) __attribute__((always_inline)) {
+        const int deep = (decltype(ends)::value ? whole : min(s - part, whole - 1)) * kDeep;      // (behind the last step: that one again)
+        // weights first: at the tile's begin the tokens' rows are not known yet
+        const int g = deep >> shift, back = decltype(ends)::value && shift == 5 && g + (pair >> 1) >= groups ? p.N : 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (decltype(whole)::value) __builtin_memcpy(&va[i], a[i] + at, 16);
-            else va[i] = load_chunk(a[i], at, p.K);
-        }
+        for (int i = 0; i < B; ++i) {
+            if constexpr (!decltype(ends)::value) {
+                to.b[i] = load_8(q, b[i], deep / 2);
+            } else {        // (levels behind the last one may be any)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int w = s * (kDeep / 8) + pair * 2;
-            const long long g = (long long)min((s * kDeep + pair * 16) >> shift, groups - 1) * p.N + row[i];
-            if constexpr (decltype(whole)::value) {
-                __builtin_memcpy(vb[i], b[i] + w, 8);
-            } else {
-                vb[i][0] = w < words ? b[i][w] : 0;
-                vb[i][1] = w + 1 < words ? b[i][w + 1] : 0;
+                for (int j = 0; j < 2; ++j) to.b[i][j] = load_4(q, b[i] - pair * 8 + min(deep / 8 + pair * 2 + j, words - 1) * 4, 0);
             }
-            scale[i] = load_real(of[i]->scale, g, p.scale_type);
-            minus[i] = of[i]->zero ? (float)(of[i]->zero[g] & 15) : 8.f;
+            if constexpr (WIDE) to.scale[i] = load_4(scales, of_scale[i] - back * kScale, g * p.N * kScale);
+            else to.scale[i] = load_2(scales, of_scale[i] - back * kScale, g * p.N * kScale);
+            to.zero[i] = load_1(zeros, has_zero ? of_zero[i] - back : 0, has_zero ? g * p.N : 0);
+        }
+        if constexpr (!decltype(ends)::value) {
+#pragma unroll
+            for (int i = 0; i < A; ++i) to.a[i] = load_16(x, a[i], deep * 2);
+        } else {            // tokens' values there are zeros
+#pragma unroll
+            for (int i = 0; i < A; ++i) {
+                uint16_t v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = deep + chunk * 8 + e;
+                    v[e] = load_2(x, a[i] - chunk * 16 + min(at, p.K - 1) * 2, 0);
+                    v[e] = at < p.K ? v[e] : 0;
+                }
+                to.a[i] = __builtin_bit_cast(i32x4, v);
+            }
         }
     };
-    auto put = [&](int s) __attribute__((always_inline)) {
-        char *const la = lds[s & 1], *const lb = la + kRows * kStep;
+    auto put = [&](int s, const Rows &from) __attribute__((always_inline)) {
+        char *const la = lds[s & 1], *const lb = la + TM * kStep;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = (t >> 3) + 32 * i;
-            *(i32x4 *)(la + r * kStep + ((chunk ^ (r & 7)) << 4)) = __builtin_bit_cast(i32x4, va[i]);
+        for (int i = 0; i < B; ++i) {
+            const int r = (t >> 2) + TM / 2 * i;
+            const float of_half = (float)__builtin_bit_cast(f16_t, (uint16_t)from.scale[i]);
+            const float by = WIDE ? __uint_as_float(from.scale[i]) : half ? of_half : __uint_as_float(from.scale[i] << 16);
+            const float less = -(has_zero ? (float)(from.zero[i] & 15u) : 8.f) * by;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) *(i32x4 *)(lb + r * kStep + (((pair * 2 + j) ^ (r & 7)) << 4)) = values_of<T>(from.b[i][j], by, less);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = (t >> 2) + 64 * i;
-            const float less = -minus[i] * scale[i];
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                *(i32x4 *)(lb + r * kStep + (((pair * 2 + j) ^ (r & 7)) << 4)) = values_of<T>(vb[i][j], scale[i], less);
+        for (int i = 0; i < A; ++i) {
+            const int r = (t >> 3) + TM / 4 * i;
+            *(i32x4 *)(la + r * kStep + ((chunk ^ (r & 7)) << 4)) = from.a[i];
         }
-    };
-    auto fetch_any = [&](int s) __attribute__((always_inline)) {
-        if ((s + 1) * kDeep <= p.K) fetch(s, std::true_type{});
-        else fetch(s, std::false_type{});
     };
 
-    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
+    const int wm = (TM == 256 ? wave & 3 : wave >> 1) * 64, wn = (TM == 256 ? wave >> 2 : wave & 1) * 64;
+    const bool busy = wm < count;       // whether the wave has tokens
     f32x4 acc[4][4] = {};
-    fetch_any(0);
-    put(0);
-    if (steps > 1) fetch_any(1);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
-    for (int s = 0; s < steps; ++s) {
-        const char *const la = lds[s & 1], *const lb = la + kRows * kStep;
+    auto step = [&](int s, Rows &rows_of, auto more) __attribute__((always_inline)) {
+        if (busy) {
+            const char *const la = lds[s & 1], *const lb = la + TM * kStep;
+            i32x4 fa[2][4], fb[2][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x4 fa[4], fb[4];
-            const int c = h * 4 + (lane >> 4);
+            for (int h = 0; h < 2; ++h) {
+                const int c = h * 4 + (lane >> 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int ra = wm + i * 16 + (lane & 15), rb = wn + i * 16 + (lane & 15);
-                fa[i] = *(const i32x4 *)(la + ra * kStep + ((c ^ (ra & 7)) << 4));
-                fb[i] = *(const i32x4 *)(lb + rb * kStep + ((c ^ (rb & 7)) << 4));
+                for (int i = 0; i < 4; ++i) {
+                    const int ra = wm + i * 16 + (lane & 15), rb = wn + i * 16 + (lane & 15);
+                    fa[h][i] = *(const i32x4 *)(la + ra * kStep + ((c ^ (ra & 7)) << 4));
+                    fb[h][i] = *(const i32x4 *)(lb + rb * kStep + ((c ^ (rb & 7)) << 4));
+                }
             }
+            // (not for some steps alone: the wait for a step's rows would be one for all that are on their way)
+            if constexpr (decltype(more)::value) put(s + 1, rows_of), fetch(s + 3, rows_of, std::false_type{});
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = Mul::mul(fb[i], fa[j], acc[i][j]);
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[i][j] = Mul::mul(fb[h][i], fa[h][j], acc[i][j]);
+            // Between the matrix instructions: the second half's operands from LDS, the next step's conversions and their way into LDS, the fetches.
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                if (i < 8) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if constexpr (decltype(more)::value) {
+                    __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
+                    if (i % 4 == 3) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+                    if (i % 2 == 1 && i >= 8) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+                }
+            }
+        } else if constexpr (decltype(more)::value) {
+            put(s + 1, rows_of), fetch(s + 3, rows_of, std::false_type{});
         }
-        if (s + 1 < steps) {
-            put(s + 1);
-            if (s + 2 < steps) fetch_any(s + 2);
-        }
+        __builtin_amdgcn_sched_barrier(0);
         // (LDS alone is waited for: the fetches are not)
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (part) fetch(0, held[0], std::true_type{});
+    else fetch(0, held[0], std::false_type{});
+    if (whole > 0) {
+        fetch(1, held[1], std::false_type{});
+        put(0, held[0]);
+        fetch(2, held[0], std::false_type{});
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        int s = 0;
+        for (; s + 1 < steps; s += 2) step(s, held[1], std::true_type{}), step(s + 1, held[0], std::true_type{});
+        if (s < steps) step(s, held[1], std::false_type{});
+    } else {
+        put(0, held[0]);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        step(0, held[1], std::false_type{});
     }
 #pragma unroll
     for (int i = 0; i < 4; i += GATED ? 2 : 1) {
@@ -168,30 +239,57 @@ __global__ __launch_bounds__(kThreads, 2) void int4_tile_kernel(const Int4Args p
     }
 }
 
-template <class T, bool GATED>
+template <class T, bool GATED, int TM>
 hipError_t tiles(const Int4Args &p, hipStream_t st)
 {
     const int tiles_n = ceil_div(p.N, GATED ? 64 : 128);
-    const long long all = p.offsets ? std::min<long long>(p.E, p.M) + p.M / kRows : (p.M + kRows - 1) / kRows;
+    const long long all = p.tiles ? most_tiles(p.M, p.E, TM) : (p.M + TM - 1) / TM;
     const long long each = std::max<long long>(1, kMaxBlocks / tiles_n);
     for (long long m = 0; m < all; m += each) {
         Int4Args q = p;
         q.first = m;
         const long long n = std::min(each, all - m) * tiles_n;
-        int4_tile_kernel<T, GATED><<<dim3((unsigned)((n + 7) / 8 * 8)), dim3(kThreads), 0, st>>>(q, tiles_n, n);
+        const dim3 grid((unsigned)((n + 7) / 8 * 8)), block(2 * TM);
+        if (p.scale_type == XNOR_TYPE_FP32) int4_tile_kernel<T, GATED, true, TM><<<grid, block, 0, st>>>(q, tiles_n, n);
+        else int4_tile_kernel<T, GATED, false, TM><<<grid, block, 0, st>>>(q, tiles_n, n);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
+template <class T, bool GATED>
+hipError_t by_tiles(const Int4Args &p, hipStream_t st)
+{
+    // the larger tile where there is one for each unit: half the conversions for a product (4096 x 8192 x 8192 bf16 748 us on the smaller, 618 on the
+    // larger), but one workgroup a unit, with nothing beside its begin and end (32768 pairs of 64 experts, 2048 x 1024, 473 and 340 us on the larger ones,
+    // half of an expert's last tile empty, 461 and 321 on the smaller)
+    const bool large = !p.tiles && (p.M + 255) / 256 * ceil_div(p.N, GATED ? 64 : 128) >= compute_units();
+    return large ? tiles<T, GATED, 256>(p, st) : tiles<T, GATED, 128>(p, st);
+}
+
 }  // namespace
+
+// Whether a tile's operands are within 31 bits of where its buffers begin.
+bool int4_tiles_support(const Int4Args &p)
+{
+    constexpr long long kMost = 0x7fffffff;
+    if (p.M == 0) return true;
+    const long long groups = (p.K + p.group - 1) / p.group, last = p.order_x ? p.M / p.chosen : 256;
+    return last * p.ldx + 2LL * p.K <= kMost && kRows * p.ldq <= kMost && (groups + 1) * p.N * 4 <= kMost;
+}
+
+int int4_expert_tile(long long pairs, int E)
+{
+    const long long each = (pairs + E - 1) / E;
+    return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : 128;
+}
 
 hipError_t launch_int4_tiles(const Int4Args &p, int type, bool gated, hipStream_t st)
 {
     if (p.M == 0) return hipSuccess;
-    if (type == XNOR_TYPE_F16) return gated ? tiles<f16_t, true>(p, st) : tiles<f16_t, false>(p, st);
-    return gated ? tiles<bf16_t, true>(p, st) : tiles<bf16_t, false>(p, st);
+    if (type == XNOR_TYPE_F16) return gated ? by_tiles<f16_t, true>(p, st) : by_tiles<f16_t, false>(p, st);
+    return gated ? by_tiles<bf16_t, true>(p, st) : by_tiles<bf16_t, false>(p, st);
 }
 
 }  // namespace xnor

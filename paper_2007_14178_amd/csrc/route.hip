@@ -337,7 +337,7 @@ __global__ __launch_bounds__(kListThreads) void list_kernel(const ListArgs p, lo
 {
     extern __shared__ unsigned long long bits[];        // [kListWaves][E], then base [E]
     int *const base = (int *)(bits + kListWaves * p.E);
-    __shared__ int wave_sums[kListWaves];
+    __shared__ int wave_sums[kListWaves], wave_tiles[kListWaves];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const long long from = blockIdx.x * run, to = min(p.pairs, from + run);
     // of expert t: all its pairs, and those of the runs before
@@ -376,6 +376,24 @@ __global__ __launch_bounds__(kListThreads) void list_kernel(const ListArgs p, lo
         if (blockIdx.x == 0) p.offsets[t + 1] = upto;
     }
     if (blockIdx.x == 0 && t == 0) p.offsets[0] = 0;
+    if (blockIdx.x == 0 && p.tiles) {
+        const int mine = (all + p.tile - 1) / max(p.tile, 1);
+        int to = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(to, d);
+            if (lane >= d) to += v;
+        }
+        if (lane == 63) wave_tiles[wave] = to;
+        __syncthreads();
+        int number = 0;
+        for (int w = 0; w < kListWaves; ++w) {
+            if (w < wave) to += wave_tiles[w];
+            number += wave_tiles[w];
+        }
+        if (t == 0) p.tiles[0] = {0, 0, number, 0};
+        for (int i = 0; i < mine; ++i) p.tiles[1 + to - mine + i] = {t, upto - all + i * p.tile, min(p.tile, all - i * p.tile), 0};
+    }
     // behind the lists
     for (long long i = from + t; i < to; i += kListThreads)
         if (i >= total) p.order[i] = -1;
