@@ -65,94 +65,163 @@ __device__ inline void best_lanes(double *v, int *at)
 
 constexpr double kNone = -__builtin_huge_val();
 
+// A lane's values of a row of n, the first at `at`: `each` of them, none behind the row's end.  Full rows by 16 bytes at a time.
+template <class X, int EACH>
+__device__ inline void load_logits(const X *row, int at, int each, int n, int lanes, float none, float (&to)[EACH])
+{
+    if (n == EACH * lanes) {
+        constexpr int V = 16 / sizeof(X) < EACH ? 16 / sizeof(X) : EACH;
+        X raw[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; i += V) __builtin_memcpy(raw + i, row + at + i, V * sizeof(X));
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) to[i] = (float)raw[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const float v = (float)row[min(at + i, n - 1)];
+            to[i] = i < each && at + i < n ? v : none;
+        }
+    }
+}
+
+__device__ inline double score_of(const RouteArgs &p, double logit, double top, double total)
+{
+    return p.score == XNOR_SCORE_SOFTMAX ? exp(logit - top) / total : 1. / (1. + exp(-logit));
+}
+
 // LANES lanes to a token, of whose experts each has EACH consecutive ones: up to LANES * EACH experts.
+//
+// Scores in 64 bits, as which of two nearly equal ones is the larger decides whole numbers: a quarter of the time is the exponentials' (16384 x 256 in fp32,
+// 8 of 4 of 8 groups, 4.9 TB/s would take 3.6 us).  The k best are taken one after the other, each by a scan of a lane's own and a tree over the lanes
+// by DPP; lane n keeps the n-th.
 template <class X, int LANES, int EACH>
 __global__ __launch_bounds__(kThreads) void route_kernel(const RouteArgs p, long long first)
 {
-    constexpr int TOKENS = kThreads / LANES;
-    __shared__ double chosen[TOKENS][kMaxChosen];
-    const int l = threadIdx.x % LANES, slot = threadIdx.x / LANES;
-    const long long t = first + (long long)blockIdx.x * TOKENS + slot;
+    constexpr int TOKENS = kThreads / LANES, SLOTS = (kMaxChosen + LANES - 1) / LANES;
+    const int l = threadIdx.x % LANES;
+    const long long t = first + (long long)blockIdx.x * TOKENS + threadIdx.x / LANES;
     const bool there = t < p.T;
     const X *const logits = (const X *)p.logits + (there ? t : p.T - 1) * p.stride;
     const int each = (p.E + LANES - 1) / LANES, e0 = l * each;
 
-    double s[EACH], c[EACH];            // scores, and what the choice goes by
+    double c[EACH];             // what the choice goes by
     bool unfit = false;
-    double top = kNone;
+    double top = kNone, total = 1.;
+    {
+        float v[EACH];
+        load_logits<X, EACH>(logits, e0, each, p.E, LANES, -__builtin_huge_valf(), v);
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const bool mine = i < each && e0 + i < p.E;
-        const float v = mine ? (float)logits[e0 + i] : -__builtin_huge_valf();
-        s[i] = v;
-        unfit |= v != v || (p.score == XNOR_SCORE_SOFTMAX && v == __builtin_huge_valf());
-        top = s[i] > top ? s[i] : top;
+        for (int i = 0; i < EACH; ++i) {
+            unfit |= v[i] != v[i] || (p.score == XNOR_SCORE_SOFTMAX && v[i] == __builtin_huge_valf());
+            c[i] = v[i];
+            top = c[i] > top ? c[i] : top;
+        }
     }
     unfit = any_lane<LANES>(unfit);
-    double total = 1.;
     if (p.score == XNOR_SCORE_SOFTMAX) {
         top = max_lanes<LANES>(top);
         total = 0.;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            s[i] = s[i] == kNone ? kNone : exp(s[i] - top);
-            total += s[i] == kNone ? 0. : s[i];
+            c[i] = c[i] == kNone ? kNone : exp(c[i] - top);
+            total += c[i] == kNone ? 0. : c[i];
         }
         total = sum_lanes<LANES>(total);
-    }
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const bool none = s[i] == kNone;
-        s[i] = none ? 0. : p.score == XNOR_SCORE_SOFTMAX ? s[i] / total : 1. / (1. + exp(-s[i]));
-        c[i] = none ? kNone : p.bias ? s[i] + (double)p.bias[e0 + i] : s[i];
-        if (!(c[i] > kNone)) c[i] = kNone;
+        for (int i = 0; i < EACH; ++i) c[i] = c[i] == kNone ? kNone : c[i] / total;
+    } else {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) c[i] = c[i] == kNone ? kNone : 1. / (1. + exp(-c[i]));
+    }
+    if (p.bias) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            c[i] += (double)p.bias[min(e0 + i, p.E - 1)];
+            if (!(c[i] > kNone)) c[i] = kNone;
+        }
     }
     if (p.kept < p.groups) {
-        // the groups' scores, one after the other, group g's kept by lane g / per
-        const int size = p.E / p.groups, per = (p.groups + LANES - 1) / LANES;
-        double score[EACH];
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) score[i] = kNone;
-        for (int g = 0; g < p.groups; ++g) {
-            double a = kNone, b = kNone;        // the two largest
+        const int size = p.E / p.groups, lanes = size / each;
+        uint32_t stay = 0;                      // of the lane's experts
+        if (size % each == 0 && (lanes & (lanes - 1)) == 0 && lanes <= 16) {
+            // a lane's experts are of one group, a group's lanes neighbours: its two largest, over 1, 2, 4, 8 or 16 lanes
+            double a = kNone, b = kNone;
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
-                const int e = e0 + i;
-                if (i < each && e >= g * size && e < (g + 1) * size) {
-                    b = c[i] > a ? a : c[i] > b ? c[i] : b;
-                    a = c[i] > a ? c[i] : a;
-                }
+                const double v = i < each ? c[i] : kNone;
+                const double low = v > a ? a : v;
+                b = low > b ? low : b;
+                a = v > a ? v : a;
             }
-            over_lanes<LANES>([&](auto ask) {
+            auto both = [&](auto ask) {
                 const double oa = ask(a), ob = ask(b);
                 const double low = oa > a ? a : oa, more = ob > b ? ob : b;
                 a = oa > a ? oa : a;
                 b = low > more ? low : more;
-            });
-            const double sum = p.top == 2 && b > kNone ? a + b : a;
+            };
+            if (lanes > 1) both([](double v) { return dpp_double<0xb1>(v); });
+            if (lanes > 2) both([](double v) { return dpp_double<0x4e>(v); });
+            if (lanes > 4) both([](double v) { return dpp_double<0x141>(v); });
+            if (lanes > 8) both([](double v) { return dpp_double<0x140>(v); });
+            const double score = p.top == 2 && b > kNone ? a + b : a;
+            const int group = l / lanes;
+            bool open = group < p.groups;       // (the last lanes may have no experts)
+            for (int n = 0; n < p.kept; ++n) {
+                double best = open ? score : kNone;
+                int at = open ? group : kMaxExperts;
+                best_lanes<LANES>(&best, &at);
+                if (at == group) open = false, stay = ~0u;
+            }
+        } else {
+            // the groups' scores, one after the other, group g's kept by lane g / per
+            const int per = (p.groups + LANES - 1) / LANES;
+            double score[EACH];
 #pragma unroll
-            for (int i = 0; i < EACH; ++i)
-                if (l * per + i == g && i < per) score[i] = sum;
-        }
-        uint32_t taken = 0, stay = 0;           // of the lane's groups, of its experts
-        for (int n = 0; n < p.kept; ++n) {
-            double best = kNone;
-            int at = kMaxExperts;               // (a group whose score is -inf can be the best that is left)
+            for (int i = 0; i < EACH; ++i) score[i] = kNone;
+            for (int g = 0; g < p.groups; ++g) {
+                double a = kNone, b = kNone;        // the two largest
 #pragma unroll
-            for (int i = 0; i < EACH; ++i)
-                if (i < per && l * per + i < p.groups && !(taken >> i & 1) && (at == kMaxExperts || score[i] > best)) best = score[i], at = l * per + i;
-            best_lanes<LANES>(&best, &at);
-            if (at / per == l) taken |= 1u << (at - l * per);
+                for (int i = 0; i < EACH; ++i) {
+                    const int e = e0 + i;
+                    if (i < each && e >= g * size && e < (g + 1) * size) {
+                        b = c[i] > a ? a : c[i] > b ? c[i] : b;
+                        a = c[i] > a ? c[i] : a;
+                    }
+                }
+                over_lanes<LANES>([&](auto ask) {
+                    const double oa = ask(a), ob = ask(b);
+                    const double low = oa > a ? a : oa, more = ob > b ? ob : b;
+                    a = oa > a ? oa : a;
+                    b = low > more ? low : more;
+                });
+                const double sum = p.top == 2 && b > kNone ? a + b : a;
 #pragma unroll
-            for (int i = 0; i < EACH; ++i)
-                if (e0 + i >= at * size && e0 + i < (at + 1) * size) stay |= 1u << i;
+                for (int i = 0; i < EACH; ++i)
+                    if (l * per + i == g && i < per) score[i] = sum;
+            }
+            uint32_t taken = 0;                     // of the lane's groups
+            for (int n = 0; n < p.kept; ++n) {
+                double best = kNone;
+                int at = kMaxExperts;               // (a group whose score is -inf can be the best that is left)
+#pragma unroll
+                for (int i = 0; i < EACH; ++i)
+                    if (i < per && l * per + i < p.groups && !(taken >> i & 1) && (at == kMaxExperts || score[i] > best)) best = score[i], at = l * per + i;
+                best_lanes<LANES>(&best, &at);
+                if (at / per == l) taken |= 1u << (at - l * per);
+#pragma unroll
+                for (int i = 0; i < EACH; ++i)
+                    if (e0 + i >= at * size && e0 + i < (at + 1) * size) stay |= 1u << i;
+            }
         }
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
             if (!(stay >> i & 1)) c[i] = kNone;
     }
 
-    double sum = 0.;                    // of the chosen that are this lane's
+    int mine[SLOTS];                // slot l + i LANES
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) mine[i] = -1;
     for (int n = 0; n < p.k; ++n) {
         double best = kNone;
         int at = kMaxExperts;
@@ -160,22 +229,29 @@ __global__ __launch_bounds__(kThreads) void route_kernel(const RouteArgs p, long
         for (int i = 0; i < EACH; ++i)
             if (c[i] > best) best = c[i], at = e0 + i;
         best_lanes<LANES>(&best, &at);
-        const bool none = unfit || !(best > kNone);
-        if (!none && at >= e0 && at < e0 + each) {
-            double mine = 0.;
+        if (unfit || !(best > kNone)) break;        // (the token's lanes together)
 #pragma unroll
-            for (int i = 0; i < EACH; ++i)
-                if (e0 + i == at) mine = s[i], c[i] = kNone;
-            chosen[slot][n] = mine;
-            sum += mine;
-        }
-        if (none && l == 0) chosen[slot][n] = 0.;
-        if (there && l == 0) p.experts[t * p.k + n] = none ? -1 : at;
+        for (int i = 0; i < EACH; ++i)
+            if (e0 + i == at) c[i] = kNone;
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i)
+            if (n == l + i * LANES) mine[i] = at;
     }
-    sum = sum_lanes<LANES>(sum);
-    __syncthreads();
-    for (int n = l; n < p.k && there; n += LANES) {
-        const double w = chosen[slot][n], share = p.renorm ? sum > 0. ? w / sum : 0. : w;
+    double w[SLOTS], sum = 0.;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        w[i] = 0.;
+        if (mine[i] >= 0) w[i] = score_of(p, (double)(float)logits[mine[i]], top, total);
+        sum += w[i];
+    }
+    if (p.renorm) sum = sum_lanes<LANES>(sum);
+    if (!there) return;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        const int n = l + i * LANES;
+        if (n >= p.k) continue;
+        const double share = !p.renorm ? w[i] : sum > 0. ? w[i] / sum : 0.;
+        p.experts[t * p.k + n] = mine[i];
         p.weights[t * p.k + n] = unfit ? __uint_as_float(0x7fc00000u) : (float)(share * (double)p.factor);
     }
 }
@@ -209,11 +285,9 @@ __global__ __launch_bounds__(kThreads) void route_back_kernel(const RouteArgs p,
     float s[EACH];              // dense: the scores
     float top = NONE, total = 1.f;
     if (dense) {
+        load_logits<X, EACH>(logits, e0, each, p.E, LANES, NONE, s);
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            s[i] = i < each && e0 + i < p.E ? (float)logits[e0 + i] : NONE;
-            top = fmaxf(top, s[i]);
-        }
+        for (int i = 0; i < EACH; ++i) top = fmaxf(top, s[i]);
         top = max_of(top);
         total = 0.f;
 #pragma unroll
@@ -276,9 +350,18 @@ __global__ __launch_bounds__(kThreads) void route_back_kernel(const RouteArgs p,
     }
     if (!there) return;
     X *const out = (X *)p.dlogits + t * p.dstride;
+    X to[EACH];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i)
-        if (i < each && e0 + i < p.E) out[e0 + i] = (X)(empty ? 0.f : dense ? s[i] * (d[i] - dot) : d[i]);
+    for (int i = 0; i < EACH; ++i) to[i] = (X)(empty ? 0.f : dense ? s[i] * (d[i] - dot) : d[i]);
+    if (p.E == EACH * LANES) {
+        constexpr int V = 16 / sizeof(X) < EACH ? 16 / sizeof(X) : EACH;
+#pragma unroll
+        for (int i = 0; i < EACH; i += V) __builtin_memcpy(out + e0 + i, to + i, V * sizeof(X));
+    } else {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (i < each && e0 + i < p.E) out[e0 + i] = to[i];
+    }
 }
 
 template <class X, int LANES, int EACH>
@@ -335,7 +418,7 @@ __global__ __launch_bounds__(kListThreads) void list_count_kernel(const ListArgs
 
 __global__ __launch_bounds__(kListThreads) void list_kernel(const ListArgs p, long long run)
 {
-    extern __shared__ unsigned long long bits[];        // [kListWaves][E], then base [E]
+    extern __shared__ unsigned long long bits[];        // [kListWaves][E], then base [E] and room for as many
     int *const base = (int *)(bits + kListWaves * p.E);
     __shared__ int wave_sums[kListWaves], wave_tiles[kListWaves];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
@@ -351,12 +434,24 @@ __global__ __launch_bounds__(kListThreads) void list_kernel(const ListArgs p, lo
         }
         __syncthreads();
         if (t < p.E) all = base[t];
-    } else if (t < p.E) {
-        for (int b = 0; b < (int)gridDim.x; ++b) {
-            const int n = p.counts[(long long)b * p.E + t];
-            if (b < (int)blockIdx.x) before += n;
-            all += n;
+    } else {
+        // (the runs in as many parts as there are threads for, whose sums meet in LDS)
+        const int parts = kListThreads / p.E, runs = gridDim.x, part = t / p.E, e = t - part * p.E;
+        for (int i = t; i < 2 * p.E; i += kListThreads) base[i] = 0;
+        __syncthreads();
+        if (part < parts) {
+            const int from_run = (int)((long long)runs * part / parts), to_run = (int)((long long)runs * (part + 1) / parts);
+            int sum = 0, early = 0;
+#pragma unroll 8
+            for (int b = from_run; b < to_run; ++b) {
+                const int n = p.counts[(long long)b * p.E + e];
+                early += b < (int)blockIdx.x ? n : 0;
+                sum += n;
+            }
+            atomicAdd(&base[e], sum), atomicAdd(&base[p.E + e], early);
         }
+        __syncthreads();
+        if (t < p.E) all = base[t], before = base[p.E + t];
     }
     int upto = all;
 #pragma unroll
@@ -462,7 +557,7 @@ hipError_t launch_route_lists(const ListArgs &p, hipStream_t st)
 {
     const long long run = list_run(p.pairs);
     const int runs = (int)std::max<long long>(1, (p.pairs + run - 1) / run);
-    const size_t lds = (size_t)kListWaves * p.E * 8 + p.E * 4;
+    const size_t lds = (size_t)kListWaves * p.E * 8 + p.E * 8;
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&list_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
