@@ -13,7 +13,7 @@ namespace xnor {
 namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * kWave, kValues = 128;
-constexpr int kMostGroups = 16;         // whose scales a wave holds at a time
+constexpr int kMostGroups = 4;          // whose scales a wave holds at a time: one a lane
 
 // d[i] of the 16 lanes g to d[g] of the 16 lanes i.
 __device__ inline void turn_about(uint32_t (&d)[4])
@@ -32,10 +32,10 @@ __device__ inline void turn_about(uint32_t (&d)[4])
 #endif
 }
 
-// A wave's scales and zero points of some groups: fp32 [kMostGroups][16], a byte each.
+// A wave's scales and zero points of some groups' 16 rows.
 struct Held {
     float scale[kMostGroups * 16];
-    uint32_t zero[kMostGroups * 4];
+    uint32_t zero[kMostGroups * 16];
 };
 
 // What a wave multiplies.
@@ -48,112 +48,107 @@ struct Span {
     Held *held;                     // [MATS]
 };
 
-// U steps from s on.  WHOLE: all of their values are there.
-template <class T, int MATS, int TT, int GROUPS, int U, bool WHOLE, bool EXACT>
-__device__ inline void some_steps(const Span<T, MATS, TT> &p, int s, f32x4 (&acc)[MATS][TT])
+// U steps as they are loaded.
+template <int MATS, int TT, int U>
+struct Stage {
+    uint32_t w[MATS][U][4];
+    uint16_t low[MATS], high[MATS];     // halves of a scale (16-bit ones: both the same)
+    uint8_t zero[MATS];
+    i32x4 x[U][4][TT];
+};
+// (Four tiles of tokens are loaded where they are used: there are no registers for them.)
+template <int TT> constexpr bool kEarly = TT < 4;
+
+template <class T, int MATS, int TT, int U, bool WHOLE>
+__device__ inline void load_x(const Span<T, MATS, TT> &p, int s, int u, Stage<MATS, TT, U> &to)
 {
-    typedef Mat<T> Mul;
-    typedef Levels<T> Level;
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int j = 0; j < TT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int from = (s + u) * kValues + i * 32 + g * 8;
+            if constexpr (WHOLE) {
+                __builtin_memcpy(&to.x[u][i][j], p.x[j] + from, 16);
+            } else {
+                T v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = p.x[j][min(from + e, p.K - 1)];
+                    v[e] = from + e < p.K ? v[e] : T(0);
+                }
+                to.x[u][i][j] = __builtin_bit_cast(i32x4, v);
+            }
+        }
+}
+
+// U steps from s on.  WHOLE: all of their values are there.
+template <class T, int MATS, int TT, int GROUPS, int U, bool WHOLE>
+__device__ inline void load_stage(const Span<T, MATS, TT> &p, int s, Stage<MATS, TT, U> &to)
+{
     static_assert(U * GROUPS <= kMostGroups, "");
-    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    // scales and zero points of group lane / 4's rows 4 (lane & 3) .. + 3
-    const int rows = p.n0 + (lane & 3) * 4;
-    const long long group = min(s * GROUPS + min(lane >> 2, U * GROUPS - 1), p.groups - 1), at = group * p.N;
-    float scale[MATS][4];
-    uint32_t zero[MATS];
-    uint32_t held[MATS][U][4];
-    i32x4 vx[U][4][TT];
-    uint32_t raw[MATS][4];
-    if (p.N >= 16) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    // group lane / 16's of row lane % 16; no branch by the scales' type or for want of zero points
+    const long long at = (long long)min(s * GROUPS + min(g, U * GROUPS - 1), p.groups - 1) * p.N + min(p.n0 + (lane & 15), p.N - 1);
+    const bool wide = p.scale_type == XNOR_TYPE_FP32;
 #pragma unroll
-        for (int k = 0; k < MATS; ++k) {
-            if (p.scale_type == XNOR_TYPE_FP32) __builtin_memcpy(raw[k], (const float *)p.view[k].scale + at + rows, 16);
-            else __builtin_memcpy(raw[k], (const f16_t *)p.view[k].scale + at + rows, 8);
-            zero[k] = 0x08080808u;
-            if (p.view[k].zero) __builtin_memcpy(&zero[k], p.view[k].zero + at + rows, 4);
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < MATS; ++k) {
-            load_scales(p.view[k], p.scale_type, group, rows, p.N, scale[k]);
-            zero[k] = p.view[k].zero ? 0u : 0x08080808u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (p.view[k].zero && rows + i < p.N) zero[k] |= (uint32_t)p.view[k].zero[at + rows + i] << 8 * i;
-        }
+    for (int k = 0; k < MATS; ++k) {
+        const uint16_t *const scale = (const uint16_t *)p.view[k].scale + (wide ? 2 * at : at);
+        to.low[k] = scale[0], to.high[k] = scale[wide ? 1 : 0];
+        to.zero[k] = *(p.view[k].zero ? p.view[k].zero + at : (const uint8_t *)scale);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int k = 0; k < MATS; ++k) {
             if constexpr (WHOLE) {
-                __builtin_memcpy(held[k][u], p.w[k] + (s + u) * (kValues / 8) + g * 4, 16);
+                __builtin_memcpy(to.w[k][u], p.w[k] + (s + u) * (kValues / 8) + g * 4, 16);
             } else {
                 // (words behind the last one: any levels, as the tokens' values are zeros there)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) held[k][u][i] = p.w[k][min((s + u) * (kValues / 8) + g * 4 + i, (p.K - 1) / 8)];
+                for (int i = 0; i < 4; ++i) to.w[k][u][i] = p.w[k][min((s + u) * (kValues / 8) + g * 4 + i, (p.K - 1) / 8)];
             }
         }
-    auto load_x = [&](int u) __attribute__((always_inline)) {
+    if constexpr (kEarly<TT>)
 #pragma unroll
-        for (int j = 0; j < TT; ++j) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int from = (s + u) * kValues + i * 32 + g * 8;
-                if constexpr (WHOLE) {
-                    __builtin_memcpy(&vx[u][i][j], p.x[j] + from, 16);
-                } else {
-                    T v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        v[e] = p.x[j][min(from + e, p.K - 1)];
-                        v[e] = from + e < p.K ? v[e] : T(0);
-                    }
-                    vx[u][i][j] = __builtin_bit_cast(i32x4, v);
-                }
-            }
-        }
-    };
-    if constexpr (TT < 4)
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_x(u);
+        for (int u = 0; u < U; ++u) load_x<T, MATS, TT, U, WHOLE>(p, s, u, to);
+}
+
+template <class T, int MATS, int TT, int GROUPS, int U, bool WHOLE, bool EXACT>
+__device__ inline void use_stage(const Span<T, MATS, TT> &p, int s, Stage<MATS, TT, U> &from, f32x4 (&acc)[MATS][TT])
+{
+    typedef Mat<T> Mul;
+    typedef Levels<T> Level;
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int k = 0; k < MATS; ++k) {
-        if (p.N >= 16) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t half = raw[k][i / 2] >> 16 * (i & 1) & 0xffffu;
-                scale[k][i] = p.scale_type == XNOR_TYPE_FP32 ? __uint_as_float(raw[k][i])
-                              : p.scale_type == XNOR_TYPE_F16 ? (float)__builtin_bit_cast(f16_t, (uint16_t)half) : __uint_as_float(half << 16);
-            }
-        }
-        if ((lane >> 2) < U * GROUPS) {
-            *(f32x4 *)&p.held[k].scale[lane * 4] = f32x4{scale[k][0], scale[k][1], scale[k][2], scale[k][3]};
-            p.held[k].zero[lane] = zero[k];
-        }
+        const uint32_t bits = p.scale_type == XNOR_TYPE_FP32 ? (uint32_t)from.high[k] << 16 | from.low[k] : (uint32_t)from.low[k] << 16;
+        const float half = (float)__builtin_bit_cast(f16_t, from.low[k]);
+        p.held[k].scale[lane] = p.scale_type == XNOR_TYPE_F16 ? half : __uint_as_float(bits);
+        p.held[k].zero[lane] = p.view[k].zero ? from.zero[k] & 15u : 8u;
     }
     // (a wave's own: its LDS instructions come in order)
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if constexpr (TT == 4) load_x(u);
+        if constexpr (!kEarly<TT>) load_x<T, MATS, TT, U, WHOLE>(p, s, u, from);
 #pragma unroll
         for (int k = 0; k < MATS; ++k) {
-            turn_about(held[k][u]);
+            turn_about(from.w[k][u]);
 #pragma unroll
             for (int i = 0; i < GROUPS; ++i) {
                 const int of = u * GROUPS + i;
-                const typename Level::Zero z = Level::zero(((const uint8_t *)p.held[k].zero)[of * 16 + r] & 15u);
+                const typename Level::Zero z = Level::zero(p.held[k].zero[of * 16 + r]);
                 const f32x4 by = *(const f32x4 *)&p.held[k].scale[of * 16 + g * 4];
                 f32x4 part[TT] = {};
 #pragma unroll
                 for (int q = i * (4 / GROUPS); q < (i + 1) * (4 / GROUPS); ++q) {
-                    const i32x4 levels = Level::template operand<EXACT>(held[k][u][q], z);
+                    const i32x4 levels = Level::template operand<EXACT>(from.w[k][u][q], z);
 #pragma unroll
                     for (int j = 0; j < TT; ++j) {
-                        part[j] = Mul::mul(levels, vx[u][q][j], part[j]);
-                        if constexpr (Level::kOffset && !EXACT) part[j] = Mul::mul(Level::offset(z), vx[u][q][j], part[j]);
+                        part[j] = Mul::mul(levels, from.x[u][q][j], part[j]);
+                        if constexpr (Level::kOffset && !EXACT) part[j] = Mul::mul(Level::offset(z), from.x[u][q][j], part[j]);
                     }
                 }
 #pragma unroll
@@ -168,8 +163,8 @@ __device__ inline void some_steps(const Span<T, MATS, TT> &p, int s, f32x4 (&acc
     __builtin_amdgcn_wave_barrier();
 }
 
-// Steps from .. to - 1.
-// U: steps whose loads are on their way together.
+// Steps from .. to - 1, U at a time: those of the next time are on their way while these are used, loaded in straight lines of code (behind a branch the wait
+// for one would be a wait for both).
 template <class T, int MATS, int TT, int GROUPS, int U>
 __device__ inline void accumulate(const Span<T, MATS, TT> &p, int from, int to, f32x4 (&acc)[MATS][TT])
 {
@@ -179,9 +174,36 @@ __device__ inline void accumulate(const Span<T, MATS, TT> &p, int from, int to, 
         for (int j = 0; j < TT; ++j) acc[k][j] = f32x4{};
     const int whole = min(to, p.K / kValues);
     int s = from;
-    for (; s + U <= whole; s += U) some_steps<T, MATS, TT, GROUPS, U, true, false>(p, s, acc);
-    for (; s < whole; ++s) some_steps<T, MATS, TT, GROUPS, 1, true, false>(p, s, acc);
-    for (; s < to; ++s) some_steps<T, MATS, TT, GROUPS, 1, false, false>(p, s, acc);
+    if (s + U <= whole) {
+        Stage<MATS, TT, U> a, b;
+        load_stage<T, MATS, TT, GROUPS, U, true>(p, s, a);
+        for (; s + 3 * U <= whole; s += 2 * U) {
+            load_stage<T, MATS, TT, GROUPS, U, true>(p, s + U, b);
+            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s, a, acc);
+            load_stage<T, MATS, TT, GROUPS, U, true>(p, s + 2 * U, a);
+            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s + U, b, acc);
+        }
+        if (s + 2 * U <= whole) {
+            load_stage<T, MATS, TT, GROUPS, U, true>(p, s + U, b);
+            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s, a, acc);
+            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s + U, b, acc);
+            s += 2 * U;
+        } else {
+            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s, a, acc);
+            s += U;
+        }
+    }
+    if constexpr (U > 1)
+        for (; s < whole; ++s) {
+            Stage<MATS, TT, 1> a;
+            load_stage<T, MATS, TT, GROUPS, 1, true>(p, s, a);
+            use_stage<T, MATS, TT, GROUPS, 1, true, false>(p, s, a, acc);
+        }
+    if (s < to) {
+        Stage<MATS, TT, 1> a;
+        load_stage<T, MATS, TT, GROUPS, 1, false>(p, s, a);
+        use_stage<T, MATS, TT, GROUPS, 1, false, false>(p, s, a, acc);
+    }
     if constexpr (Levels<T>::kOffset) {
         auto is_odd = [](float v) { return !(fabsf(v) <= 3.402823466e38f); };
         bool odd = false;
@@ -193,7 +215,11 @@ __device__ inline void accumulate(const Span<T, MATS, TT> &p, int from, int to, 
                 for (int e = 0; e < 4; ++e) odd |= is_odd(acc[k][j][e]);
         if (__any(odd)) {
             f32x4 exact[MATS][TT] = {};
-            for (s = from; s < to; ++s) some_steps<T, MATS, TT, GROUPS, 1, false, true>(p, s, exact);
+            for (s = from; s < to; ++s) {
+                Stage<MATS, TT, 1> a;
+                load_stage<T, MATS, TT, GROUPS, 1, false>(p, s, a);
+                use_stage<T, MATS, TT, GROUPS, 1, false, true>(p, s, a, exact);
+            }
 #pragma unroll
             for (int k = 0; k < MATS; ++k)
 #pragma unroll
@@ -249,7 +275,7 @@ __global__ __launch_bounds__(kThreads, TT == 1 ? 4 : 2) void int4_few_kernel(con
 
     const int steps = (p.K + kValues - 1) / kValues, share = (steps + kWaves - 1) / kWaves;
     f32x4 acc[MATS][TT];
-    accumulate<T, MATS, TT, GROUPS, (GATED || TT > 1 ? 2 : 4)>(span, wave * share, min(steps, wave * share + share), acc);
+    accumulate<T, MATS, TT, GROUPS, (GATED || TT > 1 || GROUPS == 4 ? 1 : 2)>(span, wave * share, min(steps, wave * share + share), acc);
 #pragma unroll
     for (int k = 0; k < MATS; ++k)
 #pragma unroll
@@ -337,7 +363,7 @@ __global__ __launch_bounds__(kDownWaves * kWave) void int4_down_kernel(const Int
         span.x[0] = (const T *)((const char *)p.x + m * p.ldx);
         span.n0 = n0, span.N = p.N, span.K = p.K, span.groups = (p.K + p.group - 1) / p.group, span.scale_type = p.scale_type, span.held = &held[wave];
         f32x4 acc[1][1];
-        accumulate<T, 1, 1, GROUPS, 2>(span, min(part * share, steps), min(steps, part * share + share), acc);
+        accumulate<T, 1, 1, GROUPS, (GROUPS == 4 ? 1 : 2)>(span, min(part * share, steps), min(steps, part * share + share), acc);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += weight * acc[0][0][e];
     }
