@@ -37,8 +37,22 @@ Int4Args args_of(const void *x, long long ldx, const xnor_int4 *w, const xnor_in
     Int4Args a{};
     a.x = x, a.ldx = ldx, a.w = {w->q, w->scale, w->zero}, a.ldq = w->q_stride, a.scale_type = w->scale_type, a.group = w->group;
     if (w2) a.w2 = {w2->q, w2->scale, w2->zero};
-    a.M = M, a.N = w->rows, a.K = w->cols, a.out = out, a.out_type = out_type, a.ldo = ldo;
+    a.parts = 1, a.M = M, a.N = w->rows, a.K = w->cols, a.out = out, a.out_type = out_type, a.ldo = ldo;
     return a;
+}
+
+int product_workspace(long long M, int N, int K, bool gated, size_t *bytes)
+{
+    if (M < 0 || M > kMaxRows || N <= 0 || N > kMaxCols || K <= 0 || K > kMaxCols) return XNOR_E_SHAPE;
+    const int parts = int4_tile_parts(M, N, K, gated);
+    *bytes = parts > 1 ? (size_t)parts * (gated ? 2 : 1) * M * N * sizeof(float) : 0;
+    return XNOR_OK;
+}
+// Shares of the contraction, given the workspace for them.
+void take_workspace(Int4Args *a, bool gated, void *workspace, size_t bytes)
+{
+    const int parts = int4_tile_parts(a->M, a->N, a->K, gated);
+    if (parts > 1 && workspace && bytes >= (size_t)parts * (gated ? 2 : 1) * a->M * a->N * sizeof(float)) a->parts = parts, a->sums = (float *)workspace;
 }
 
 // Sizes of a call of xnor_int4_experts, and its workspace's parts, each at a multiple of 256 bytes.
@@ -125,9 +139,7 @@ int xnor_int4_dequantize(const xnor_int4 *w, void *out, int out_type, long long 
 int xnor_int4_linear_workspace_bytes(long long M, int N, int K, size_t *bytes)
 {
     if (!bytes) return XNOR_E_NULL;
-    if (M < 0 || M > kMaxRows || N <= 0 || N > kMaxCols || K <= 0 || K > kMaxCols) return XNOR_E_SHAPE;
-    *bytes = 0;
-    return XNOR_OK;
+    return product_workspace(M, N, K, false, bytes);
 }
 
 int xnor_int4_linear(const void *x, int type, long long x_stride, const xnor_int4 *w, const float *bias, long long M, void *out, int out_type,
@@ -141,10 +153,15 @@ int xnor_int4_linear(const void *x, int type, long long x_stride, const xnor_int
     if (!aligned(bias, 4) || !aligned(workspace, 16)) return XNOR_E_ALIGN;
     Int4Args a = args_of(x, 2 * x_stride, w, nullptr, M, out, out_type, out_stride);
     a.bias = bias;
+    take_workspace(&a, false, workspace, workspace_bytes);
     return hip_status(launch_int4(a, type, false, (hipStream_t)stream));
 }
 
-int xnor_int4_gated_workspace_bytes(long long M, int F, int K, size_t *bytes) { return xnor_int4_linear_workspace_bytes(M, F, K, bytes); }
+int xnor_int4_gated_workspace_bytes(long long M, int F, int K, size_t *bytes)
+{
+    if (!bytes) return XNOR_E_NULL;
+    return product_workspace(M, F, K, true, bytes);
+}
 
 int xnor_int4_gated(const void *x, int type, long long x_stride, const xnor_int4 *wg, const xnor_int4 *wu, int act, long long M, void *h, int h_type,
                     long long h_stride, void *workspace, size_t workspace_bytes, void *stream)
@@ -157,6 +174,7 @@ int xnor_int4_gated(const void *x, int type, long long x_stride, const xnor_int4
     if (!aligned(workspace, 16)) return XNOR_E_ALIGN;
     Int4Args a = args_of(x, 2 * x_stride, wg, wu, M, h, h_type, h_stride);
     a.act = act;
+    take_workspace(&a, true, workspace, workspace_bytes);
     return hip_status(launch_int4(a, type, true, (hipStream_t)stream));
 }
 

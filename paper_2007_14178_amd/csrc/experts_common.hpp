@@ -64,12 +64,20 @@ struct Int4Args {
     const int32_t *order_x, *order_out;
     const int32_t *pairs;       // experts' pairs, each by itself (tiles NULL): row m is that of expert pairs[m], x's row m / chosen
     int E, chosen;
+    int parts;                  // > 1: shares of the contraction, their sums fp32 [parts][matrices][M][N] in `sums`, joined by a second launch
+    float *sums;
     long long first;            // (set by the launchers: the launch's first tile of tokens)
 };
-// Tiles of more tokens than this go to the kernel for many.
+// Tiles of more of an expert's tokens than this go to the kernel for many.
 constexpr int kInt4Few = 64;
-// Whether so few pairs are better taken each by itself, without lists.
-inline bool int4_pairs_pay(long long pairs, int E) { return pairs <= 64 && pairs <= E; }
+// Whether a product goes there: of more than 64 tokens unless that is little work (us on the kernel for few and for many, with its shares of the contraction:
+// 256 x 1024 x 1024 9.1 and 13.9, 128 x 4096 x 4096 22.2 and 25.8, 192 x 4096 x 4096 40.9 and 30.6, 128 x 8192 x 8192 74 and 43).
+inline bool int4_many(long long M, long long N, long long K) { return M > kInt4Few && (M + 63) / 64 * N * K > 1LL << 23; }
+// Whether so few pairs are better taken each by itself, without lists: experts of several are read for each of theirs, from the caches mostly.  us, by
+// lists and by pairs, for tokens to k of E experts, width x hidden (bf16, groups of 128):
+//     8 of 64, 2048 x 1024    1: 21.9 16.2    4: 40.1 35.7    8: 51.3 61.9        2 of 8, 4096 x 2048     1: 18.7 13.4    2: 27.7 22.2    4: 31.9 37.3
+//     8 of 128, 2048 x 512    1: 17.8 10.6    8: 43.7 37.9   16: 60.4 67.4        4 of 32, 1024 x 768     4: 18.4 11.9    8: 23.7 19.3   16: 26.7 32.9
+inline bool int4_pairs_pay(long long pairs, int E) { return pairs <= 4 || 4 * pairs <= 3LL * E; }
 // A token's chosen experts' second products and their sum in one launch: x holds the rows of the pairs, weights their shares, M the tokens.
 hipError_t launch_int4_down(const Int4Args &p, const float *weights, int type, hipStream_t st);
 // GATED: w and w2 with the activation.
@@ -78,6 +86,7 @@ bool int4_tiles_support(const Int4Args &p);
 hipError_t launch_int4_tiles(const Int4Args &p, int type, bool gated, hipStream_t st);
 // By the number of tokens (experts: by the tiles that they were cut into).
 hipError_t launch_int4(const Int4Args &p, int type, bool gated, hipStream_t st);
+int int4_tile_parts(long long M, int N, int K, bool gated);
 int int4_expert_tile(long long pairs, int E);
 
 struct Int4Make {

@@ -78,6 +78,28 @@ template <> struct Levels<bf16_t> {
     }
 };
 
+// Eight 16-bit values of a row of n from `at` on, of which those behind the row's end are zeros: the row's last eight, moved down.
+template <class T>
+__device__ inline i32x4 load_end(const T *row, int at, int n)
+{
+    if (n >= 8) {
+        unsigned long long v[2];
+        __builtin_memcpy(v, row + min(at, n - 8), 16);
+        const int by = min(max(at - (n - 8), 0), 8), bits = 16 * (by & 3);
+        unsigned long long low = by >= 8 ? 0 : by >= 4 ? v[1] : v[0], high = by >= 4 ? 0 : v[1];
+        low = low >> bits | (bits ? high << (64 - bits) : 0);
+        high >>= bits;
+        return i32x4{(int)low, (int)(low >> 32), (int)high, (int)(high >> 32)};
+    }
+    T v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] = row[min(at + e, n - 1)];
+        v[e] = at + e < n ? v[e] : T(0);
+    }
+    return __builtin_bit_cast(i32x4, v);
+}
+
 // Scales of rows n .. n + 3 in group g, 0 behind the last row.
 __device__ inline void load_scales(const Int4View &w, int type, long long g, int n, int N, float (&to)[4])
 {

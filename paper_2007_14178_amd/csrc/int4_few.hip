@@ -1,6 +1,6 @@
 // Products of few tokens with 4-bit weights (a decoding step): the weights are read once, and that is what they take.
 //
-// A workgroup has 16 rows of the weights (of each matrix in the gated block), its eight waves an eighth of the contraction each, whose sums are added
+// A workgroup has 16 rows of the weights (of each matrix in the gated block), its eight waves an eighth of the contraction each (or four a quarter), whose sums are added
 // in LDS.  A step is 128 values, 64 bytes of a row: lane (r, g) loads 16 bytes, row r's values 32 g .. 32 g + 31, and two exchanges across the wave
 // turn the four words of the four lanes of a row about, so that instruction i takes the values 32 i .. 32 i + 31, which have one scale.
 // A group's sum is multiplied by its scale in fp32: the weights are never rounded.  Some steps' loads are on their way together, behind no branch; their
@@ -12,7 +12,7 @@
 namespace xnor {
 namespace {
 
-constexpr int kWaves = 8, kThreads = kWaves * kWave, kValues = 128;
+constexpr int kValues = 128;
 constexpr int kMostGroups = 4;          // whose scales a wave holds at a time: one a lane
 
 // d[i] of the 16 lanes g to d[g] of the 16 lanes i.
@@ -44,7 +44,8 @@ struct Span {
     Int4View view[MATS];
     const uint32_t *w[MATS];        // the lane's row
     const T *x[TT];                 // the lane's token (or another's, where there is none)
-    int n0, N, K, groups, scale_type;
+    int row[MATS];                  // the lane's
+    int N, K, groups, scale_type;
     Held *held;                     // [MATS]
 };
 
@@ -68,17 +69,8 @@ __device__ inline void load_x(const Span<T, MATS, TT> &p, int s, int u, Stage<MA
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int from = (s + u) * kValues + i * 32 + g * 8;
-            if constexpr (WHOLE) {
-                __builtin_memcpy(&to.x[u][i][j], p.x[j] + from, 16);
-            } else {
-                T v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] = p.x[j][min(from + e, p.K - 1)];
-                    v[e] = from + e < p.K ? v[e] : T(0);
-                }
-                to.x[u][i][j] = __builtin_bit_cast(i32x4, v);
-            }
+            if constexpr (WHOLE) __builtin_memcpy(&to.x[u][i][j], p.x[j] + from, 16);
+            else to.x[u][i][j] = load_end(p.x[j], from, p.K);
         }
 }
 
@@ -89,10 +81,11 @@ __device__ inline void load_stage(const Span<T, MATS, TT> &p, int s, Stage<MATS,
     static_assert(U * GROUPS <= kMostGroups, "");
     const int lane = threadIdx.x & 63, g = lane >> 4;
     // group lane / 16's of row lane % 16; no branch by the scales' type or for want of zero points
-    const long long at = (long long)min(s * GROUPS + min(g, U * GROUPS - 1), p.groups - 1) * p.N + min(p.n0 + (lane & 15), p.N - 1);
+    const long long group = (long long)min(s * GROUPS + min(g, U * GROUPS - 1), p.groups - 1) * p.N;
     const bool wide = p.scale_type == XNOR_TYPE_FP32;
 #pragma unroll
     for (int k = 0; k < MATS; ++k) {
+        const long long at = group + p.row[k];
         const uint16_t *const scale = (const uint16_t *)p.view[k].scale + (wide ? 2 * at : at);
         to.low[k] = scale[0], to.high[k] = scale[wide ? 1 : 0];
         to.zero[k] = *(p.view[k].zero ? p.view[k].zero + at : (const uint8_t *)scale);
@@ -231,22 +224,24 @@ __device__ inline void accumulate(const Span<T, MATS, TT> &p, int from, int to, 
     }
 }
 
-// The first of a workgroup's 16 rows: the last workgroup's are the matrix's last ones, some of them another's too, which come out alike.
-__device__ inline int first_row(int block, int N) { return max(0, min(block * 16, N - 16)); }
+// The first of a workgroup's `rows` rows: the last workgroup's are the matrix's last ones, some of them another's too, which come out alike.
+__device__ inline int first_row(int block, int rows, int N) { return max(0, min(block * rows, N - rows)); }
 
-// TT: tiles of 16 tokens.  GROUPS: of a step.
-template <class T, bool GATED, int TT, int GROUPS>
-__global__ __launch_bounds__(kThreads, TT == 1 ? 4 : 2) void int4_few_kernel(const Int4Args p)
+// TT: tiles of 16 tokens.  GROUPS: of a step.  MATS: 2: the gated block's matrices, or two times 16 rows of one (more than 16 tokens, whose values
+// are most of what is read: 64 x 4096 x 4096 20 us by 16 rows).
+template <class T, bool GATED, int TT, int GROUPS, int WAVES, int MATS>
+__global__ __launch_bounds__(WAVES * kWave, TT == 1 ? 4 : 2) void int4_few_kernel(const Int4Args p)
 {
-    constexpr int MATS = GATED ? 2 : 1;
-    __shared__ f32x4 sums[kWaves][MATS][TT][kWave];
-    __shared__ Held held[kWaves][MATS];
+    static_assert(!GATED || MATS == 2, "");
+    constexpr int ROWS = GATED ? 16 : 16 * MATS;
+    __shared__ f32x4 sums[WAVES][MATS][TT][kWave];
+    __shared__ Held held[WAVES][MATS];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = lane & 15, g = lane >> 4;
-    const int n0 = first_row(blockIdx.x, p.N);
+    const int n0 = first_row(blockIdx.x, ROWS, p.N);
 
     Span<T, MATS, TT> span;
-    span.view[0] = p.w;
-    if constexpr (GATED) span.view[1] = p.w2;
+#pragma unroll
+    for (int k = 0; k < MATS; ++k) span.view[k] = GATED && k ? p.w2 : p.w;
     long long m0 = (p.first + blockIdx.y) * (16 * TT);
     int count = (int)min(p.M - m0, 16LL * TT);
     int expert = -1;
@@ -259,11 +254,11 @@ __global__ __launch_bounds__(kThreads, TT == 1 ? 4 : 2) void int4_few_kernel(con
         const ExpertTile tile = p.tiles[1 + p.first + blockIdx.y];
         m0 = tile.first, count = tile.count, expert = tile.expert;
     }
-    const int row = min(n0 + r, p.N - 1);
 #pragma unroll
     for (int k = 0; k < MATS; ++k) {
         if (expert >= 0) span.view[k] = of_stack(span.view[k], p, expert);
-        span.w[k] = (const uint32_t *)(span.view[k].q + row * p.ldq);
+        span.row[k] = min(n0 + (GATED ? 0 : 16 * k) + r, p.N - 1);
+        span.w[k] = (const uint32_t *)(span.view[k].q + span.row[k] * p.ldq);
     }
 #pragma unroll
     for (int j = 0; j < TT; ++j) {
@@ -271,11 +266,11 @@ __global__ __launch_bounds__(kThreads, TT == 1 ? 4 : 2) void int4_few_kernel(con
         const long long from = p.pairs ? m / p.chosen : p.order_x ? p.order_x[m] / p.chosen : m;
         span.x[j] = (const T *)((const char *)p.x + from * p.ldx);
     }
-    span.n0 = n0, span.N = p.N, span.K = p.K, span.groups = (p.K + p.group - 1) / p.group, span.scale_type = p.scale_type, span.held = held[wave];
+    span.N = p.N, span.K = p.K, span.groups = (p.K + p.group - 1) / p.group, span.scale_type = p.scale_type, span.held = held[wave];
 
-    const int steps = (p.K + kValues - 1) / kValues, share = (steps + kWaves - 1) / kWaves;
+    const int steps = (p.K + kValues - 1) / kValues;
     f32x4 acc[MATS][TT];
-    accumulate<T, MATS, TT, GROUPS, (GATED || TT > 1 || GROUPS == 4 ? 1 : 2)>(span, wave * share, min(steps, wave * share + share), acc);
+    accumulate<T, MATS, TT, GROUPS, (MATS == 2 || TT > 1 || GROUPS == 4 ? 1 : 2)>(span, steps * wave / WAVES, steps * (wave + 1) / WAVES, acc);
 #pragma unroll
     for (int k = 0; k < MATS; ++k)
 #pragma unroll
@@ -283,45 +278,63 @@ __global__ __launch_bounds__(kThreads, TT == 1 ? 4 : 2) void int4_few_kernel(con
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < TT; ++j) {
-        const int n = n0 + g * 4;
-        if (wave != j % kWaves || j * 16 + r >= count || n >= p.N) continue;       // (a wave a tile of tokens)
+        if (wave != j % WAVES || j * 16 + r >= count) continue;       // (a wave a tile of tokens)
         f32x4 v[MATS];
 #pragma unroll
         for (int k = 0; k < MATS; ++k) {
             v[k] = sums[0][k][j][lane];
 #pragma unroll
-            for (int i = 1; i < kWaves; ++i) v[k] += sums[i][k][j][lane];
+            for (int i = 1; i < WAVES; ++i) v[k] += sums[i][k][j][lane];
         }
-        float out[4], bias[4];
-        load_params(p.bias, n, p.N, 0.f, bias);
+        const long long m = m0 + j * 16 + r, to = p.order_out ? p.order_out[m] : m;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if constexpr (GATED) out[e] = gate(p.act, p.out_type != XNOR_TYPE_FP32, v[0][e]) * v[1][e];
-            else out[e] = p.bias ? v[0][e] + bias[e] : v[0][e];
+        for (int k = 0; k < (GATED ? 1 : MATS); ++k) {
+            const int n = n0 + 16 * k + g * 4;
+            if (n >= p.N) continue;
+            float out[4], bias[4];
+            load_params(p.bias, n, p.N, 0.f, bias);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (GATED) out[e] = gate(p.act, p.out_type != XNOR_TYPE_FP32, v[0][e]) * v[1][e];
+                else out[e] = p.bias ? v[k][e] + bias[e] : v[k][e];
+            }
+            store_outputs(p, to, n, out);
         }
-        const long long m = m0 + j * 16 + r;
-        store_outputs(p, p.order_out ? p.order_out[m] : m, n, out);
     }
+}
+
+template <class T, bool GATED, int TT, int WAVES, int MATS>
+hipError_t few_of(const Int4Args &p, hipStream_t st)
+{
+    constexpr long long kMost = 32768;          // tiles of tokens in a launch
+    const int TM = 16 * TT;
+    const long long tiles = p.pairs ? p.M : p.tiles ? most_tiles(p.M, p.E, TM) : (p.M + TM - 1) / TM;
+    const long long each = std::max<long long>(1, std::min<long long>(kMost, kMaxBlocks / ceil_div(p.N, GATED ? 16 : 16 * MATS)));
+    for (long long m = 0; m < tiles; m += each) {
+        Int4Args q = p;
+        q.first = m;
+        const dim3 grid((unsigned)ceil_div(p.N, GATED ? 16 : 16 * MATS), (unsigned)std::min(each, tiles - m)), block(WAVES * kWave);
+        if (p.group == 128) int4_few_kernel<T, GATED, TT, 1, WAVES, MATS><<<grid, block, 0, st>>>(q);
+        else if (p.group == 64) int4_few_kernel<T, GATED, TT, 2, WAVES, MATS><<<grid, block, 0, st>>>(q);
+        else int4_few_kernel<T, GATED, TT, 4, WAVES, MATS><<<grid, block, 0, st>>>(q);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <class T, bool GATED, int TT>
 hipError_t few(const Int4Args &p, hipStream_t st)
 {
-    constexpr long long kMost = 32768;          // tiles of tokens in a launch
-    const int TM = 16 * TT;
-    const long long tiles = p.pairs ? p.M : p.tiles ? most_tiles(p.M, p.E, TM) : (p.M + TM - 1) / TM;
-    const long long each = std::max<long long>(1, std::min<long long>(kMost, kMaxBlocks / ceil_div(p.N, 16)));
-    for (long long m = 0; m < tiles; m += each) {
-        Int4Args q = p;
-        q.first = m;
-        const dim3 grid((unsigned)ceil_div(p.N, 16), (unsigned)std::min(each, tiles - m)), block(kThreads);
-        if (p.group == 128) int4_few_kernel<T, GATED, TT, 1><<<grid, block, 0, st>>>(q);
-        else if (p.group == 64) int4_few_kernel<T, GATED, TT, 2><<<grid, block, 0, st>>>(q);
-        else int4_few_kernel<T, GATED, TT, 4><<<grid, block, 0, st>>>(q);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    // Four waves where there is a workgroup for each unit (24 tokens to 3 of 30 experts, 1100 x 777, in groups of 32: 16.9 and 13.4 us, with eight 19.9 and 16.0;
+    // 1 x 4096 x 4096 6.1 and 6.0), eight where there are fewer
+    const long long tiles = p.pairs || p.tiles ? p.M : (p.M + 16 * TT - 1) / (16 * TT);
+    // (and of one matrix twice 16 rows where that leaves a workgroup a unit: 64 x 8192 x 8192 41 us, by 16 rows 67, x 4096 x 4096 21.8 and 20.4)
+    const long long units = compute_units();
+    if constexpr (!GATED)
+        if (!p.pairs && (TT > 1 || (p.tiles ? p.tile : p.M) > 4) && tiles * ceil_div(p.N, 32) >= units) return tiles * ceil_div(p.N, 32) >= 2 * units ? few_of<T, GATED, TT, 4, 2>(p, st) : few_of<T, GATED, TT, 8, 2>(p, st);
+    constexpr int MATS = GATED ? 2 : 1;
+    return tiles * ceil_div(p.N, 16) >= units * (TT == 1 ? 1 : 2) ? few_of<T, GATED, TT, 4, MATS>(p, st) : few_of<T, GATED, TT, 8, MATS>(p, st);
 }
 
 template <class T, bool GATED>
@@ -343,9 +356,9 @@ __global__ __launch_bounds__(kDownWaves * kWave) void int4_down_kernel(const Int
     __shared__ f32x4 sums[kDownWaves][4];
     __shared__ Held held[kDownWaves];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = lane & 15, g = lane >> 4;
-    const int n0 = first_row(blockIdx.x, p.N), row = min(n0 + r, p.N - 1);
+    const int n0 = first_row(blockIdx.x, 16, p.N), row = min(n0 + r, p.N - 1);
     const long long token = p.first + blockIdx.y;
-    const int steps = (p.K + kValues - 1) / kValues, share = (steps + shares - 1) / shares;
+    const int steps = (p.K + kValues - 1) / kValues;
     f32x4 sum = {};
     float none = 0.f;           // of slots without an expert: weight * 0
     for (int item = wave; item < p.chosen * shares; item += kDownWaves) {
@@ -361,9 +374,9 @@ __global__ __launch_bounds__(kDownWaves * kWave) void int4_down_kernel(const Int
         span.view[0] = of_stack(p.w, p, expert);
         span.w[0] = (const uint32_t *)(span.view[0].q + row * p.ldq);
         span.x[0] = (const T *)((const char *)p.x + m * p.ldx);
-        span.n0 = n0, span.N = p.N, span.K = p.K, span.groups = (p.K + p.group - 1) / p.group, span.scale_type = p.scale_type, span.held = &held[wave];
+        span.row[0] = row, span.N = p.N, span.K = p.K, span.groups = (p.K + p.group - 1) / p.group, span.scale_type = p.scale_type, span.held = &held[wave];
         f32x4 acc[1][1];
-        accumulate<T, 1, 1, GROUPS, (GROUPS == 4 ? 1 : 2)>(span, min(part * share, steps), min(steps, part * share + share), acc);
+        accumulate<T, 1, 1, GROUPS, (GROUPS == 4 ? 1 : 2)>(span, steps * part / shares, steps * (part + 1) / shares, acc);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += weight * acc[0][0][e];
     }
@@ -416,7 +429,7 @@ hipError_t launch_int4_down(const Int4Args &p, const float *weights, int type, h
 
 hipError_t launch_int4(const Int4Args &p, int type, bool gated, hipStream_t st)
 {
-    const bool many = p.tiles ? p.tile > kInt4Few : !p.pairs && p.M > kInt4Few && int4_tiles_support(p);
+    const bool many = p.tiles ? p.tile > kInt4Few : !p.pairs && int4_many(p.M, p.N, p.K) && int4_tiles_support(p);
     return many ? launch_int4_tiles(p, type, gated, st) : launch_int4_few(p, type, gated, st);
 }
 

@@ -97,7 +97,9 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
         b[i] = row * (int)p.ldq + pair * 8, of_scale[i] = value * kScale, of_zero[i] = has_zero ? value : 0;
     }
     // Steps in the order that they are taken: one that the contraction ends inside comes first.
-    const int whole = p.K / kDeep, part = p.K % kDeep ? 1 : 0, steps = whole + part;
+    // (parts: of the contraction's whole steps a share, the last one's after an end that is the first's.)
+    const int all = p.K / kDeep, before = all * (int)blockIdx.y / p.parts;
+    const int whole = all * ((int)blockIdx.y + 1) / p.parts - before, part = p.K % kDeep && blockIdx.y == 0 ? 1 : 0, steps = whole + part;
 
     // Two steps' rows are on their way.
     struct Rows {
@@ -107,7 +109,7 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
     };
     Rows held[2];
     auto fetch = [&](int s, Rows &to, auto ends) __attribute__((always_inline)) {
-        const int deep = (decltype(ends)::value ? whole : min(s - part, whole - 1)) * kDeep;      // (behind the last step: that one again)
+        const int deep = (decltype(ends)::value ? all : before + min(s - part, whole - 1)) * kDeep;      // (behind the last step: that one again)
         // weights first: at the tile's begin the tokens' rows are not known yet
         const int g = deep >> shift, back = decltype(ends)::value && shift == 5 && g + (pair >> 1) >= groups ? p.N : 0;
 #pragma unroll
@@ -128,14 +130,8 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
         } else {            // tokens' values there are zeros
 #pragma unroll
             for (int i = 0; i < A; ++i) {
-                uint16_t v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int at = deep + chunk * 8 + e;
-                    v[e] = load_2(x, a[i] - chunk * 16 + min(at, p.K - 1) * 2, 0);
-                    v[e] = at < p.K ? v[e] : 0;
-                }
-                to.a[i] = __builtin_bit_cast(i32x4, v);
+                const T *const row = (const T *)((const char *)p.x + from_x + (a[i] - chunk * 16));
+                to.a[i] = load_end(row, deep + chunk * 8, p.K);
             }
         }
     };
@@ -227,6 +223,14 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
         for (int j = 0; j < 4; ++j) {
             const int at = wm + j * 16 + (lane & 15);
             if (at >= count) continue;
+            if (p.parts > 1) {          // [part][matrix][M][N]
+#pragma unroll
+                for (int k = 0; k < (GATED ? 2 : 1); ++k) {
+                    const float v[4] = {acc[i + k][j][0], acc[i + k][j][1], acc[i + k][j][2], acc[i + k][j][3]};
+                    store_values(p.sums + (((long long)blockIdx.y * (GATED ? 2 : 1) + k) * p.M + m0 + at) * p.N, n, p.N, v);
+                }
+                continue;
+            }
             float out[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -239,6 +243,42 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
     }
 }
 
+// The parts' sums, in order, and what becomes of them.
+template <bool GATED>
+__global__ __launch_bounds__(256) void int4_join_kernel(const Int4Args p, int blocks_n)
+{
+    const long long m = blockIdx.x / (unsigned)blocks_n;
+    const int n = ((int)(blockIdx.x % (unsigned)blocks_n) * 256 + threadIdx.x) * 4;
+    if (n >= p.N) return;
+    float sum[GATED ? 2 : 1][4] = {}, bias[4];
+    constexpr int MATS = GATED ? 2 : 1, U = 4;            // U parts' sums on their way together
+    for (int part = 0; part < p.parts; part += U) {
+        float v[U][MATS][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < MATS; ++k) {
+                const float *const row = p.sums + ((long long)(min(part + u, p.parts - 1) * MATS + k) * p.M + m) * p.N;
+                if (n + 4 <= p.N) __builtin_memcpy(v[u][k], row + n, 16);
+                else load_params(row, n, p.N, 0.f, v[u][k]);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < MATS; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[k][e] += part + u < p.parts ? v[u][k][e] : 0.f;
+    }
+    load_params(p.bias, n, p.N, 0.f, bias);
+    float out[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (GATED) out[e] = gate(p.act, p.out_type != XNOR_TYPE_FP32, sum[0][e]) * sum[1][e];
+        else out[e] = p.bias ? sum[0][e] + bias[e] : sum[0][e];
+    }
+    store_outputs(p, m, n, out);
+}
+
 template <class T, bool GATED, int TM>
 hipError_t tiles(const Int4Args &p, hipStream_t st)
 {
@@ -249,7 +289,7 @@ hipError_t tiles(const Int4Args &p, hipStream_t st)
         Int4Args q = p;
         q.first = m;
         const long long n = std::min(each, all - m) * tiles_n;
-        const dim3 grid((unsigned)((n + 7) / 8 * 8)), block(2 * TM);
+        const dim3 grid((unsigned)((n + 7) / 8 * 8), p.parts), block(2 * TM);
         if (p.scale_type == XNOR_TYPE_FP32) int4_tile_kernel<T, GATED, true, TM><<<grid, block, 0, st>>>(q, tiles_n, n);
         else int4_tile_kernel<T, GATED, false, TM><<<grid, block, 0, st>>>(q, tiles_n, n);
         const hipError_t e = hipGetLastError();
@@ -265,7 +305,12 @@ hipError_t by_tiles(const Int4Args &p, hipStream_t st)
     // larger), but one workgroup a unit, with nothing beside its begin and end (32768 pairs of 64 experts, 2048 x 1024, 473 and 340 us on the larger ones,
     // half of an expert's last tile empty, 461 and 321 on the smaller)
     const bool large = !p.tiles && (p.M + 255) / 256 * ceil_div(p.N, GATED ? 64 : 128) >= compute_units();
-    return large ? tiles<T, GATED, 256>(p, st) : tiles<T, GATED, 128>(p, st);
+    if (large) return tiles<T, GATED, 256>(p, st);
+    hipError_t e = tiles<T, GATED, 128>(p, st);
+    if (e != hipSuccess || p.parts == 1) return e;
+    const int blocks_n = ceil_div(p.N, 1024);
+    int4_join_kernel<GATED><<<dim3((unsigned)(p.M * blocks_n)), dim3(256), 0, st>>>(p, blocks_n);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -283,6 +328,17 @@ int int4_expert_tile(long long pairs, int E)
 {
     const long long each = (pairs + E - 1) / E;
     return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : 128;
+}
+
+// Shares of the contraction for few tiles: a step takes a workgroup 0.75 us, whether it is alone on its unit or not quite.  As many as make a workgroup a unit,
+// of at least four steps, or two a unit where that leaves many steps each; at most 16.  us without and with 2, 4, 8, 16 shares (bf16):
+//     128 x 2048 x 8192  102  -  35.6  -  25.8     128 x 4096 x 4096  54.8  -  25.8  -  30.7     128 x 8192 x 2048  32.4  -  18.9  24.1
+//     192 x 8192 x 8192  113  -  54.9              384 x 8192 x 2048  33.5  35.7                 gated 192 x 8192 x 2048  34.6  39.4
+int int4_tile_parts(long long M, int N, int K, bool gated)
+{
+    if (!int4_many(M, N, K)) return 1;
+    const long long tiles = (M + 127) / 128 * ceil_div(N, gated ? 64 : 128), units = compute_units(), steps = K / kDeep;
+    return (int)std::min<long long>(16, std::max<long long>({1, std::min(units / tiles, steps / 4), std::min(2 * units / tiles, steps / 32)}));
 }
 
 hipError_t launch_int4_tiles(const Int4Args &p, int type, bool gated, hipStream_t st)
