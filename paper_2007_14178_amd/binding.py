@@ -1028,26 +1028,33 @@ def _int4(w: Int4, name: str, cols: int | None = None, count: int | None = None)
                  _dev(zero, torch.uint8, shape, f"{name}.zero") if zero is not None else None, N, K, group, kind)
 
 
-def _int4_rows(like: torch.Tensor, rows: int, cols: int) -> torch.Tensor:
-    """Memory for rows of levels, at multiples of 64 bytes."""
+def _int4_rows(like: torch.Tensor, rows: int, cols: int, count: int | None = None) -> torch.Tensor:
+    """Memory for rows of levels (``count``: of a stack), at multiples of 64 bytes."""
     held = (cols + 7) // 8 * 4
     stride = (held + 63) // 64 * 64
-    return torch.empty_strided((rows, held), (stride, 1), dtype=torch.uint8, device=like.device)
+    if count is None:
+        return torch.empty_strided((rows, held), (stride, 1), dtype=torch.uint8, device=like.device)
+    return torch.empty_strided((count, rows, held), (rows * stride, stride, 1), dtype=torch.uint8, device=like.device)
 
 
 def xnor_int4_quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, scale_dtype: torch.dtype | None = None) -> Int4:
-    """Weights [rows][cols] (fp32, f16, bf16) to 4 bits by row and group of columns; ``zeros``: with a zero point for each group,
-    ``scale_dtype``: w's by default."""
+    """Weights [rows][cols] (fp32, f16, bf16), or a stack of them, to 4 bits by row and group of columns; ``zeros``: with a zero point for each
+    group, ``scale_dtype``: w's by default."""
     kind = _real(w.dtype, "w")
     if group not in (32, 64, 128):
         raise XnorError(E_UNSUPPORTED, f"xnor_int4_quantize: group of {group}")
-    rows, cols, ptr, stride = _rows(w, w.dtype, "w")
-    q = _int4_rows(w, rows, cols)
+    many = w.dim() == 3
+    rows, cols, _, stride = _rows(w[0] if many and w.shape[0] else w.flatten(0, 1) if many else w, w.dtype, "w")
+    lead = (w.shape[0],) if many else ()
+    q = _int4_rows(w, rows, cols, *lead)
     groups = (cols + group - 1) // group
-    scale = torch.empty(groups, rows, dtype=scale_dtype or w.dtype, device=w.device)
-    zero = torch.empty(groups, rows, dtype=torch.uint8, device=w.device) if zeros else None
-    _ok(lib.xnor_int4_quantize(ptr, kind, rows, cols, stride, group, q.data_ptr(), q.stride(0), scale.data_ptr(), _real(scale.dtype, "scale"),
-                               zero.data_ptr() if zeros else None, _stream()), "xnor_int4_quantize")
+    scale = torch.empty(*lead, groups, rows, dtype=scale_dtype or w.dtype, device=w.device)
+    s_kind = _real(scale.dtype, "scale")
+    zero = torch.empty(*lead, groups, rows, dtype=torch.uint8, device=w.device) if zeros else None
+    for e in range(w.shape[0] if many else 1):
+        of = (w[e], q[e], scale[e], zero[e] if zeros else None) if many else (w, q, scale, zero)
+        _ok(lib.xnor_int4_quantize(of[0].data_ptr(), kind, rows, cols, stride, group, of[1].data_ptr(), q.stride(-2), of[2].data_ptr(), s_kind,
+                                   of[3].data_ptr() if zeros else None, _stream()), "xnor_int4_quantize")
     return Int4(q, scale, zero, cols, group)
 
 

@@ -253,3 +253,97 @@ def test_routed_experts_replayed(xb, T):
         torch.cuda.synchronize()
         for out in outs:
             assert all(torch.equal(a, b) for a, b in zip(eager, out))
+
+
+MANY = [(65, 300, 30000), (129, 1100, 2600), (1000, 520, 1100), (8200, 1030, 70), (20000, 260, 130), (40000, 300, 60), (300, 1024, 4096), (90, 1, 5000000)]
+
+
+@pytest.mark.parametrize("M,N,K", MANY, ids=str)
+@pytest.mark.parametrize("dtype,scale_dtype,group,zeros,out_dtype", [(BF16, BF16, 128, False, BF16), (F16, F32, 32, True, F32)], ids=str)
+def test_many_tokens(xb, M, N, K, dtype, scale_dtype, group, zeros, out_dtype):
+    """Products that go to the tiles: whole and in shares of the contraction, of 128 and 256 tokens, of a contraction that ends inside the only step; with
+    the workspace and without one."""
+    x, w = rand(M + N, M, K, dtype=dtype), weights(xb, K, N, K, group, zeros, scale_dtype)
+    bias = rand(5, N) if zeros else None
+    want, bound = xref.linear(x, w, bias, out_dtype, True)
+    got = xb.xnor_int4_linear(x, w, bias, out_dtype=out_dtype)
+    ref.assert_within(got, want, bound, "y")
+    assert torch.equal(got, xb.xnor_int4_linear(x, w, bias, out_dtype=out_dtype))
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    ref.assert_within(xb.xnor_int4_linear(x, w, bias, out_dtype=out_dtype, workspace=none), want, bound, "y without a workspace")
+
+
+@pytest.mark.parametrize("M,F,K", [(70, 520, 9000), (129, 1100, 2600), (700, 555, 1500), (8200, 515, 131)], ids=str)
+@pytest.mark.parametrize("dtype,scale_dtype,group,zeros,act,out_dtype", [(BF16, BF16, 64, True, ref.SILU, BF16), (F16, F16, 128, False, ref.GELU, F32)], ids=str)
+def test_many_tokens_gated(xb, M, F, K, dtype, scale_dtype, group, zeros, act, out_dtype):
+    x = rand(M + F, M, K, dtype=dtype)
+    wg, wu = weights(xb, K, F, K, group, zeros, scale_dtype), weights(xb, K + 1, F, K, group, zeros, scale_dtype)
+    want, bound = xref.gated(x, wg, wu, act, out_dtype, True)
+    ref.assert_within(xb.xnor_int4_gated(x, wg, wu, act, out_dtype=out_dtype), want, bound, "h")
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    ref.assert_within(xb.xnor_int4_gated(x, wg, wu, act, out_dtype=out_dtype, workspace=none), want, bound, "h without a workspace")
+
+
+def test_many_tokens_strides_and_what_is_not_finite(xb):
+    """As test_strides_and_edges and test_values_that_are_not_finite, on the tiles, in shares of the contraction."""
+    M, N, K = 150, 515, 5643
+    assert xb.xnor_int4_linear_workspace_bytes(M, N, K) > 0
+    w = weights(xb, 3, N, K, 32, True, F16)
+    held = torch.as_strided(torch.zeros(N * 2828 + 4, dtype=torch.uint8, device="cuda"), (N, 2824), (2828, 1), 4)
+    held.copy_(w.q)
+    buffer = torch.full((M + 2, N + 5), 7.0, device="cuda")
+    x = rand(1, M, K + 3, dtype=BF16)[:, 3:]
+    x[1, 5], x[2, 6], x[3, K - 1] = float("inf"), float("nan"), float("-inf")
+    got = xb.xnor_int4_linear(x, w._replace(q=held), out=buffer[1:M + 1, 2:N + 2]).cpu().double()
+    clean = x.clone()
+    clean[1, 5], clean[2, 6], clean[3, K - 1] = 0.0, 0.0, 0.0
+    want, bound = xref.linear(clean, w, None, F32, True)
+    v = xref.values(w)[0]
+    want[1] += v[:, 5] * float("inf")
+    want[3] += v[:, K - 1] * float("-inf")
+    want[2] = float("nan")
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+    assert torch.equal(got[got.isinf()] > 0, want[want.isinf()] > 0)
+    fine = torch.isfinite(want)
+    assert ((got - want).abs()[fine] <= bound[fine]).all()
+    buffer[1:M + 1, 2:N + 2] = 7.0
+    assert (buffer == 7.0).all()
+
+
+def test_many_tokens_replayed(xb):
+    """Shares of the contraction in a captured graph, two graphs on one workspace and eager calls in turn."""
+    M, N, K = 200, 1024, 4096
+    x, w, wu = rand(1, M, K, dtype=BF16), weights(xb, 2, N, K, 128, False, BF16), weights(xb, 3, N, K, 128, False, BF16)
+    space = torch.empty(max(xb.xnor_int4_linear_workspace_bytes(M, N, K), xb.xnor_int4_gated_workspace_bytes(M, N, K)), dtype=torch.uint8, device="cuda")
+    assert xb.xnor_int4_linear_workspace_bytes(M, N, K) > 0 and xb.xnor_int4_gated_workspace_bytes(M, N, K) > 0
+    out = [torch.empty(M, N, dtype=BF16, device="cuda") for _ in range(2)]
+    xb.xnor_int4_linear(x, w, workspace=space), xb.xnor_int4_gated(x, w, wu, workspace=space)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    with torch.cuda.graph(graphs[0]):
+        xb.xnor_int4_linear(x, w, out=out[0], workspace=space)
+    with torch.cuda.graph(graphs[1]):
+        xb.xnor_int4_gated(x, w, wu, h=out[1], workspace=space)
+    for seed in range(4, 8):
+        x.copy_(rand(seed, M, K, dtype=BF16))
+        eager = [xb.xnor_int4_linear(x, w), xb.xnor_int4_gated(x, w, wu)]
+        torch.cuda.synchronize()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, out))
+
+
+@pytest.mark.parametrize("T,k,E,K,F,N", [(400, 1, 2, 40, 50, 40), (700, 2, 3, 190, 130, 190), (64, 1, 1, 300, 200, 100), (2, 2, 16, 4000, 40, 600),
+                                         (3, 5, 64, 130, 1000, 7)], ids=str)
+def test_experts_by_tiles_and_pairs(xb, T, k, E, K, F, N):
+    chosen = torch.rand(T, E, generator=torch.Generator().manual_seed(T)).argsort(1)[:, :k].int()
+    share = torch.rand(T, k, generator=torch.Generator().manual_seed(1))
+    chosen[0, 0] = -1
+    wg, wu, wd = stacks(xb, E, K, F, N, 64, True, BF16)
+    x = rand(9, T, K, dtype=BF16)
+    x[T - 1, K // 2] = float("nan")
+    want, bound = xref.experts(x[:T - 1], chosen[:T - 1], share[:T - 1], wg, wu, wd, ref.SILU, F32, T * k > ROUNDED)
+    got = xb.xnor_int4_experts(x, chosen.cuda(), share.cuda(), wg, wu, wd, out_dtype=F32)
+    ref.assert_within(got[:T - 1], want, bound, "y")
+    assert got[T - 1].isnan().all()
