@@ -603,10 +603,11 @@ int xnor_int4_dequantize(const xnor_int4 *w, void *out, int out_type, long long 
  *   x      in   [M][K], type XNOR_TYPE_F16 or _BF16
  *   bias   in   fp32 [N] or NULL
  *   out    out  [M][rows of the weights], out_type any
- * Sums are fp32.  For few tokens (and without a workspace) the products are of levels less their zero point, which the tokens' type holds
- * exactly, and a group's sum is multiplied by its scale; for many a weight is rounded to the tokens' type first, as the matrix instructions take it.
- *   workspace  16-byte aligned, xnor_int4_*_workspace_bytes bytes (host only), or NULL or smaller: then not used; its contents mean nothing
- *              afterwards
+ * Sums are fp32: the products are of tokens and levels less their zero point, which the tokens' type holds exactly, and a group's sum is multiplied by
+ * its scale, so that weights are never rounded.  An infinity or NaN among a token's values, or a scale that is NaN, reaches the outputs that it would in
+ * products of the values.
+ *   workspace  16-byte aligned, xnor_int4_*_workspace_bytes bytes (host only): for sums over shares of the contraction, where tokens and rows are too
+ *              few to fill the GPU; NULL or smaller: then not used.  Its contents mean nothing afterwards
  */
 int xnor_int4_linear_workspace_bytes(long long M, int N, int K, size_t *bytes);
 int xnor_int4_linear(const void *x, int type, long long x_stride, const xnor_int4 *w, const float *bias, long long M, void *out, int out_type,

@@ -1,8 +1,11 @@
-// Products of many tokens with 4-bit weights: 128 tokens x 128 rows of the weights (gated: 64 of each matrix) by four waves of 64 x 64.
+// Products of many tokens with 4-bit weights: 128 or 256 tokens x 128 rows of the weights (gated: 64 of each matrix) by four or eight waves of 64 x 64.
 //
-// Tokens and weights go through registers into LDS, 64 values of a row at a time, the weights as values of the tokens' type: (level - zero) * scale
-// in fp32, rounded once, which is what the matrix instructions take.  A step's rows are on their way while the one before is multiplied, and are
-// turned into values and written to the other half of LDS between its instructions.
+// Tokens and weights go through registers into LDS, 64 values of a row at a time, the weights as levels less their zero point, which the tokens' type
+// holds exactly; a step's sums (of groups of 32: of each half) are multiplied by their scales in fp32 and added.  Two steps' rows are on their way, a step's are
+// turned into operands and written to one half of LDS while the other is multiplied.
+// Bound by the operands' way out of LDS, 64 KB a step of 128 x 128: without those reads 4096 x 8192 x 4096 bf16 takes 185 us of 335, without the conversions 290.
+// 4096 x 8192 x 8192 bf16 650-760 us, 0.73-0.85 PFLOP/s.  With weights rounded to the tokens' type on their way, (level - zero) * scale, there are no scales to
+// multiply by and it takes 560-640, but outputs are up to 1.6 times as far from the exact ones as those of products in fp32.
 #include <algorithm>
 
 #include "int4_common.hpp"
@@ -12,17 +15,21 @@ namespace {
 
 constexpr int kRows = 128, kDeep = 64;       // rows of the weights a tile, values of a step
 
-// The values of a word: level * scale - zero * scale.
-template <class T>
-__device__ inline i32x4 values_of(uint32_t w, float scale, float minus)
+// A word's levels less their zero point, exactly: as f16, or as bf16 times 2^-8 (so that sums of tokens near the largest value stay finite), which the
+// group's scale gets back.
+template <class T> constexpr float kBack = 1.f;
+template <> constexpr float kBack<bf16_t> = 0x1p8f;
+__device__ inline i32x4 operand_of(f16_t, uint32_t w, uint32_t zero) { return Levels<f16_t>::operand<false>(w, Levels<f16_t>::zero(zero)); }
+__device__ inline i32x4 operand_of(bf16_t, uint32_t w, uint32_t zero)
 {
     uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
     // (so that a byte's conversion is one instruction)
     asm("" : "+v"(even));
     asm("" : "+v"(odd));
-    auto at = [&](uint32_t v, int byte) { return (T)__builtin_fmaf((float)(v >> 8 * byte & 255u), scale, minus); };
-    const T to[8] = {at(even, 0), at(even, 2), at(odd, 0), at(odd, 2), at(even, 1), at(even, 3), at(odd, 1), at(odd, 3)};
-    return __builtin_bit_cast(i32x4, to);
+    const float less = (float)zero * -0x1p-8f;
+    auto at = [&](uint32_t v, int byte) { return __float_as_uint(__builtin_fmaf((float)(v >> 8 * byte & 255u), 0x1p-8f, less)); };
+    auto two = [](uint32_t low, uint32_t high) { return (int)__builtin_amdgcn_perm(high, low, 0x07060302u); };        // (small integers: no bits are lost)
+    return i32x4{two(at(even, 0), at(even, 2)), two(at(odd, 0), at(odd, 2)), two(at(even, 1), at(even, 3)), two(at(odd, 1), at(odd, 3))};
 }
 
 // Loads from a buffer: a lane's offset and a scalar one.  (The host's pass does not know the builtins.)
@@ -42,14 +49,15 @@ template <class R> __device__ inline uint16_t load_2(R, int, int) { return 0; }
 template <class R> __device__ inline uint8_t load_1(R, int, int) { return 0; }
 #endif
 
-// WIDE: scales of 32 bits.
-template <class T, bool GATED, bool WIDE, int TM>
+// SHORT: groups of 32, two of them in a step.
+template <class T, bool GATED, bool SHORT, int TM>
 __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, int tiles_n, long long tiles)
 {
     constexpr int TN = GATED ? 64 : 128;        // outputs n of a tile
     constexpr int kThreads = 2 * TM, A = 4, B = 512 / kThreads;         // chunks of the tokens and word pairs of the weights that a thread stages
     typedef Mat<T> Mul;
     __shared__ __align__(16) char lds[2][(TM + kRows) * kStep];
+    __shared__ float by[2][2][kRows];           // a step's scales, of its first and its second 32 values
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     // Workgroups go round the eight XCDs by their index: each takes a run of consecutive tiles, groups of eight tiles of tokens for a tile of the
     // weights' rows, so that what its units work on at a time shares both in its L2.  (Experts: of the tiles that there are.)
@@ -82,7 +90,8 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
     }
     const int words = (p.K + 7) / 8, groups = (p.K + p.group - 1) / p.group, shift = __builtin_ctz(p.group);
     const bool has_zero = view[0].zero != nullptr, half = p.scale_type == XNOR_TYPE_F16;
-    constexpr int kScale = WIDE ? 4 : 2;
+    const bool wide = p.scale_type == XNOR_TYPE_FP32;
+    const int scale_bytes = wide ? 4 : 2;
     // (a lane's matrix: in the gated block that of its row's 16; a wave's rows t / 4 are 16 of one)
     const bool second = GATED && (wave & 1);
     const Int4View &mine = second ? view[1] : view[0];
@@ -93,8 +102,8 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
 #pragma unroll
     for (int i = 0; i < B; ++i) {
         const int r = (t >> 2) + TM / 2 * i, row = min(GATED ? (r >> 5) * 16 + (r & 15) : r, p.N - 1 - n0);
-        const int value = n0 + row + (shift == 5 ? (pair >> 1) * p.N : 0);
-        b[i] = row * (int)p.ldq + pair * 8, of_scale[i] = value * kScale, of_zero[i] = has_zero ? value : 0;
+        const int value = n0 + row + (SHORT ? (pair >> 1) * p.N : 0);
+        b[i] = row * (int)p.ldq + pair * 8, of_scale[i] = value * scale_bytes, of_zero[i] = has_zero ? value : 0;
     }
     // Steps in the order that they are taken: one that the contraction ends inside comes first.
     // (parts: of the contraction's whole steps a share, the last one's after an end that is the first's.)
@@ -105,13 +114,13 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
     struct Rows {
         i32x4 a[A];
         i32x2 b[B];
-        uint32_t scale[B], zero[B];        // as they are loaded: a conversion beside the loads would wait for them
+        uint32_t low[B], high[B], zero[B];        // (halves of a scale, 16-bit ones twice) as they are loaded: a conversion beside the loads would wait for them
     };
     Rows held[2];
     auto fetch = [&](int s, Rows &to, auto ends) __attribute__((always_inline)) {
         const int deep = (decltype(ends)::value ? all : before + min(s - part, whole - 1)) * kDeep;      // (behind the last step: that one again)
         // weights first: at the tile's begin the tokens' rows are not known yet
-        const int g = deep >> shift, back = decltype(ends)::value && shift == 5 && g + (pair >> 1) >= groups ? p.N : 0;
+        const int g = deep >> shift, back = decltype(ends)::value && SHORT && g + (pair >> 1) >= groups ? p.N : 0;
 #pragma unroll
         for (int i = 0; i < B; ++i) {
             if constexpr (!decltype(ends)::value) {
@@ -120,8 +129,8 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
 #pragma unroll
                 for (int j = 0; j < 2; ++j) to.b[i][j] = load_4(q, b[i] - pair * 8 + min(deep / 8 + pair * 2 + j, words - 1) * 4, 0);
             }
-            if constexpr (WIDE) to.scale[i] = load_4(scales, of_scale[i] - back * kScale, g * p.N * kScale);
-            else to.scale[i] = load_2(scales, of_scale[i] - back * kScale, g * p.N * kScale);
+            to.low[i] = load_2(scales, of_scale[i] - back * scale_bytes, g * p.N * scale_bytes);
+            to.high[i] = load_2(scales, of_scale[i] - back * scale_bytes + (wide ? 2 : 0), g * p.N * scale_bytes);
             to.zero[i] = load_1(zeros, has_zero ? of_zero[i] - back : 0, has_zero ? g * p.N : 0);
         }
         if constexpr (!decltype(ends)::value) {
@@ -140,11 +149,12 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
 #pragma unroll
         for (int i = 0; i < B; ++i) {
             const int r = (t >> 2) + TM / 2 * i;
-            const float of_half = (float)__builtin_bit_cast(f16_t, (uint16_t)from.scale[i]);
-            const float by = WIDE ? __uint_as_float(from.scale[i]) : half ? of_half : __uint_as_float(from.scale[i] << 16);
-            const float less = -(has_zero ? (float)(from.zero[i] & 15u) : 8.f) * by;
+            const float of_half = (float)__builtin_bit_cast(f16_t, (uint16_t)from.low[i]);
+            const float scale = half ? of_half : __uint_as_float(wide ? from.high[i] << 16 | from.low[i] : from.low[i] << 16);
+            by[s & 1][pair >> 1][r] = scale * kBack<T>;         // (pairs 0 and 1, 2 and 3 are of one group)
+            const uint32_t zero = has_zero ? from.zero[i] & 15u : 8u;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) *(i32x4 *)(lb + r * kStep + (((pair * 2 + j) ^ (r & 7)) << 4)) = values_of<T>(from.b[i][j], by, less);
+            for (int j = 0; j < 2; ++j) *(i32x4 *)(lb + r * kStep + (((pair * 2 + j) ^ (r & 7)) << 4)) = operand_of(T(), from.b[i][j], zero);
         }
 #pragma unroll
         for (int i = 0; i < A; ++i) {
@@ -173,21 +183,21 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
             // (not for some steps alone: the wait for a step's rows would be one for all that are on their way)
             if constexpr (decltype(more)::value) put(s + 1, rows_of), fetch(s + 3, rows_of, std::false_type{});
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 first = *(const f32x4 *)&by[s & 1][0][wn + i * 16 + (lane >> 4) * 4];
+                const f32x4 then = SHORT ? *(const f32x4 *)&by[s & 1][1][wn + i * 16 + (lane >> 4) * 4] : first;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int j = 0; j < 4; ++j) {
+                    f32x4 sum = Mul::mul(fb[0][i], fa[0][j], f32x4{});
+                    if constexpr (SHORT) {
+                        const f32x4 more = Mul::mul(fb[1][i], fa[1][j], f32x4{});
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = Mul::mul(fb[h][i], fa[h][j], acc[i][j]);
-            // Between the matrix instructions: the second half's operands from LDS, the next step's conversions and their way into LDS, the fetches.
-            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] += first[e] * sum[e] + then[e] * more[e];
+                    } else {
+                        sum = Mul::mul(fb[1][i], fa[1][j], sum);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                if (i < 8) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                if constexpr (decltype(more)::value) {
-                    __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
-                    if (i % 4 == 3) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-                    if (i % 2 == 1 && i >= 8) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+                        for (int e = 0; e < 4; ++e) acc[i][j][e] += first[e] * sum[e];
+                    }
                 }
             }
         } else if constexpr (decltype(more)::value) {
@@ -290,7 +300,7 @@ hipError_t tiles(const Int4Args &p, hipStream_t st)
         q.first = m;
         const long long n = std::min(each, all - m) * tiles_n;
         const dim3 grid((unsigned)((n + 7) / 8 * 8), p.parts), block(2 * TM);
-        if (p.scale_type == XNOR_TYPE_FP32) int4_tile_kernel<T, GATED, true, TM><<<grid, block, 0, st>>>(q, tiles_n, n);
+        if (p.group == 32) int4_tile_kernel<T, GATED, true, TM><<<grid, block, 0, st>>>(q, tiles_n, n);
         else int4_tile_kernel<T, GATED, false, TM><<<grid, block, 0, st>>>(q, tiles_n, n);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

@@ -4,7 +4,7 @@ import math
 
 import torch
 
-from dense_reference import U, UT, _gate, rounding
+from dense_reference import U, _gate, rounding
 
 SOFTMAX, SIGMOID = 0, 1
 
@@ -47,37 +47,31 @@ def values(w):
     return (levels_of(w.q, w.cols).double() - z) * s, s, z
 
 
-def product(x, e_x, w, dtype, rounded):
-    """x w^T and its bound but for the output's rounding.  e_x: x's own.  rounded: the weights are rounded to the tokens' type."""
+def product(x, e_x, w, dtype):
+    """x w^T and its bound but for the output's rounding.  e_x: x's own."""
     v, s, z = values(w)
     x = x.cpu().double()
     y = x @ v.t()
     n = x.shape[1]
     a = x.abs() + e_x
-    if rounded:
-        e = (2 * n * U + 1.01 * UT[dtype] + U) * (a @ v.abs().t())
-        if dtype is torch.float16:
-            e = e + 2.0 ** -25 * a.sum(1, keepdim=True)
-    else:
-        # a group's sum: of levels less zeros, or (bf16) of 16 + level and -(16 + zero), whose sums twice as many terms form; the groups' sums with
-        # their scales behind it
-        most = (v.abs() if dtype is torch.float16 else (levels_of(w.q, w.cols).double() + z + 32.0) * s.abs())
-        depth = 2 * (1 if dtype is torch.float16 else 2) * min(n, w.group) + n / w.group / 8 + 12
-        e = depth * U * (a @ most.t())
-    return y, e + e_x @ v.abs().t()
+    # a group's sum: of levels less zeros, or (bf16) of 16 + level and -(16 + zero), whose sums twice as many terms form; then the groups' sums (of at
+    # least 32 values) with their scales after one another, at most 16 shares of them and 8 waves', a scale's product and the last addition
+    most = (v.abs() if dtype is torch.float16 else (levels_of(w.q, w.cols).double() + z + 32.0) * s.abs())
+    depth = 2 * (1 if dtype is torch.float16 else 2) * min(n, w.group) + n / 32 + 32
+    return y, depth * U * (a @ most.t()) + e_x @ v.abs().t()
 
 
-def linear(x, w, bias, out_dtype, rounded):
-    y, e = product(x, torch.zeros(x.shape).double(), w, x.dtype, rounded)
+def linear(x, w, bias, out_dtype):
+    y, e = product(x, torch.zeros(x.shape).double(), w, x.dtype)
     if bias is not None:
         y = y + bias.cpu().double()
     return y, e + U * y.abs() + rounding(y, out_dtype)
 
 
-def gated(x, wg, wu, act, out_dtype, rounded):
+def gated(x, wg, wu, act, out_dtype):
     none = torch.zeros(x.shape).double()
-    g, e_g = product(x, none, wg, x.dtype, rounded)
-    u, e_u = product(x, none, wu, x.dtype, rounded)
+    g, e_g = product(x, none, wg, x.dtype)
+    u, e_u = product(x, none, wu, x.dtype)
     h, e = _gate(g, u, e_g, e_u, act)
     return h, e + rounding(h, out_dtype)
 
@@ -86,7 +80,7 @@ def one(w, e):
     return type(w)(w.q[e], w.scale[e], None if w.zero is None else w.zero[e], w.cols, w.group)
 
 
-def experts(x, chosen, weights, wg, wu, wd, act, out_dtype, rounded):
+def experts(x, chosen, weights, wg, wu, wd, act, out_dtype):
     T, k = chosen.shape
     E, N = wd.q.shape[0], wd.rows
     y, e_y = torch.zeros(T, N).double(), torch.zeros(T, N).double()
@@ -96,8 +90,8 @@ def experts(x, chosen, weights, wg, wu, wd, act, out_dtype, rounded):
             rows = (chosen[:, s].cpu() == e).nonzero()[:, 0]
             if rows.numel() == 0:
                 continue
-            h, e_h = gated(x[rows.to(x.device)], one(wg, e), one(wu, e), act, x.dtype, rounded)
-            p, e_p = product(h, e_h, one(wd, e), x.dtype, rounded)
+            h, e_h = gated(x[rows.to(x.device)], one(wg, e), one(wu, e), act, x.dtype)
+            p, e_p = product(h, e_h, one(wd, e), x.dtype)
             w = weights[rows, s, None]
             y[rows] += w * p
             e_y[rows] += w.abs() * (e_p + (k + 2) * U * (p.abs() + e_p))

@@ -13,7 +13,6 @@ import experts_reference as xref  # noqa: E402
 pytestmark = pytest.mark.gpu
 
 F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
-ROUNDED = 64        # from so many tokens on a weight may be rounded to the tokens' type
 
 
 @pytest.fixture(scope="module")
@@ -75,7 +74,7 @@ SIZES = [(1, 1, 1), (1, 16, 128), (1, 17, 7), (1, 2050, 4100), (3, 33, 129), (5,
 def test_linear(xb, M, N, K, dtype, scale_dtype, group, zeros, out_dtype):
     x, w = rand(M + N, M, K, dtype=dtype), weights(xb, K, N, K, group, zeros, scale_dtype)
     bias = rand(5, N) if zeros else None
-    want, bound = xref.linear(x, w, bias, out_dtype, M > ROUNDED)
+    want, bound = xref.linear(x, w, bias, out_dtype)
     got = xb.xnor_int4_linear(x, w, bias, out_dtype=out_dtype)
     assert got.dtype is out_dtype
     ref.assert_within(got, want, bound, "y")
@@ -89,7 +88,7 @@ def test_linear(xb, M, N, K, dtype, scale_dtype, group, zeros, out_dtype):
 def test_gated(xb, M, F, K, dtype, scale_dtype, group, zeros, act, out_dtype):
     x = rand(M + F, M, K, dtype=dtype)
     wg, wu = weights(xb, K, F, K, group, zeros, scale_dtype), weights(xb, K + 1, F, K, group, zeros, scale_dtype)
-    want, bound = xref.gated(x, wg, wu, act, out_dtype, M > ROUNDED)
+    want, bound = xref.gated(x, wg, wu, act, out_dtype)
     ref.assert_within(xb.xnor_int4_gated(x, wg, wu, act, out_dtype=out_dtype), want, bound, "h")
 
 
@@ -104,14 +103,14 @@ def test_strides_and_edges(xb, M):
     odd = w._replace(q=held)
     buffer = torch.full((M + 2, N + 5), 7.0, dtype=BF16, device="cuda")
     for x in (rand(1, M, K + 3, dtype=BF16)[:, 3:], rand(2, 1, K, dtype=BF16).expand(M, K)):
-        want, bound = xref.linear(x, w, None, BF16, M > ROUNDED)
+        want, bound = xref.linear(x, w, None, BF16)
         got = xb.xnor_int4_linear(x, odd, out=buffer[1:M + 1, 2:N + 2])
         ref.assert_within(got, want, bound, "y")
         assert torch.equal(got, xb.xnor_int4_linear(x.contiguous(), w))
         edge = buffer.clone()
         edge[1:M + 1, 2:N + 2] = 7.0
         assert (edge == 7.0).all()
-        want, bound = xref.gated(x, w, w, ref.SILU, F32, M > ROUNDED)
+        want, bound = xref.gated(x, w, w, ref.SILU, F32)
         ref.assert_within(xb.xnor_int4_gated(x, odd, odd, out_dtype=F32), want, bound, "h")
 
 
@@ -127,7 +126,7 @@ def test_values_that_are_not_finite(xb, M, dtype):
     clean = x.clone()
     clean[1, 5], clean[2, 6], clean[3, 299] = 0.0, 0.0, 0.0
     well = w._replace(scale=w.scale.nan_to_num(1.0))
-    want, bound = xref.linear(clean, well, None, F32, M > ROUNDED)
+    want, bound = xref.linear(clean, well, None, F32)
     v = xref.values(well)[0]
     want[1] += v[:, 5] * float("inf")
     want[3] += v[:, 299] * float("-inf")
@@ -145,7 +144,7 @@ def test_large_values(xb, M):
     x, w = torch.full((M, K), 2.0 ** 124, dtype=BF16, device="cuda"), weights(xb, 2, N, K, 128, False, BF16)
     x[:, 64:] *= -1.0
     w.scale.fill_(2.0 ** -20)
-    want, bound = xref.linear(x, w, None, F32, M > ROUNDED)
+    want, bound = xref.linear(x, w, None, F32)
     got = xb.xnor_int4_linear(x, w, out_dtype=F32)
     assert torch.isfinite(got).all()
     assert ((got.cpu().double() - want).abs() <= bound * 1.01).all()
@@ -197,7 +196,7 @@ def test_experts(xb, T, k, E, K, F, N, dtype, scale_dtype, group, zeros, act, ou
     share = torch.rand(T, k, generator=g)
     wg, wu, wd = stacks(xb, E, K, F, N, group, zeros, scale_dtype)
     x = rand(9, T, K, dtype=dtype)
-    want, bound = xref.experts(x, chosen, share, wg, wu, wd, act, out_dtype, T * k > ROUNDED)
+    want, bound = xref.experts(x, chosen, share, wg, wu, wd, act, out_dtype)
     got = xb.xnor_int4_experts(x, chosen.cuda(), share.cuda(), wg, wu, wd, act, out_dtype=out_dtype)
     assert got.dtype is out_dtype
     ref.assert_within(got, want, bound, "y")
@@ -265,7 +264,7 @@ def test_many_tokens(xb, M, N, K, dtype, scale_dtype, group, zeros, out_dtype):
     the workspace and without one."""
     x, w = rand(M + N, M, K, dtype=dtype), weights(xb, K, N, K, group, zeros, scale_dtype)
     bias = rand(5, N) if zeros else None
-    want, bound = xref.linear(x, w, bias, out_dtype, True)
+    want, bound = xref.linear(x, w, bias, out_dtype)
     got = xb.xnor_int4_linear(x, w, bias, out_dtype=out_dtype)
     ref.assert_within(got, want, bound, "y")
     assert torch.equal(got, xb.xnor_int4_linear(x, w, bias, out_dtype=out_dtype))
@@ -278,7 +277,7 @@ def test_many_tokens(xb, M, N, K, dtype, scale_dtype, group, zeros, out_dtype):
 def test_many_tokens_gated(xb, M, F, K, dtype, scale_dtype, group, zeros, act, out_dtype):
     x = rand(M + F, M, K, dtype=dtype)
     wg, wu = weights(xb, K, F, K, group, zeros, scale_dtype), weights(xb, K + 1, F, K, group, zeros, scale_dtype)
-    want, bound = xref.gated(x, wg, wu, act, out_dtype, True)
+    want, bound = xref.gated(x, wg, wu, act, out_dtype)
     ref.assert_within(xb.xnor_int4_gated(x, wg, wu, act, out_dtype=out_dtype), want, bound, "h")
     none = torch.empty(0, dtype=torch.uint8, device="cuda")
     ref.assert_within(xb.xnor_int4_gated(x, wg, wu, act, out_dtype=out_dtype, workspace=none), want, bound, "h without a workspace")
@@ -297,7 +296,7 @@ def test_many_tokens_strides_and_what_is_not_finite(xb):
     got = xb.xnor_int4_linear(x, w._replace(q=held), out=buffer[1:M + 1, 2:N + 2]).cpu().double()
     clean = x.clone()
     clean[1, 5], clean[2, 6], clean[3, K - 1] = 0.0, 0.0, 0.0
-    want, bound = xref.linear(clean, w, None, F32, True)
+    want, bound = xref.linear(clean, w, None, F32)
     v = xref.values(w)[0]
     want[1] += v[:, 5] * float("inf")
     want[3] += v[:, K - 1] * float("-inf")
@@ -343,7 +342,7 @@ def test_experts_by_tiles_and_pairs(xb, T, k, E, K, F, N):
     wg, wu, wd = stacks(xb, E, K, F, N, 64, True, BF16)
     x = rand(9, T, K, dtype=BF16)
     x[T - 1, K // 2] = float("nan")
-    want, bound = xref.experts(x[:T - 1], chosen[:T - 1], share[:T - 1], wg, wu, wd, ref.SILU, F32, T * k > ROUNDED)
+    want, bound = xref.experts(x[:T - 1], chosen[:T - 1], share[:T - 1], wg, wu, wd, ref.SILU, F32)
     got = xb.xnor_int4_experts(x, chosen.cuda(), share.cuda(), wg, wu, wd, out_dtype=F32)
     ref.assert_within(got[:T - 1], want, bound, "y")
     assert got[T - 1].isnan().all()
