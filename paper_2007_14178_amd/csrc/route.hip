@@ -1,5 +1,6 @@
 // Routing of tokens to experts: the choice with its weights, the experts' lists, the logits' gradient, and the sum over a token's experts.
 #include <algorithm>
+#include <atomic>
 
 #include "experts_common.hpp"
 
@@ -559,8 +560,15 @@ hipError_t launch_route_lists(const ListArgs &p, hipStream_t st)
     const int runs = (int)std::max<long long>(1, (p.pairs + run - 1) / run);
     const size_t lds = (size_t)kListWaves * p.E * 8 + p.E * 8;
     if (lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&list_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        static std::atomic<bool> raised[64];
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;
+        if (dev < 0 || dev >= 64 || !raised[dev].load(std::memory_order_relaxed)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void *>(&list_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxExperts * (kListWaves * 8 + 8));
+            if (e != hipSuccess) return e;
+            if (dev >= 0 && dev < 64) raised[dev].store(true, std::memory_order_relaxed);
+        }
     }
     if (runs > 1) {
         list_count_kernel<<<dim3(runs), dim3(kListThreads), 0, st>>>(p, run);
