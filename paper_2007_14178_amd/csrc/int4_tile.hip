@@ -341,14 +341,14 @@ int int4_expert_tile(long long pairs, int E)
 }
 
 // Shares of the contraction for few tiles: a step takes a workgroup 0.75 us, whether it is alone on its unit or not quite.  As many as make a workgroup a unit,
-// of at least four steps, or two a unit where that leaves many steps each; at most 16.  us without and with 2, 4, 8, 16 shares (bf16):
+// of at least four steps, or two a unit where that leaves 20 steps each; at most 16.  us without and with 2, 4, 8, 16 shares (bf16):
 //     128 x 2048 x 8192  102  -  35.6  -  25.8     128 x 4096 x 4096  54.8  -  25.8  -  30.7     128 x 8192 x 2048  32.4  -  18.9  24.1
 //     192 x 8192 x 8192  113  -  54.9              384 x 8192 x 2048  33.5  35.7                 gated 192 x 8192 x 2048  34.6  39.4
 int int4_tile_parts(long long M, int N, int K, bool gated)
 {
     if (!int4_many(M, N, K)) return 1;
     const long long tiles = (M + 127) / 128 * ceil_div(N, gated ? 64 : 128), units = compute_units(), steps = K / kDeep;
-    return (int)std::min<long long>(16, std::max<long long>({1, std::min(units / tiles, steps / 4), std::min(2 * units / tiles, steps / 32)}));
+    return (int)std::min<long long>(16, std::max<long long>({1, std::min(units / tiles, steps / 4), std::min(2 * units / tiles, steps / 20)}));
 }
 
 hipError_t launch_int4_tiles(const Int4Args &p, int type, bool gated, hipStream_t st)
