@@ -71,8 +71,12 @@ struct Int4Args {
 // Tiles of more of an expert's tokens than this go to the kernel for many.
 constexpr int kInt4Few = 64;
 // Whether a product goes there: of more than 64 tokens unless that is little work (us on the kernel for few and for many, with its shares of the contraction:
-// 256 x 1024 x 1024 9.1 and 13.9, 128 x 4096 x 4096 22.2 and 25.8, 192 x 4096 x 4096 40.9 and 30.6, 128 x 8192 x 8192 74 and 43).
-inline bool int4_many(long long M, long long N, long long K) { return M > kInt4Few && (M + 63) / 64 * N * K > 1LL << 23; }
+// 256 x 1024 x 1024 9.1 and 13.9, 128 x 4096 x 4096 22.2 and 25.8, 192 x 4096 x 4096 40.9 and 30.6, 128 x 8192 x 8192 74 and 43), and of more than 32 where the
+// contraction is long (40 x 2048 x 8192 25.8 and 20.3, 64 x 2048 x 8192 33.7 and 21.8, gated 64 x 8192 x 8192 72 and 55; 64 x 4096 x 4096 18.8 and 20.4).
+inline bool int4_many(long long M, long long N, long long K)
+{
+    return (M > kInt4Few && (M + 63) / 64 * N * K > 1LL << 23) || (M > kInt4Few / 2 && K >= 8192 && N * K >= 1LL << 23);
+}
 // Whether so few pairs are better taken each by itself, without lists: experts of several are read for each of theirs, from the caches mostly.  us, by
 // lists and by pairs, for tokens to k of E experts, width x hidden (bf16, groups of 128):
 //     8 of 64, 2048 x 1024    1: 21.9 16.2    4: 40.1 35.7    8: 51.3 61.9        2 of 8, 4096 x 2048     1: 18.7 13.4    2: 27.7 22.2    4: 31.9 37.3

@@ -254,7 +254,8 @@ def test_routed_experts_replayed(xb, T):
             assert all(torch.equal(a, b) for a, b in zip(eager, out))
 
 
-MANY = [(65, 300, 30000), (129, 1100, 2600), (1000, 520, 1100), (8200, 1030, 70), (20000, 260, 130), (40000, 300, 60), (300, 1024, 4096), (90, 1, 5000000)]
+MANY = [(65, 300, 30000), (129, 1100, 2600), (1000, 520, 1100), (8200, 1030, 70), (20000, 260, 130), (40000, 300, 60), (300, 1024, 4096), (90, 1, 5000000), (40, 1030, 8200),
+        (33, 2050, 8195)]
 
 
 @pytest.mark.parametrize("M,N,K", MANY, ids=str)
