@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 from dataclasses import dataclass
 from typing import NamedTuple
 
@@ -104,7 +105,7 @@ def _load() -> ctypes.CDLL:
     L.xnor_conv2d_fwd.argtypes = [vp, vp, vp, vp, sp, vp, vp, vp, sz, vp]
     L.xnor_conv2d_fwd_algo.argtypes = [vp, vp, vp, vp, sp, vp, vp, vp, sz, ci, vp]
     ll, cf = ctypes.c_longlong, ctypes.c_float
-    wp = ctypes.POINTER(CInt4)
+    wp = vp         # an xnor_int4: CInt4 by reference, or its bytes
     L.xnor_int4_quantize.argtypes = [vp, ci, ll, ci, ll, ci, vp, ll, vp, ci, vp, vp]
     L.xnor_int4_pack.argtypes = [vp, ll, ci, ll, vp, ll, vp]
     L.xnor_int4_dequantize.argtypes = [wp, vp, ci, ll, vp]
@@ -1003,29 +1004,40 @@ class Int4(NamedTuple):
         return self.q.shape[-2]
 
 
-def _int4(w: Int4, name: str, cols: int | None = None, count: int | None = None) -> CInt4:
-    """The matrix (``count``: stack) as the library takes it, checked."""
+_INT4 = struct.Struct("PqPPiiii")       # CInt4's bytes: made in a third of the time of a ctypes structure
+
+
+def _int4(w: Int4, name: str, cols: int | None = None, count: int | None = None) -> tuple[bytes, int]:
+    """The matrix (``count``: stack) as the library takes it, checked, and its rows."""
     q, scale, zero, K, group = w
-    many = () if count is None else (count,)
     if group not in (32, 64, 128):
         raise XnorError(E_UNSUPPORTED, f"{name}: group of {group}")
     if cols is not None and K != cols:
         raise ValueError(f"{name}: {K} columns, expected {cols}")
-    if q.dim() != 2 + len(many) or q.shape[:-2] != many:
-        raise ValueError(f"{name}.q: shape {tuple(q.shape)}, expected {(*many, 'rows', 'bytes')}")
-    N, held = q.shape[-2:]
+    shape, stride = q.shape, q.stride()
+    if count is None:
+        if len(shape) != 2:
+            raise ValueError(f"{name}.q: shape {tuple(shape)}, expected (rows, bytes)")
+        N, held = shape
+        apart = stride[0] if N > 1 else held            # (one row's stride means nothing)
+        by_scale = ((K + group - 1) // group, N)
+    else:
+        if len(shape) != 3 or shape[0] != count:
+            raise ValueError(f"{name}.q: shape {tuple(shape)}, expected ({count}, rows, bytes)")
+        _, N, held = shape
+        apart = stride[1] if N > 1 else stride[0] if count > 1 else held
+        by_scale = (count, (K + group - 1) // group, N)
     if K < 1 or K > _MOST or N > _MOST:
         raise XnorError(E_SHAPE, f"{name} of {N} x {K}")
     if held != (K + 7) // 8 * 4:
         raise ValueError(f"{name}.q: rows of {held} bytes, {K} columns take {(K + 7) // 8 * 4}")
-    stride = q.stride()
-    apart = stride[-2] if N > 1 else stride[0] if count is not None and count > 1 else held       # (one row's stride means nothing)
     if not q.is_cuda or q.dtype is not torch.uint8 or stride[-1] != 1 or (count is not None and count > 1 and stride[0] != N * apart):
         raise TypeError(f"{name}.q: need GPU rows of torch.uint8, a stack's at one distance, got {q.dtype} on {q.device}, strides {stride}")
-    kind = _real(scale.dtype, f"{name}.scale")
-    shape = (*many, (K + group - 1) // group, N)
-    return CInt4(q.data_ptr(), apart, _dev(scale, scale.dtype, shape, f"{name}.scale"),
-                 _dev(zero, torch.uint8, shape, f"{name}.zero") if zero is not None else None, N, K, group, kind)
+    kind = _TYPES.get(scale.dtype)
+    if kind is None:
+        raise TypeError(f"{name}.scale: need torch.float32, float16 or bfloat16, got {scale.dtype}")
+    return _INT4.pack(q.data_ptr(), apart, _dev(scale, scale.dtype, by_scale, "scale"), 0 if zero is None else _dev(zero, torch.uint8, by_scale, "zero"),
+                      N, K, group, kind), N
 
 
 def _int4_rows(like: torch.Tensor, rows: int, cols: int, count: int | None = None) -> torch.Tensor:
@@ -1070,11 +1082,11 @@ def xnor_int4_pack(levels: torch.Tensor, q: torch.Tensor | None = None) -> torch
 
 def xnor_int4_dequantize(w: Int4, out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """The values [rows][cols] that a matrix of 4-bit weights stands for."""
-    c = _int4(w, "w")
+    c, _ = _int4(w, "w")
     dtype = out.dtype if out is not None else out_dtype
     kind = _real(dtype, "out")
     out, o_ptr, o_stride = _out_rows(out, w.q, dtype, w.rows, w.cols, "out")
-    _ok(lib.xnor_int4_dequantize(ctypes.byref(c), o_ptr, kind, o_stride, _stream()), "xnor_int4_dequantize")
+    _ok(lib.xnor_int4_dequantize(c, o_ptr, kind, o_stride, _stream()), "xnor_int4_dequantize")
     return out
 
 
@@ -1093,14 +1105,13 @@ def xnor_int4_linear(x: torch.Tensor, w: Int4, bias: torch.Tensor | None = None,
     dtype = x.dtype
     x_kind = kind = _real(dtype, "x")
     M, K, x_ptr, x_stride = _rows(x, dtype, "x")
-    c = _int4(w, "w", K)
-    N = c.rows
+    c, N = _int4(w, "w", K)
     if out is not None or out_dtype is not None:
         dtype = out.dtype if out is not None else out_dtype
         kind = _real(dtype, "out")
     out, o_ptr, o_stride = _out_rows(out, x, dtype, M, N, "out")
     workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int4_linear_workspace_bytes(M, N, K))
-    _ok(lib.xnor_int4_linear(x_ptr, x_kind, x_stride, ctypes.byref(c), _dev(bias, torch.float32, (N,), "bias") if bias is not None else None, M,
+    _ok(lib.xnor_int4_linear(x_ptr, x_kind, x_stride, c, _dev(bias, torch.float32, (N,), "bias") if bias is not None else None, M,
                              o_ptr, kind, o_stride, ws, ws_bytes, _stream()), "xnor_int4_linear")
     return out
 
@@ -1120,14 +1131,13 @@ def xnor_int4_gated(x: torch.Tensor, wg: Int4, wu: Int4, act: int = ACT_SILU, h:
     dtype = x.dtype
     x_kind = kind = _real(dtype, "x")
     M, K, x_ptr, x_stride = _rows(x, dtype, "x")
-    cg, cu = _int4(wg, "wg", K), _int4(wu, "wu", K)
-    F = cg.rows
+    (cg, F), (cu, _) = _int4(wg, "wg", K), _int4(wu, "wu", K)
     if h is not None or out_dtype is not None:
         dtype = h.dtype if h is not None else out_dtype
         kind = _real(dtype, "h")
     h, h_ptr, h_stride = _out_rows(h, x, dtype, M, F, "h")
     workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int4_gated_workspace_bytes(M, F, K))
-    _ok(lib.xnor_int4_gated(x_ptr, x_kind, x_stride, ctypes.byref(cg), ctypes.byref(cu), act, M, h_ptr, kind, h_stride, ws, ws_bytes, _stream()),
+    _ok(lib.xnor_int4_gated(x_ptr, x_kind, x_stride, cg, cu, act, M, h_ptr, kind, h_stride, ws, ws_bytes, _stream()),
         "xnor_int4_gated")
     return h
 
@@ -1148,9 +1158,8 @@ def xnor_route_fwd(logits: torch.Tensor, k: int, bias: torch.Tensor | None = Non
     their ``group_top`` best stay; ``renorm``: weights are divided by their sum; ``factor`` multiplies them."""
     kind = _real(logits.dtype, "logits")
     T, E, ptr, stride = _rows(logits, logits.dtype, "logits")
-    _counted("xnor_route_fwd", k, groups, groups_kept, group_top, T * max(k, 0))
-    if not 0 < k <= 32:
-        raise XnorError(E_SHAPE, f"xnor_route_fwd: {k} experts a token")
+    if not 0 < k <= 32 or T * k > _MOST or groups > _MOST or groups_kept > _MOST or group_top > _MOST:
+        raise XnorError(E_SHAPE, f"xnor_route_fwd: {k} experts for each of {T} tokens")
     experts, e_ptr = _slots(experts, logits, torch.int32, T, k, "experts")
     weights, w_ptr = _slots(weights, logits, torch.float32, T, k, "weights")
     _ok(lib.xnor_route_fwd(ptr, kind, T, E, stride, _dev(bias, torch.float32, (E,), "bias") if bias is not None else None, score, groups, groups_kept,
@@ -1217,15 +1226,14 @@ def xnor_int4_experts(x: torch.Tensor, experts: torch.Tensor, weights: torch.Ten
     if experts.dim() != 2 or experts.shape[0] != T:
         raise ValueError(f"experts: shape {tuple(experts.shape)}, expected {(T, 'k')}")
     k, E = experts.shape[1], wg.q.shape[0]
-    cg, cu = _int4(wg, "wg", K, E), _int4(wu, "wu", K, E)
-    cd = _int4(wd, "wd", cg.rows, E)
-    N = cd.rows
+    (cg, F), (cu, _) = _int4(wg, "wg", K, E), _int4(wu, "wu", K, E)
+    cd, N = _int4(wd, "wd", F, E)
     if out is not None or out_dtype is not None:
         dtype = out.dtype if out is not None else out_dtype
         kind = _real(dtype, "out")
     out, o_ptr, o_stride = _out_rows(out, x, dtype, T, N, "out")
-    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int4_experts_workspace_bytes(T, k, E, K, cg.rows, N))
+    workspace, ws, ws_bytes = _workspace(workspace, x, xnor_int4_experts_workspace_bytes(T, k, E, K, F, N))
     _ok(lib.xnor_int4_experts(x_ptr, x_kind, x_stride, T, _dev(experts, torch.int32, (T, k), "experts"), _dev(weights, torch.float32, (T, k), "weights"), k,
-                              E, ctypes.byref(cg), ctypes.byref(cu), ctypes.byref(cd), act, o_ptr, kind, o_stride, ws, ws_bytes, _stream()),
+                              E, cg, cu, cd, act, o_ptr, kind, o_stride, ws, ws_bytes, _stream()),
         "xnor_int4_experts")
     return out
