@@ -71,7 +71,7 @@ struct Int4Args {
 // Tiles of more of an expert's tokens than this go to the kernel for many.
 constexpr int kInt4Few = 64;
 // Whether a product goes there: of more than 64 tokens unless that is little work (us on the kernel for few and for many, with its shares of the contraction:
-// 256 x 1024 x 1024 9.1 and 13.9, 128 x 4096 x 4096 22.2 and 25.8, 192 x 4096 x 4096 40.9 and 30.6, 128 x 8192 x 8192 74 and 43), and of more than 32 where the
+// 256 x 1024 x 1024 9.1 and 13.9, 128 x 4096 x 4096 22.2 and 27.1, 192 x 4096 x 4096 40.9 and 32.9, 128 x 8192 x 8192 74 and 48), and of more than 32 where the
 // contraction is long (40 x 2048 x 8192 25.8 and 20.3, 64 x 2048 x 8192 33.7 and 21.8, gated 64 x 8192 x 8192 72 and 55; 64 x 4096 x 4096 18.8 and 20.4).
 inline bool int4_many(long long M, long long N, long long K)
 {

@@ -311,9 +311,9 @@ hipError_t tiles(const Int4Args &p, hipStream_t st)
 template <class T, bool GATED>
 hipError_t by_tiles(const Int4Args &p, hipStream_t st)
 {
-    // the larger tile where there is one for each unit: half the conversions for a product (4096 x 8192 x 8192 bf16 748 us on the smaller, 618 on the
-    // larger), but one workgroup a unit, with nothing beside its begin and end (32768 pairs of 64 experts, 2048 x 1024, 473 and 340 us on the larger ones,
-    // half of an expert's last tile empty, 461 and 321 on the smaller)
+    // the larger tile where there is one for each unit: half the conversions for a product (4096 x 8192 x 8192 bf16 a fifth more on the smaller than on
+    // the larger), but one workgroup a unit, with nothing beside its begin and end (32768 pairs of 64 experts, 2048 x 1024, 976 and 982 us in all on
+    // the smaller and the larger ones, of 8 experts with 1024 pairs each 252 and 267)
     const bool large = !p.tiles && (p.M + 255) / 256 * ceil_div(p.N, GATED ? 64 : 128) >= compute_units();
     if (large) return tiles<T, GATED, 256>(p, st);
     hipError_t e = tiles<T, GATED, 128>(p, st);
@@ -341,7 +341,8 @@ int int4_expert_tile(long long pairs, int E)
 }
 
 // Shares of the contraction for few tiles: a step takes a workgroup 0.75 us, whether it is alone on its unit or not quite.  As many as make a workgroup a unit,
-// of at least four steps, or two a unit where that leaves 20 steps each; at most 16.  us without and with 2, 4, 8, 16 shares (bf16):
+// of at least four steps, or two a unit where that leaves 20 steps each; at most 16.  us without and with 2, 4, 8, 16 shares (bf16, all
+// 10 to 20 % more since the scales went to the sums):
 //     128 x 2048 x 8192  102  -  35.6  -  25.8     128 x 4096 x 4096  54.8  -  25.8  -  30.7     128 x 8192 x 2048  32.4  -  18.9  24.1
 //     192 x 8192 x 8192  113  -  54.9              384 x 8192 x 2048  33.5  35.7                 gated 192 x 8192 x 2048  34.6  39.4
 int int4_tile_parts(long long M, int N, int K, bool gated)

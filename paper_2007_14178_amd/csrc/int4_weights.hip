@@ -1,4 +1,5 @@
-// Real weights to levels of 4 bits and back: read once, written once.
+// Real weights to levels of 4 bits and back: read once, written once, eight values a lane.  (8192 x 8192 bf16: 69 us to levels, 30 to 39 back, 40 for levels that
+// are there; what a program does once.)
 #include "experts_common.hpp"
 
 namespace xnor {
@@ -26,6 +27,23 @@ struct Min {
 
 __device__ inline float as_type(float v, int type) { return type == XNOR_TYPE_FP32 ? v : type == XNOR_TYPE_F16 ? (float)(f16_t)v : (float)(bf16_t)v; }
 
+// Eight values of a row of n from `at` on, zeros behind its end.
+__device__ inline void load_eight(const void *p, long long row, int at, int n, int type, float (&to)[8])
+{
+    if (type == XNOR_TYPE_FP32) load_params((const float *)p + row, at, n, 0.f, to);
+    else if (type == XNOR_TYPE_F16) load_params((const f16_t *)p + row, at, n, 0.f, to);
+    else load_params((const bf16_t *)p + row, at, n, 0.f, to);
+}
+
+template <class T>
+__device__ inline void store_eight(void *p, long long row, int at, int n, const float (&v)[8])
+{
+    T to[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) to[i] = (T)v[i];
+    store_values((T *)p + row, at, n, to);
+}
+
 // A lane makes one word, eight values; the lanes of a group are neighbours.
 __global__ __launch_bounds__(kThreads) void int4_quantize_kernel(const Int4Make p, int w_type, long long first)
 {
@@ -33,11 +51,11 @@ __global__ __launch_bounds__(kThreads) void int4_quantize_kernel(const Int4Make 
     const int words = (p.cols + 7) / 8, lanes = p.group / 8, words_up = (words + lanes - 1) / lanes * lanes;
     for (int at = threadIdx.x; at < words_up; at += kThreads) {
         float v[8];
+        load_eight(p.from, row * p.stride, at * 8, p.cols, w_type, v);
         float top = 0.f, low = 0.f, high = 0.f;
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            v[i] = at * 8 + i < p.cols ? load_real(p.from, row * p.stride + at * 8 + i, w_type) : 0.f;
             bad |= !(fabsf(v[i]) <= 3.402823466e38f);
             low = fminf(low, v[i]), high = fmaxf(high, v[i]);
         }
@@ -85,10 +103,12 @@ __global__ __launch_bounds__(kThreads) void int4_dequantize_kernel(const Int4Mak
         const uint32_t word = *(const uint32_t *)(p.q + row * p.q_stride + at * 4);
         const long long g = (long long)(at * 8 / p.group) * p.rows + row;
         const float scale = load_real(p.scale, g, p.scale_type), zero = p.zero ? (float)(p.zero[g] & 15) : 8.f;
+        float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (at * 8 + i < p.cols)
-                store_real(p.out, row * p.stride + at * 8 + i, p.out_type, ((float)(word >> (4 * (i >> 1) + 16 * (i & 1)) & 15u) - zero) * scale);
+        for (int i = 0; i < 8; ++i) v[i] = ((float)(word >> (4 * (i >> 1) + 16 * (i & 1)) & 15u) - zero) * scale;
+        if (p.out_type == XNOR_TYPE_FP32) store_eight<float>(p.out, row * p.stride, at * 8, p.cols, v);
+        else if (p.out_type == XNOR_TYPE_F16) store_eight<f16_t>(p.out, row * p.stride, at * 8, p.cols, v);
+        else store_eight<bf16_t>(p.out, row * p.stride, at * 8, p.cols, v);
     }
 }
 
