@@ -314,9 +314,8 @@ hipError_t by_tiles(const Int4Args &p, hipStream_t st)
     // the larger tile where there is one for each unit: half the conversions for a product (4096 x 8192 x 8192 bf16 a fifth more on the smaller than on
     // the larger), but one workgroup a unit, with nothing beside its begin and end (32768 pairs of 64 experts, 2048 x 1024, 976 and 982 us in all on
     // the smaller and the larger ones, of 8 experts with 1024 pairs each 252 and 267)
-    const bool large = !p.tiles && (p.M + 255) / 256 * ceil_div(p.N, GATED ? 64 : 128) >= compute_units();
-    if (large) return tiles<T, GATED, 256>(p, st);
-    hipError_t e = tiles<T, GATED, 128>(p, st);
+    const bool large = !p.tiles && p.parts == 1 && p.M > 128 && (p.M + 255) / 256 * ceil_div(p.N, GATED ? 64 : 128) >= compute_units();
+    const hipError_t e = large ? tiles<T, GATED, 256>(p, st) : tiles<T, GATED, 128>(p, st);
     if (e != hipSuccess || p.parts == 1) return e;
     const int blocks_n = ceil_div(p.N, 1024);
     int4_join_kernel<GATED><<<dim3((unsigned)(p.M * blocks_n)), dim3(256), 0, st>>>(p, blocks_n);

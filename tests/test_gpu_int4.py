@@ -347,3 +347,19 @@ def test_experts_by_tiles_and_pairs(xb, T, k, E, K, F, N):
     got = xb.xnor_int4_experts(x, chosen.cuda(), share.cuda(), wg, wu, wd, out_dtype=F32)
     ref.assert_within(got[:T - 1], want, bound, "y")
     assert got[T - 1].isnan().all()
+
+
+@pytest.mark.parametrize("M,gated", [(100, False), (128, True), (250, False), (130, True)])
+def test_as_many_tiles_as_units(xb, M, gated):
+    """Wide layers whose tiles of 128 tokens are as many as the units or half of those, in shares of the contraction all the same."""
+    N, K = (16384 if gated else 32768) // (1 if M <= 128 else 2), 2560
+    ask = xb.xnor_int4_gated_workspace_bytes if gated else xb.xnor_int4_linear_workspace_bytes
+    assert ask(M, N, K) > 0
+    x, w, wu = rand(1, M, K, dtype=BF16), weights(xb, 2, N, K, 128, False, BF16), weights(xb, 3, N, K, 128, False, BF16)
+    out = torch.full((M, N), float("nan"), dtype=F32, device="cuda")
+    got = xb.xnor_int4_gated(x, w, wu, h=out) if gated else xb.xnor_int4_linear(x, w, out=out)
+    assert torch.isfinite(got).all()
+    for part in (slice(0, 150), slice(N - 150, N)):
+        of = [m._replace(q=m.q[part], scale=m.scale[:, part].contiguous()) for m in (w, wu)]
+        want, bound = xref.gated(x, *of, ref.SILU, F32) if gated else xref.linear(x, of[0], None, F32)
+        ref.assert_within(got[:, part], want, bound, "rows")
