@@ -229,8 +229,8 @@ __device__ inline void accumulate(const Span<T, MATS, TT> &p, int from, int to, 
 // The first of a workgroup's `rows` rows: the last workgroup's are the matrix's last ones, some of them another's too, which come out alike.
 __device__ inline int first_row(int block, int rows, int N) { return max(0, min(block * rows, N - rows)); }
 
-// TT: tiles of 16 tokens.  GROUPS: of a step.  MATS: 2: the gated block's matrices, or two times 16 rows of one (more than 16 tokens, whose values
-// are most of what is read: 64 x 4096 x 4096 20 us by 16 rows).
+// TT: tiles of 16 tokens.  GROUPS: of a step.  MATS: 2: the gated block's matrices, or two times 16 rows of one, which share the tokens' values (from
+// five tokens on these are most of what is read).
 template <class T, bool GATED, int TT, int GROUPS, int WAVES, int MATS>
 __global__ __launch_bounds__(WAVES * kWave, TT == 1 ? 4 : 2) void int4_few_kernel(const Int4Args p)
 {
