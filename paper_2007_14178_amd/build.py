@@ -5,6 +5,8 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -18,10 +20,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fno
          "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
 
 
-def build(verbose: bool = False, extra: list[str] | None = None) -> str:
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [hipcc, *FLAGS, *(extra or []), "-o", tmp, *SOURCES]
+def _run(cmd: list[str], verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -32,6 +31,19 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> str:
         print("\n".join(log), flush=True)
     if proc.returncode != 0:
         raise RuntimeError(f"hipcc failed with exit code {proc.returncode}")
+
+
+def build(verbose: bool = False, extra: list[str] | None = None) -> str:
+    """Compiles the sources side by side (one after the other they take nine minutes) and links them."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    tmp = LIB + f".tmp{os.getpid()}"
+    jobs = int(os.environ.get("MAX_JOBS", 0)) or min(8, os.cpu_count() or 1)
+    with tempfile.TemporaryDirectory() as place, ThreadPoolExecutor(jobs) as pool:
+        objects = [os.path.join(place, os.path.basename(src) + ".o") for src in SOURCES]
+        compile_flags = [f for f in FLAGS if f != "-shared"]
+        for done in [pool.submit(_run, [hipcc, *compile_flags, *(extra or []), "-c", "-o", obj, src], verbose) for src, obj in zip(SOURCES, objects)]:
+            done.result()
+        _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objects], verbose)
     os.replace(tmp, LIB)
     return LIB
 
