@@ -6,17 +6,17 @@
 
 namespace xnor {
 
-// (a & mask) | set as one instruction: of its operands only one can be a scalar, so that the compiler, which keeps both constants in scalars, makes two.
+// (a & MASK) | SET as one instruction: of its operands only one can be a scalar, so that the compiler, which keeps both constants in scalars, makes two unless one
+// of them is hidden from it.  (Not an instruction written as asm: the compiler does not see what that writes, and leaves no wait before it where a matrix
+// instruction in flight still has to write or read the same registers.)
 template <uint32_t MASK, uint32_t SET>
 __device__ inline uint32_t and_or(uint32_t a)
 {
+    uint32_t set = SET;
 #ifdef __HIP_DEVICE_COMPILE__
-    uint32_t to;
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(to) : "v"(a), "s"(MASK), "v"(SET));
-    return to;
-#else
-    return (a & MASK) | SET;
+    asm("" : "+v"(set));
 #endif
+    return (a & MASK) | set;
 }
 
 // Eight values of a word as the operand's four registers: register j holds the values 2 j and 2 j + 1, as f16 or bf16.
