@@ -655,8 +655,8 @@ int xnor_route_bwd(const float *dweights, const void *logits, int type, long lon
 /*
  * The chosen experts' gated blocks on 4-bit weights:
  *     out[t] = sum_s weights[t][s] * ((act(x[t] wg_e^T) * (x[t] wu_e^T)) wd_e^T),  e = experts[t][s]
- * added in fp32 in an order that depends on the sizes alone; the gated blocks' outputs are rounded to the tokens' type, as the matrix instructions take them.  Slots whose
- * expert is outside 0 .. E-1 add weight * 0 (so that the weights NaN of a token that could not be routed are seen).
+ * added in fp32 in an order that depends on the sizes alone.  The gated blocks' outputs, formed in fp32, reach the second product as sums of bf16 values: of
+ * two for 16-bit outputs (16 bits of a value, over fp32's range), of three for fp32 ones (24 bits).  Slots whose expert is outside 0 .. E-1 add weight * 0 (so that the weights NaN of a token that could not be routed are seen).
  *   x        in   [T][K], type XNOR_TYPE_F16 or _BF16
  *   experts, weights   in   int32, fp32 [T][k], k <= 32, T k < 2^31
  *   wg, wu   in   stacks of E matrices [F][K], as for xnor_int4_gated       wd  in  a stack of E matrices [N][F]; E <= 1024

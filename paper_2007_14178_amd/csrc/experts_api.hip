@@ -80,7 +80,7 @@ ExpertParts expert_parts(long long T, int k, int E, int F, int N)
     to.lists = part(route_lists_workspace(pairs, E));
     to.tile = int4_expert_tile(pairs, E);
     to.tiles = part((size_t)(1 + most_tiles(pairs, E, std::min(to.tile, kInt4Few))) * sizeof(ExpertTile));
-    to.hidden = part((size_t)pairs * F * 2);
+    to.hidden = part((size_t)pairs * hidden_stride(F) * kMostTerms * 2);
     to.pairs = part((size_t)pairs * N * 4);
     to.bytes = at;
     return to;
@@ -259,30 +259,33 @@ int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, 
     if (workspace_bytes < at.bytes) return XNOR_E_WORKSPACE;
     char *const held = (char *)workspace;
     const hipStream_t st = (hipStream_t)stream;
+    // hidden rows: of bf16 terms
+    const int terms = hidden_terms(out_type);
+    const long long ldh = (long long)terms * hidden_stride(F);
 
     if (int4_pairs_pay(T * k, E)) {
         // hidden: rows by pair
-        Int4Args a = args_of(x, 2 * x_stride, wg, wu, T * k, held + at.hidden, type, F);
-        a.act = act, a.pairs = experts, a.E = E, a.chosen = k;
+        Int4Args a = args_of(x, 2 * x_stride, wg, wu, T * k, held + at.hidden, out_type, ldh);
+        a.act = act, a.pairs = experts, a.E = E, a.chosen = k, a.out_terms = terms;
         const hipError_t e = launch_int4(a, type, true, st);
         if (e != hipSuccess) return hip_status(e);
-        Int4Args b = args_of(held + at.hidden, 2LL * F, wd, nullptr, T, out, out_type, out_stride);
-        b.pairs = experts, b.E = E, b.chosen = k;
-        return hip_status(launch_int4_down(b, weights, type, st));
+        Int4Args b = args_of(held + at.hidden, 2 * ldh, wd, nullptr, T, out, out_type, out_stride);
+        b.pairs = experts, b.E = E, b.chosen = k, b.terms = terms;
+        return hip_status(launch_int4_down(b, weights, st));
     }
     ListArgs l{};
     l.experts = experts, l.pairs = T * k, l.E = E, l.offsets = (int32_t *)(held + at.offsets), l.order = (int32_t *)(held + at.order);
     l.counts = (int32_t *)(held + at.lists), l.tiles = (ExpertTile *)(held + at.tiles);
     // hidden: rows by sorted position; pairs: rows by token and slot
-    Int4Args a = args_of(x, 2 * x_stride, wg, wu, T * k, held + at.hidden, type, F);
-    a.act = act, a.tiles = l.tiles, a.order_x = l.order, a.E = E, a.chosen = k;
-    Int4Args b = args_of(held + at.hidden, 2LL * F, wd, nullptr, T * k, held + at.pairs, XNOR_TYPE_FP32, N);
-    b.tiles = l.tiles, b.order_out = l.order, b.E = E, b.chosen = k;
+    Int4Args a = args_of(x, 2 * x_stride, wg, wu, T * k, held + at.hidden, out_type, ldh);
+    a.act = act, a.tiles = l.tiles, a.order_x = l.order, a.E = E, a.chosen = k, a.out_terms = terms;
+    Int4Args b = args_of(held + at.hidden, 2 * ldh, wd, nullptr, T * k, held + at.pairs, XNOR_TYPE_FP32, N);
+    b.tiles = l.tiles, b.order_out = l.order, b.E = E, b.chosen = k, b.terms = terms;
     if (!int4_tiles_support(a) || !int4_tiles_support(b)) at.tile = std::min(at.tile, kInt4Few);
     l.tile = a.tile = b.tile = at.tile;
     hipError_t e = launch_route_lists(l, st);
     if (e == hipSuccess) e = launch_int4(a, type, true, st);
-    if (e == hipSuccess) e = launch_int4(b, type, false, st);
+    if (e == hipSuccess) e = launch_int4(b, XNOR_TYPE_BF16, false, st);
     if (e != hipSuccess) return hip_status(e);
     CombineArgs c{};
     c.pairs = (const float *)(held + at.pairs), c.experts = experts, c.weights = weights, c.T = T, c.ldo = out_stride, c.k = k, c.E = E, c.N = N;

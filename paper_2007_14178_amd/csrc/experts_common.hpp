@@ -64,10 +64,21 @@ struct Int4Args {
     const int32_t *order_x, *order_out;
     const int32_t *pairs;       // experts' pairs, each by itself (tiles NULL): row m is that of expert pairs[m], x's row m / chosen
     int E, chosen;
+    int terms;                  // > 0: x's rows are so many rows of bf16 each, hidden_stride(K) values from one another, whose sum is the token
+    int out_terms;              // > 0 (gated): outputs are left as such rows; out_type is then that of what is computed from them
+    int cuts;                   // (terms; set by the launchers: workgroups for a tile's pairs)
     int parts;                  // > 1: shares of the contraction, their sums fp32 [parts][matrices][M][N] in `sums`, joined by a second launch
     float *sums;
     long long first;            // (set by the launchers: the launch's first tile of tokens)
 };
+// Between the experts' two products a value is held as the sum of bf16 ones: two hold 16 bits of it (outputs in 16 bits are then as far from the definition as
+// those of products in fp32; rounded to the tokens' type they are 1.35 to 1.5 times as far), three the 24 of fp32, for outputs in fp32.  bf16 for f16 tokens
+// too: a block's outputs may pass f16's largest value.  (4096 tokens to 8 of 64 experts, 2048 x 1024, bf16: 1076 us, with hidden values in bf16 837; 24 tokens to 3 of 30
+// 37.9 and 32.8, one token to 8 of 64 18.9 and 17.2.)
+constexpr int kMostTerms = 3;
+inline int hidden_terms(int out_type) { return out_type == XNOR_TYPE_FP32 ? 3 : 2; }
+__host__ __device__ inline int hidden_stride(int F) { return (F + 7) / 8 * 8; }
+
 // Tiles of more of an expert's tokens than this go to the kernel for many.
 constexpr int kInt4Few = 64;
 // Whether a product goes there: of more than 64 tokens unless that is little work (us on the kernel for few and for many, with its shares of the contraction:
@@ -83,7 +94,7 @@ inline bool int4_many(long long M, long long N, long long K)
 //     8 of 128, 2048 x 512    1: 17.8 10.6    8: 43.7 37.9   16: 60.4 67.4        4 of 32, 1024 x 768     4: 18.4 11.9    8: 23.7 19.3   16: 26.7 32.9
 inline bool int4_pairs_pay(long long pairs, int E) { return pairs <= 4 || 4 * pairs <= 3LL * E; }
 // A token's chosen experts' second products and their sum in one launch: x holds the rows of the pairs, weights their shares, M the tokens.
-hipError_t launch_int4_down(const Int4Args &p, const float *weights, int type, hipStream_t st);
+hipError_t launch_int4_down(const Int4Args &p, const float *weights, hipStream_t st);
 // GATED: w and w2 with the activation.
 hipError_t launch_int4_few(const Int4Args &p, int type, bool gated, hipStream_t st);
 bool int4_tiles_support(const Int4Args &p);

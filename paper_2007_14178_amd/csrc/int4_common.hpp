@@ -132,6 +132,28 @@ __device__ inline void store_outputs(const Int4Args &p, long long m, int n, cons
     }
 }
 
+// Values n .. n + 3 of row m as the sums of p.out_terms bf16 ones, the largest first.  An infinity or a NaN is the first term, and the others are 0; a
+// finite value that would round past the largest is cut instead.
+__device__ inline void store_terms(const Int4Args &p, long long m, int n, const float (&v)[4])
+{
+    float rest[4] = {v[0], v[1], v[2], v[3]};
+    bf16_t *const to = (bf16_t *)p.out + m * p.ldo;
+    const int apart = hidden_stride(p.N);
+#pragma unroll
+    for (int t = 0; t < kMostTerms; ++t) {
+        if (t >= p.out_terms) break;
+        bf16_t term[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool finite = fabsf(rest[e]) <= 3.402823466e38f;
+            term[e] = (bf16_t)rest[e];
+            if (finite && !(fabsf((float)term[e]) <= 3.402823466e38f)) term[e] = (bf16_t)__uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+            rest[e] = finite ? rest[e] - (float)term[e] : 0.f;
+        }
+        store_values(to + t * apart, n, p.N, term);
+    }
+}
+
 // Matrix e of a stack.
 __device__ inline Int4View of_stack(const Int4View &w, const Int4Args &p, int e)
 {

@@ -236,6 +236,9 @@ __global__ __launch_bounds__(WAVES * kWave, TT == 1 ? 4 : 2) void int4_few_kerne
 {
     static_assert(!GATED || MATS == 2, "");
     constexpr int ROWS = GATED ? 16 : 16 * MATS;
+    // Tokens in terms: the tiles of 16 columns hold one term after the other of `own` tiles of tokens (of three terms in four, the last one's twice).
+    constexpr bool TERMS = !GATED && TT > 1 && std::is_same<T, bf16_t>::value;
+    const int own = !TERMS || p.terms == 0 ? TT : p.terms == 2 ? TT / 2 : 1;
     __shared__ f32x4 sums[WAVES][MATS][TT][kWave];
     __shared__ Held held[WAVES][MATS];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = lane & 15, g = lane >> 4;
@@ -252,9 +255,18 @@ __global__ __launch_bounds__(WAVES * kWave, TT == 1 ? 4 : 2) void int4_few_kerne
         expert = p.pairs[m0];
         if (expert < 0 || expert >= p.E) return;
     } else if (p.tiles) {
-        if (p.first + blockIdx.y >= p.tiles[0].count) return;
-        const ExpertTile tile = p.tiles[1 + p.first + blockIdx.y];
-        m0 = tile.first, count = tile.count, expert = tile.expert;
+        const long long at = p.first + blockIdx.y;
+        if constexpr (TERMS) {
+            const int cut = (int)(at % p.cuts) * 16 * own;
+            if (at / p.cuts >= p.tiles[0].count) return;
+            const ExpertTile tile = p.tiles[1 + at / p.cuts];
+            m0 = tile.first + cut, count = min(tile.count - cut, 16 * own), expert = tile.expert;
+            if (count <= 0) return;
+        } else {
+            if (at >= p.tiles[0].count) return;
+            const ExpertTile tile = p.tiles[1 + at];
+            m0 = tile.first, count = tile.count, expert = tile.expert;
+        }
     }
 #pragma unroll
     for (int k = 0; k < MATS; ++k) {
@@ -264,15 +276,26 @@ __global__ __launch_bounds__(WAVES * kWave, TT == 1 ? 4 : 2) void int4_few_kerne
     }
 #pragma unroll
     for (int j = 0; j < TT; ++j) {
-        const long long m = m0 + min(j * 16 + r, count - 1);
+        const long long m = m0 + min((TERMS ? j & (own - 1) : j) * 16 + r, count - 1);
         const long long from = p.pairs ? m / p.chosen : p.order_x ? p.order_x[m] / p.chosen : m;
-        span.x[j] = (const T *)((const char *)p.x + from * p.ldx);
+        span.x[j] = (const T *)((const char *)p.x + from * p.ldx) + (TERMS && p.terms ? (long long)min(j / own, p.terms - 1) * hidden_stride(p.K) : 0);
     }
     span.N = p.N, span.K = p.K, span.groups = (p.K + p.group - 1) / p.group, span.scale_type = p.scale_type, span.held = held[wave];
 
     const int steps = (p.K + kValues - 1) / kValues;
     f32x4 acc[MATS][TT];
     accumulate<T, MATS, TT, GROUPS, (MATS == 2 || TT > 1 || GROUPS == 4 ? 1 : 2)>(span, steps * wave / WAVES, steps * (wave + 1) / WAVES, acc);
+    if constexpr (TERMS) {
+#pragma unroll
+        for (int k = 0; k < MATS; ++k) {
+            if (p.terms == 2) {
+#pragma unroll
+                for (int j = 0; j < TT / 2; ++j) acc[k][j] += acc[k][j + TT / 2];
+            } else if (TT == 4 && p.terms == 3) {
+                acc[k][0] += acc[k][1] + acc[k][TT / 2];
+            }
+        }
+    }
 #pragma unroll
     for (int k = 0; k < MATS; ++k)
 #pragma unroll
@@ -300,7 +323,8 @@ __global__ __launch_bounds__(WAVES * kWave, TT == 1 ? 4 : 2) void int4_few_kerne
                 if constexpr (GATED) out[e] = gate(p.act, p.out_type != XNOR_TYPE_FP32, v[0][e]) * v[1][e];
                 else out[e] = p.bias ? v[k][e] + bias[e] : v[k][e];
             }
-            store_outputs(p, to, n, out);
+            if (GATED && p.out_terms) store_terms(p, to, n, out);
+            else store_outputs(p, to, n, out);
         }
     }
 }
@@ -309,12 +333,12 @@ template <class T, bool GATED, int TT, int WAVES, int MATS>
 hipError_t few_of(const Int4Args &p, hipStream_t st)
 {
     constexpr long long kMost = 32768;          // tiles of tokens in a launch
-    const int TM = 16 * TT;
-    const long long tiles = p.pairs ? p.M : p.tiles ? most_tiles(p.M, p.E, TM) : (p.M + TM - 1) / TM;
+    const int TM = 16 * TT, own = p.terms == 0 ? TM : p.terms == 2 ? TM / 2 : 16, cuts = p.tiles ? std::max(1, p.tile / own) : 1;
+    const long long tiles = p.pairs ? p.M : p.tiles ? most_tiles(p.M, p.E, p.tile) * cuts : (p.M + TM - 1) / TM;
     const long long each = std::max<long long>(1, std::min<long long>(kMost, kMaxBlocks / ceil_div(p.N, GATED ? 16 : 16 * MATS)));
     for (long long m = 0; m < tiles; m += each) {
         Int4Args q = p;
-        q.first = m;
+        q.first = m, q.cuts = cuts;
         const dim3 grid((unsigned)ceil_div(p.N, GATED ? 16 : 16 * MATS), (unsigned)std::min(each, tiles - m)), block(WAVES * kWave);
         if (p.group == 128) int4_few_kernel<T, GATED, TT, 1, WAVES, MATS><<<grid, block, 0, st>>>(q);
         else if (p.group == 64) int4_few_kernel<T, GATED, TT, 2, WAVES, MATS><<<grid, block, 0, st>>>(q);
@@ -342,20 +366,24 @@ hipError_t few(const Int4Args &p, hipStream_t st)
 template <class T, bool GATED>
 hipError_t few_by_tokens(const Int4Args &p, hipStream_t st)
 {
+    if constexpr (!GATED)
+        if (p.terms) return p.terms == 2 && p.tile <= 16 ? few<T, GATED, 2>(p, st) : few<T, GATED, 4>(p, st);
     const long long each = p.pairs ? 1 : p.tiles ? p.tile : p.M;
     return each <= 16 ? few<T, GATED, 1>(p, st) : each <= 32 ? few<T, GATED, 2>(p, st) : few<T, GATED, 4>(p, st);
 }
 
 // ---- a token's experts' second products and their sum -------------------------------------------------------------------
 // A workgroup has 16 rows of every chosen expert's matrix for one token; a wave has a share of the contraction of one of them, or of several in turn.
+// The matrix instruction's columns, which would all be the one token, are its terms: they cost nothing.
 // Sums are multiplied by their slot's weight before they are added, slots in order within a wave, then the waves'.
 
 constexpr int kDownWaves = 16;
 
-template <class T, int GROUPS>
+template <int GROUPS>
 __global__ __launch_bounds__(kDownWaves * kWave) void int4_down_kernel(const Int4Args p, const float *weights, int shares)
 {
-    __shared__ f32x4 sums[kDownWaves][4];
+    typedef bf16_t T;
+    __shared__ f32x4 sums[kDownWaves][4][kMostTerms];
     __shared__ Held held[kDownWaves];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), r = lane & 15, g = lane >> 4;
     const int n0 = first_row(blockIdx.x, 16, p.N), row = min(n0 + r, p.N - 1);
@@ -375,7 +403,7 @@ __global__ __launch_bounds__(kDownWaves * kWave) void int4_down_kernel(const Int
         Span<T, 1, 1> span;
         span.view[0] = of_stack(p.w, p, expert);
         span.w[0] = (const uint32_t *)(span.view[0].q + row * p.ldq);
-        span.x[0] = (const T *)((const char *)p.x + m * p.ldx);
+        span.x[0] = (const T *)((const char *)p.x + m * p.ldx) + (long long)min(r, p.terms - 1) * hidden_stride(p.K);
         span.row[0] = row, span.N = p.N, span.K = p.K, span.groups = (p.K + p.group - 1) / p.group, span.scale_type = p.scale_type, span.held = &held[wave];
         f32x4 acc[1][1];
         accumulate<T, 1, 1, GROUPS, (GROUPS == 4 ? 1 : 2)>(span, steps * part / shares, steps * (part + 1) / shares, acc);
@@ -384,7 +412,7 @@ __global__ __launch_bounds__(kDownWaves * kWave) void int4_down_kernel(const Int
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[e] += none;
-    if (r == 0) sums[wave][g] = sum;
+    if (r < kMostTerms) sums[wave][g][r] = sum;
     __syncthreads();
     const int n = n0 + t * 4;
     if (t >= 4 || n >= p.N) return;
@@ -392,11 +420,10 @@ __global__ __launch_bounds__(kDownWaves * kWave) void int4_down_kernel(const Int
 #pragma unroll
     for (int w = 0; w < kDownWaves; ++w)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[e] += sums[w][t][e];
+        for (int e = 0; e < 4; ++e) out[e] += p.terms == 2 ? sums[w][t][0][e] + sums[w][t][1][e] : sums[w][t][0][e] + (sums[w][t][1][e] + sums[w][t][2][e]);
     store_outputs(p, token, n, out);
 }
 
-template <class T>
 hipError_t down(const Int4Args &p, const float *weights, hipStream_t st)
 {
     const int shares = std::max(1, kDownWaves / p.chosen);
@@ -406,9 +433,9 @@ hipError_t down(const Int4Args &p, const float *weights, hipStream_t st)
         Int4Args q = p;
         q.first = m;
         const dim3 grid((unsigned)ceil_div(p.N, 16), (unsigned)std::min(each, p.M - m)), block(kDownWaves * kWave);
-        if (p.group == 128) int4_down_kernel<T, 1><<<grid, block, 0, st>>>(q, weights, shares);
-        else if (p.group == 64) int4_down_kernel<T, 2><<<grid, block, 0, st>>>(q, weights, shares);
-        else int4_down_kernel<T, 4><<<grid, block, 0, st>>>(q, weights, shares);
+        if (p.group == 128) int4_down_kernel<1><<<grid, block, 0, st>>>(q, weights, shares);
+        else if (p.group == 64) int4_down_kernel<2><<<grid, block, 0, st>>>(q, weights, shares);
+        else int4_down_kernel<4><<<grid, block, 0, st>>>(q, weights, shares);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -424,10 +451,7 @@ hipError_t launch_int4_few(const Int4Args &p, int type, bool gated, hipStream_t 
     return gated ? few_by_tokens<bf16_t, true>(p, st) : few_by_tokens<bf16_t, false>(p, st);
 }
 
-hipError_t launch_int4_down(const Int4Args &p, const float *weights, int type, hipStream_t st)
-{
-    return type == XNOR_TYPE_F16 ? down<f16_t>(p, weights, st) : down<bf16_t>(p, weights, st);
-}
+hipError_t launch_int4_down(const Int4Args &p, const float *weights, hipStream_t st) { return down(p, weights, st); }
 
 hipError_t launch_int4(const Int4Args &p, int type, bool gated, hipStream_t st)
 {

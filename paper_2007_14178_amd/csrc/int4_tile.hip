@@ -50,10 +50,13 @@ template <class R> __device__ inline uint8_t load_1(R, int, int) { return 0; }
 #endif
 
 // SHORT: groups of 32, two of them in a step.
-template <class T, bool GATED, bool SHORT, int TM>
+// TERMS: 2 or 3: a token is the sum of so many rows, which stand in a wave's tiles of 16 one term after the other (of three in four, the last one's twice,
+// which is not multiplied) and are added where they are multiplied: a workgroup has the tokens that its TM rows make.
+template <class T, bool GATED, bool SHORT, int TM, int TERMS>
 __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, int tiles_n, long long tiles)
 {
     constexpr int TN = GATED ? 64 : 128;        // outputs n of a tile
+    constexpr int OWN = TERMS == 0 ? 4 : TERMS == 2 ? 2 : 1, TOKENS = TM / 4 * OWN;         // a wave's tiles of tokens, and the workgroup's tokens
     constexpr int kThreads = 2 * TM, A = 4, B = 512 / kThreads;         // chunks of the tokens and word pairs of the weights that a thread stages
     typedef Mat<T> Mul;
     __shared__ __align__(16) char lds[2][(TM + kRows) * kStep];
@@ -61,7 +64,7 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     // Workgroups go round the eight XCDs by their index: each takes a run of consecutive tiles, groups of eight tiles of tokens for a tile of the
     // weights' rows, so that what its units work on at a time shares both in its L2.  (Experts: of the tiles that there are.)
-    if (p.tiles) tiles = min(tiles, (p.tiles[0].count - p.first) * tiles_n);
+    if (p.tiles) tiles = min(tiles, ((long long)p.tiles[0].count * (TERMS ? p.cuts : 1) - p.first) * tiles_n);
     const long long eighth = (tiles + 7) >> 3, index = (blockIdx.x & 7) * eighth + (blockIdx.x >> 3);
     if ((blockIdx.x >> 3) >= eighth || index >= tiles) return;
     const int rows = (int)(tiles / tiles_n), group8 = (int)(index / (8 * tiles_n)), in = (int)(index - (long long)group8 * 8 * tiles_n);
@@ -69,11 +72,17 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
     const int tn = __builtin_amdgcn_readfirstlane(in / high), tm = __builtin_amdgcn_readfirstlane(group8 * 8 + in % high);
     const int n0 = tn * TN;
     Int4View view[2] = {p.w, GATED ? p.w2 : p.w};
-    long long m0 = (p.first + tm) * TM;
-    int count = (int)min(p.M - m0, (long long)TM);
+    long long m0 = (p.first + tm) * TOKENS;
+    int count = (int)min(p.M - m0, (long long)TOKENS);
     if (p.tiles) {
-        const ExpertTile tile = p.tiles[1 + p.first + tm];
-        m0 = tile.first, count = tile.count;
+        const long long at = p.first + tm;
+        const int cut = TERMS ? (int)(at % p.cuts) * TOKENS : 0;
+        const ExpertTile tile = p.tiles[1 + (TERMS ? at / p.cuts : at)];
+        m0 = tile.first + cut, count = tile.count - cut;
+        if (TERMS) {
+            if (count <= 0) return;
+            count = min(count, TOKENS);
+        }
         view[0] = of_stack(view[0], p, tile.expert), view[1] = of_stack(view[1], p, tile.expert);
     }
 
@@ -85,8 +94,8 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
     int a[A];
 #pragma unroll
     for (int i = 0; i < A; ++i) {
-        const int m = min((t >> 3) + TM / 4 * i, count - 1);
-        a[i] = (int)((p.order_x ? p.order_x[m0 + m] / p.chosen : m) * p.ldx) + chunk * 16;
+        const int r = (t >> 3) + TM / 4 * i, m = min(TERMS ? r / 64 * (16 * OWN) + r % (16 * OWN) : r, count - 1);
+        a[i] = (int)((p.order_x ? p.order_x[m0 + m] / p.chosen : m) * p.ldx) + (TERMS ? min(r % 64 / (16 * OWN), TERMS - 1) * hidden_stride(p.K) * 2 : 0) + chunk * 16;
     }
     const int words = (p.K + 7) / 8, groups = (p.K + p.group - 1) / p.group, shift = __builtin_ctz(p.group);
     const bool has_zero = view[0].zero != nullptr, half = p.scale_type == XNOR_TYPE_F16;
@@ -164,8 +173,9 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
     };
 
     const int wm = (TM == 256 ? wave & 3 : wave >> 1) * 64, wn = (TM == 256 ? wave >> 2 : wave & 1) * 64;
-    const bool busy = wm < count;       // whether the wave has tokens
-    f32x4 acc[4][4] = {};
+    const int own = wm / 4 * OWN;       // the wave's first token
+    const bool busy = own < count;      // whether it has any
+    f32x4 acc[4][OWN] = {};
     auto step = [&](int s, Rows &rows_of, auto more) __attribute__((always_inline)) {
         if (busy) {
             const char *const la = lds[s & 1], *const lb = la + TM * kStep;
@@ -187,14 +197,20 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
                 const f32x4 first = *(const f32x4 *)&by[s & 1][0][wn + i * 16 + (lane >> 4) * 4];
                 const f32x4 then = SHORT ? *(const f32x4 *)&by[s & 1][1][wn + i * 16 + (lane >> 4) * 4] : first;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < OWN; ++j) {
                     f32x4 sum = Mul::mul(fb[0][i], fa[0][j], f32x4{});
+#pragma unroll
+                    for (int of = 1; of < TERMS; ++of) sum = Mul::mul(fb[0][i], fa[0][j + of * OWN], sum);
                     if constexpr (SHORT) {
-                        const f32x4 more = Mul::mul(fb[1][i], fa[1][j], f32x4{});
+                        f32x4 more = Mul::mul(fb[1][i], fa[1][j], f32x4{});
+#pragma unroll
+                        for (int of = 1; of < TERMS; ++of) more = Mul::mul(fb[1][i], fa[1][j + of * OWN], more);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[i][j][e] += first[e] * sum[e] + then[e] * more[e];
                     } else {
                         sum = Mul::mul(fb[1][i], fa[1][j], sum);
+#pragma unroll
+                        for (int of = 1; of < TERMS; ++of) sum = Mul::mul(fb[1][i], fa[1][j + of * OWN], sum);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[i][j][e] += first[e] * sum[e];
                     }
@@ -230,8 +246,8 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
         float bias[4];
         load_params(p.bias, n, p.N, 0.f, bias);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int at = wm + j * 16 + (lane & 15);
+        for (int j = 0; j < OWN; ++j) {
+            const int at = own + j * 16 + (lane & 15);
             if (at >= count) continue;
             if (p.parts > 1) {          // [part][matrix][M][N]
 #pragma unroll
@@ -248,7 +264,8 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
                 else out[e] = p.bias ? acc[i][j][e] + bias[e] : acc[i][j][e];
             }
             const long long m = m0 + at;
-            store_outputs(p, p.order_out ? p.order_out[m] : m, n, out);
+            if (GATED && p.out_terms) store_terms(p, m, n, out);
+            else store_outputs(p, p.order_out ? p.order_out[m] : m, n, out);
         }
     }
 }
@@ -289,19 +306,20 @@ __global__ __launch_bounds__(256) void int4_join_kernel(const Int4Args p, int bl
     store_outputs(p, m, n, out);
 }
 
-template <class T, bool GATED, int TM>
+template <class T, bool GATED, int TM, int TERMS>
 hipError_t tiles(const Int4Args &p, hipStream_t st)
 {
-    const int tiles_n = ceil_div(p.N, GATED ? 64 : 128);
-    const long long all = p.tiles ? most_tiles(p.M, p.E, TM) : (p.M + TM - 1) / TM;
+    constexpr int TOKENS = TERMS == 0 ? TM : TERMS == 2 ? TM / 2 : TM / 4;
+    const int tiles_n = ceil_div(p.N, GATED ? 64 : 128), cuts = p.tiles ? std::max(1, p.tile / TOKENS) : 1;
+    const long long all = p.tiles ? most_tiles(p.M, p.E, p.tile) * cuts : (p.M + TOKENS - 1) / TOKENS;
     const long long each = std::max<long long>(1, kMaxBlocks / tiles_n);
     for (long long m = 0; m < all; m += each) {
         Int4Args q = p;
-        q.first = m;
+        q.first = m, q.cuts = cuts;
         const long long n = std::min(each, all - m) * tiles_n;
         const dim3 grid((unsigned)((n + 7) / 8 * 8), p.parts), block(2 * TM);
-        if (p.group == 32) int4_tile_kernel<T, GATED, true, TM><<<grid, block, 0, st>>>(q, tiles_n, n);
-        else int4_tile_kernel<T, GATED, false, TM><<<grid, block, 0, st>>>(q, tiles_n, n);
+        if (p.group == 32) int4_tile_kernel<T, GATED, true, TM, TERMS><<<grid, block, 0, st>>>(q, tiles_n, n);
+        else int4_tile_kernel<T, GATED, false, TM, TERMS><<<grid, block, 0, st>>>(q, tiles_n, n);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -311,11 +329,13 @@ hipError_t tiles(const Int4Args &p, hipStream_t st)
 template <class T, bool GATED>
 hipError_t by_tiles(const Int4Args &p, hipStream_t st)
 {
+    if constexpr (!GATED && std::is_same<T, bf16_t>::value)
+        if (p.terms) return p.terms == 2 ? tiles<T, GATED, 256, 2>(p, st) : tiles<T, GATED, 256, 3>(p, st);
     // the larger tile where there is one for each unit: half the conversions for a product (4096 x 8192 x 8192 bf16 a fifth more on the smaller than on
     // the larger), but one workgroup a unit, with nothing beside its begin and end (32768 pairs of 64 experts, 2048 x 1024, 976 and 982 us in all on
     // the smaller and the larger ones, of 8 experts with 1024 pairs each 252 and 267)
     const bool large = !p.tiles && p.parts == 1 && p.M > 128 && (p.M + 255) / 256 * ceil_div(p.N, GATED ? 64 : 128) >= compute_units();
-    const hipError_t e = large ? tiles<T, GATED, 256>(p, st) : tiles<T, GATED, 128>(p, st);
+    const hipError_t e = large ? tiles<T, GATED, 256, 0>(p, st) : tiles<T, GATED, 128, 0>(p, st);
     if (e != hipSuccess || p.parts == 1) return e;
     const int blocks_n = ceil_div(p.N, 1024);
     int4_join_kernel<GATED><<<dim3((unsigned)(p.M * blocks_n)), dim3(256), 0, st>>>(p, blocks_n);
