@@ -15,10 +15,10 @@ namespace {
 
 constexpr int kRows = 128, kDeep = 64;       // rows of the weights a tile, values of a step
 
-// A word's levels less their zero point, exactly: as f16, or as bf16 times 2^-8 (so that sums of tokens near the largest value stay finite), which the
-// group's scale gets back.
+// A word's levels less their zero point, exactly: as f16, or as bf16 times 2^-11, which the group's scale gets back: a step's sums, of up to 64 times 15 tokens, stay
+// finite for tokens up to the largest.
 template <class T> constexpr float kBack = 1.f;
-template <> constexpr float kBack<bf16_t> = 0x1p8f;
+template <> constexpr float kBack<bf16_t> = 0x1p11f;
 __device__ inline i32x4 operand_of(f16_t, uint32_t w, uint32_t zero) { return Levels<f16_t>::operand<false>(w, Levels<f16_t>::zero(zero)); }
 __device__ inline i32x4 operand_of(bf16_t, uint32_t w, uint32_t zero)
 {
@@ -26,8 +26,8 @@ __device__ inline i32x4 operand_of(bf16_t, uint32_t w, uint32_t zero)
     // (so that a byte's conversion is one instruction)
     asm("" : "+v"(even));
     asm("" : "+v"(odd));
-    const float less = (float)zero * -0x1p-8f;
-    auto at = [&](uint32_t v, int byte) { return __float_as_uint(__builtin_fmaf((float)(v >> 8 * byte & 255u), 0x1p-8f, less)); };
+    const float less = (float)zero * -0x1p-11f;
+    auto at = [&](uint32_t v, int byte) { return __float_as_uint(__builtin_fmaf((float)(v >> 8 * byte & 255u), 0x1p-11f, less)); };
     auto two = [](uint32_t low, uint32_t high) { return (int)__builtin_amdgcn_perm(high, low, 0x07060302u); };        // (small integers: no bits are lost)
     return i32x4{two(at(even, 0), at(even, 2)), two(at(odd, 0), at(odd, 2)), two(at(even, 1), at(even, 3)), two(at(odd, 1), at(odd, 3))};
 }
