@@ -604,7 +604,7 @@ int xnor_int4_dequantize(const xnor_int4 *w, void *out, int out_type, long long 
  *   bias   in   fp32 [N] or NULL
  *   out    out  [M][rows of the weights], out_type any
  * Sums are fp32: the products are of tokens and levels less their zero point, which the tokens' type holds exactly, and a group's sum is multiplied by
- * its scale, so that weights are never rounded.  An infinity or NaN among a token's values, or a scale that is NaN, reaches the outputs that it would in
+ * its scale, so that weights are never rounded; with bf16 tokens scales of 2^116 and more overflow.  An infinity or NaN among a token's values, or a scale that is NaN, reaches the outputs that it would in
  * products of the values.
  *   workspace  16-byte aligned, xnor_int4_*_workspace_bytes bytes (host only): for sums over shares of the contraction, where tokens and rows are too
  *              few to fill the GPU; NULL or smaller: then not used.  Its contents mean nothing afterwards

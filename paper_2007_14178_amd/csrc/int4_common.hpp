@@ -19,13 +19,14 @@ __device__ inline uint32_t and_or(uint32_t a)
     return (a & MASK) | set;
 }
 
-// Eight values of a word as the operand's four registers: register j holds the values 2 j and 2 j + 1, as f16 or bf16.
+// Eight values of a word, levels less their zero point, as the operand's four registers: register j holds the values 2 j and 2 j + 1, as f16 or bf16, which hold
+// them exactly.  Sums get kBack back with their group's scale.
 template <class T> struct Levels;
 
 // f16 has ten bits behind the point: a level in the lowest four of 1024's is 1024 + level, in the next four of 64's 64 + level, and a packed
-// addition leaves level - zero, exactly: 9 instructions for eight values.
+// addition leaves level - zero: 9 instructions for eight values.
 template <> struct Levels<f16_t> {
-    static constexpr bool kOffset = false;
+    static constexpr float kBack = 1.f;
     struct Zero {
         uint32_t far, near;             // -(1024 + zero), -(64 + zero), twice
     };
@@ -34,13 +35,11 @@ template <> struct Levels<f16_t> {
         const uint32_t zz = z | z << 16;
         return {0xe400e400u | zz, 0xd400d400u | zz << 4};
     }
-    static __device__ i32x4 offset(const Zero &) { return i32x4{}; }        // (not called)
     static __device__ uint32_t add(uint32_t a, uint32_t b)
     {
         typedef f16_t f16x2 __attribute__((ext_vector_type(2)));
         return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, a) + __builtin_bit_cast(f16x2, b));
     }
-    template <bool EXACT>
     static __device__ i32x4 operand(uint32_t w, const Zero &z)
     {
         const uint32_t v = w >> 8;
@@ -49,32 +48,26 @@ template <> struct Levels<f16_t> {
     }
 };
 
-// bf16 has seven, and no packed addition: a level in the upper four of 16's is 16 + level, at 8 instructions for eight values, and a second matrix
-// instruction adds -(16 + zero) times the same tokens in fp32.  That costs up to 5 bits of the 24 in sums of a group and makes NaN of a token's
-// infinity (and infinities of sums near the largest value): sums that are not finite are formed again (EXACT), from levels less zeros times
-// 2^-16, which their group's scale gets back.
+// bf16 has no packed addition: a byte's conversion to fp32, an addition and half a packing for each value, 23 instructions for eight.  (16 + level, which takes 8,
+// with a second matrix instruction that takes (16 + zero) times the tokens off, would cost sums the low bits of 31 times the largest token's magnitude, also
+// where that one meets a level that is its zero point.)  Times 2^-11: sums of up to 128 times 15 tokens stay finite for tokens up to the largest.
 template <> struct Levels<bf16_t> {
-    static constexpr bool kOffset = true;
+    static constexpr float kBack = 0x1p11f;
     struct Zero {
-        uint32_t minus;                 // -(16 + zero), twice
-        float z;
+        float less;
     };
-    static __device__ Zero zero(uint32_t z) { return {0xc180c180u | (z | z << 16) << 3, (float)z}; }
-    static __device__ i32x4 offset(const Zero &z) { return i32x4{(int)z.minus, (int)z.minus, (int)z.minus, (int)z.minus}; }
-    template <bool EXACT>
+    static __device__ Zero zero(uint32_t z) { return {(float)z * -0x1p-11f}; }
     static __device__ i32x4 operand(uint32_t w, const Zero &z)
     {
-        if constexpr (EXACT) {
-            i32x4 to;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float low = ((float)(w >> 4 * j & 15u) - z.z) * 0x1p-16f, high = ((float)(w >> (16 + 4 * j) & 15u) - z.z) * 0x1p-16f;
-                to[j] = (int)(__float_as_uint(low) >> 16 | (__float_as_uint(high) & 0xffff0000u));      // (small integers: no bits are lost)
-            }
-            return to;
-        }
-        return i32x4{(int)and_or<0x00780078u, 0x41804180u>(w << 3), (int)and_or<0x00780078u, 0x41804180u>(w >> 1),
-                     (int)and_or<0x00780078u, 0x41804180u>(w >> 5), (int)and_or<0x00780078u, 0x41804180u>(w >> 9)};
+        uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
+#ifdef __HIP_DEVICE_COMPILE__
+        // (so that a byte's conversion is one instruction)
+        asm("" : "+v"(even));
+        asm("" : "+v"(odd));
+#endif
+        auto at = [&](uint32_t v, int byte) { return __float_as_uint(__builtin_fmaf((float)(v >> 8 * byte & 255u), 0x1p-11f, z.less)); };
+        auto two = [](uint32_t low, uint32_t high) { return (int)__builtin_amdgcn_perm(high, low, 0x07060302u); };        // (small integers: no bits are lost)
+        return i32x4{two(at(even, 0), at(even, 2)), two(at(odd, 0), at(odd, 2)), two(at(even, 1), at(even, 3)), two(at(odd, 1), at(odd, 3))};
     }
 };
 

@@ -109,7 +109,7 @@ __device__ inline void load_stage(const Span<T, MATS, TT> &p, int s, Stage<MATS,
         for (int u = 0; u < U; ++u) load_x<T, MATS, TT, U, WHOLE>(p, s, u, to);
 }
 
-template <class T, int MATS, int TT, int GROUPS, int U, bool WHOLE, bool EXACT>
+template <class T, int MATS, int TT, int GROUPS, int U, bool WHOLE>
 __device__ inline void use_stage(const Span<T, MATS, TT> &p, int s, Stage<MATS, TT, U> &from, f32x4 (&acc)[MATS][TT])
 {
     typedef Mat<T> Mul;
@@ -119,7 +119,7 @@ __device__ inline void use_stage(const Span<T, MATS, TT> &p, int s, Stage<MATS, 
     for (int k = 0; k < MATS; ++k) {
         const uint32_t bits = p.scale_type == XNOR_TYPE_FP32 ? (uint32_t)from.high[k] << 16 | from.low[k] : (uint32_t)from.low[k] << 16;
         const float half = (float)__builtin_bit_cast(f16_t, from.low[k]);
-        p.held[k].scale[lane] = p.scale_type == XNOR_TYPE_F16 ? half : __uint_as_float(bits);
+        p.held[k].scale[lane] = (p.scale_type == XNOR_TYPE_F16 ? half : __uint_as_float(bits)) * Level::kBack;
         p.held[k].zero[lane] = p.view[k].zero ? from.zero[k] & 15u : 8u;
     }
     // (a wave's own: its LDS instructions come in order)
@@ -139,17 +139,14 @@ __device__ inline void use_stage(const Span<T, MATS, TT> &p, int s, Stage<MATS, 
                 f32x4 part[TT] = {};
 #pragma unroll
                 for (int q = i * (4 / GROUPS); q < (i + 1) * (4 / GROUPS); ++q) {
-                    const i32x4 levels = Level::template operand<EXACT>(from.w[k][u][q], z);
+                    const i32x4 levels = Level::operand(from.w[k][u][q], z);
 #pragma unroll
-                    for (int j = 0; j < TT; ++j) {
-                        part[j] = Mul::mul(levels, from.x[u][q][j], part[j]);
-                        if constexpr (Level::kOffset && !EXACT) part[j] = Mul::mul(Level::offset(z), from.x[u][q][j], part[j]);
-                    }
+                    for (int j = 0; j < TT; ++j) part[j] = Mul::mul(levels, from.x[u][q][j], part[j]);
                 }
 #pragma unroll
                 for (int j = 0; j < TT; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[k][j][e] += (EXACT && Level::kOffset ? by[e] * 0x1p16f : by[e]) * part[j][e];
+                    for (int e = 0; e < 4; ++e) acc[k][j][e] += by[e] * part[j][e];
             }
             __builtin_amdgcn_sched_barrier(0);          // (all groups' operands at a time would not fit the registers)
         }
@@ -174,17 +171,17 @@ __device__ inline void accumulate(const Span<T, MATS, TT> &p, int from, int to, 
         load_stage<T, MATS, TT, GROUPS, U, true>(p, s, a);
         for (; s + 3 * U <= whole; s += 2 * U) {
             load_stage<T, MATS, TT, GROUPS, U, true>(p, s + U, b);
-            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s, a, acc);
+            use_stage<T, MATS, TT, GROUPS, U, true>(p, s, a, acc);
             load_stage<T, MATS, TT, GROUPS, U, true>(p, s + 2 * U, a);
-            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s + U, b, acc);
+            use_stage<T, MATS, TT, GROUPS, U, true>(p, s + U, b, acc);
         }
         if (s + 2 * U <= whole) {
             load_stage<T, MATS, TT, GROUPS, U, true>(p, s + U, b);
-            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s, a, acc);
-            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s + U, b, acc);
+            use_stage<T, MATS, TT, GROUPS, U, true>(p, s, a, acc);
+            use_stage<T, MATS, TT, GROUPS, U, true>(p, s + U, b, acc);
             s += 2 * U;
         } else {
-            use_stage<T, MATS, TT, GROUPS, U, true, false>(p, s, a, acc);
+            use_stage<T, MATS, TT, GROUPS, U, true>(p, s, a, acc);
             s += U;
         }
     }
@@ -192,37 +189,12 @@ __device__ inline void accumulate(const Span<T, MATS, TT> &p, int from, int to, 
         for (; s < whole; ++s) {
             Stage<MATS, TT, 1> a;
             load_stage<T, MATS, TT, GROUPS, 1, true>(p, s, a);
-            use_stage<T, MATS, TT, GROUPS, 1, true, false>(p, s, a, acc);
+            use_stage<T, MATS, TT, GROUPS, 1, true>(p, s, a, acc);
         }
     if (s < to) {
         Stage<MATS, TT, 1> a;
         load_stage<T, MATS, TT, GROUPS, 1, false>(p, s, a);
-        use_stage<T, MATS, TT, GROUPS, 1, false, false>(p, s, a, acc);
-    }
-    if constexpr (Levels<T>::kOffset) {
-        auto is_odd = [](float v) { return !(fabsf(v) <= 3.402823466e38f); };
-        bool odd = false;
-#pragma unroll
-        for (int k = 0; k < MATS; ++k)
-#pragma unroll
-            for (int j = 0; j < TT; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) odd |= is_odd(acc[k][j][e]);
-        if (__any(odd)) {
-            f32x4 exact[MATS][TT] = {};
-            for (s = from; s < to; ++s) {
-                Stage<MATS, TT, 1> a;
-                load_stage<T, MATS, TT, GROUPS, 1, false>(p, s, a);
-                use_stage<T, MATS, TT, GROUPS, 1, false, true>(p, s, a, exact);
-            }
-#pragma unroll
-            for (int k = 0; k < MATS; ++k)
-#pragma unroll
-                for (int j = 0; j < TT; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (is_odd(acc[k][j][e])) acc[k][j][e] = exact[k][j][e];
-        }
+        use_stage<T, MATS, TT, GROUPS, 1, false>(p, s, a, acc);
     }
 }
 

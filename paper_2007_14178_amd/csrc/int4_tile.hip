@@ -15,23 +15,6 @@ namespace {
 
 constexpr int kRows = 128, kDeep = 64;       // rows of the weights a tile, values of a step
 
-// A word's levels less their zero point, exactly: as f16, or as bf16 times 2^-11, which the group's scale gets back: a step's sums, of up to 64 times 15 tokens, stay
-// finite for tokens up to the largest.
-template <class T> constexpr float kBack = 1.f;
-template <> constexpr float kBack<bf16_t> = 0x1p11f;
-__device__ inline i32x4 operand_of(f16_t, uint32_t w, uint32_t zero) { return Levels<f16_t>::operand<false>(w, Levels<f16_t>::zero(zero)); }
-__device__ inline i32x4 operand_of(bf16_t, uint32_t w, uint32_t zero)
-{
-    uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
-    // (so that a byte's conversion is one instruction)
-    asm("" : "+v"(even));
-    asm("" : "+v"(odd));
-    const float less = (float)zero * -0x1p-11f;
-    auto at = [&](uint32_t v, int byte) { return __float_as_uint(__builtin_fmaf((float)(v >> 8 * byte & 255u), 0x1p-11f, less)); };
-    auto two = [](uint32_t low, uint32_t high) { return (int)__builtin_amdgcn_perm(high, low, 0x07060302u); };        // (small integers: no bits are lost)
-    return i32x4{two(at(even, 0), at(even, 2)), two(at(odd, 0), at(odd, 2)), two(at(even, 1), at(even, 3)), two(at(odd, 1), at(odd, 3))};
-}
-
 // Loads from a buffer: a lane's offset and a scalar one.  (The host's pass does not know the builtins.)
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 __device__ inline auto buffer(const void *p, int size) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, size, 0x00027000); }
@@ -160,10 +143,10 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
             const int r = (t >> 2) + TM / 2 * i;
             const float of_half = (float)__builtin_bit_cast(f16_t, (uint16_t)from.low[i]);
             const float scale = half ? of_half : __uint_as_float(wide ? from.high[i] << 16 | from.low[i] : from.low[i] << 16);
-            by[s & 1][pair >> 1][r] = scale * kBack<T>;         // (pairs 0 and 1, 2 and 3 are of one group)
-            const uint32_t zero = has_zero ? from.zero[i] & 15u : 8u;
+            by[s & 1][pair >> 1][r] = scale * Levels<T>::kBack;         // (pairs 0 and 1, 2 and 3 are of one group)
+            const typename Levels<T>::Zero zero = Levels<T>::zero(has_zero ? from.zero[i] & 15u : 8u);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) *(i32x4 *)(lb + r * kStep + (((pair * 2 + j) ^ (r & 7)) << 4)) = operand_of(T(), from.b[i][j], zero);
+            for (int j = 0; j < 2; ++j) *(i32x4 *)(lb + r * kStep + (((pair * 2 + j) ^ (r & 7)) << 4)) = Levels<T>::operand(from.b[i][j], zero);
         }
 #pragma unroll
         for (int i = 0; i < A; ++i) {

@@ -40,3 +40,26 @@ def test_tokens_near_the_largest_value(xb, M, N, K, group):
     want = torch.full((M, N), 2.0 ** 97 * 15 * K)
     want[1] = -want[1]
     assert torch.equal(xb.xnor_int4_linear(x, w, out_dtype=F32).cpu(), want)
+
+
+@pytest.mark.parametrize("M", [1, 5, 20, 40, 64, 300])
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)], ids=str)
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=str)
+def test_a_token_that_meets_zero_points_costs_nothing(xb, M, group, zeros, dtype):
+    """Tokens far larger than the others at columns where every level is its zero point: their products are 0, and the others' sums keep all their bits."""
+    N, K = 130, 300
+    gen = torch.Generator().manual_seed(M)
+    x = torch.randint(-2, 3, (M, K), generator=gen).to(dtype)
+    levels = torch.randint(0, 16, (N, K), generator=gen, dtype=torch.uint8)
+    groups = (K + group - 1) // group
+    zero = torch.randint(0, 16, (groups, N), generator=gen, dtype=torch.uint8)
+    for c in (7, 100, 299):
+        x[:, c] = 2.0 ** (15 if dtype is F16 else 40)
+        levels[:, c] = zero[c // group] if zeros else 8
+    x = x.cuda()
+    w = xb.Int4(xb.xnor_int4_pack(levels.cuda()), torch.ones(groups, N, dtype=dtype, device="cuda"), zero.cuda() if zeros else None, K, group)
+    want = x.cpu().double() @ xref.values(w)[0].t()
+    assert 0 < float(want.abs().max()) < 2.0 ** 15
+    assert torch.equal(xb.xnor_int4_linear(x, w, out_dtype=F32).cpu().double(), want)
+    got = xb.xnor_int4_gated(x, w, w, ref.RELU, out_dtype=F32).cpu().double()
+    assert torch.equal(got, (want.clamp(min=0.0) * want).float().double())
