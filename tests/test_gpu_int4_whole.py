@@ -63,3 +63,53 @@ def test_a_token_that_meets_zero_points_costs_nothing(xb, M, group, zeros, dtype
     assert torch.equal(xb.xnor_int4_linear(x, w, out_dtype=F32).cpu().double(), want)
     got = xb.xnor_int4_gated(x, w, w, ref.RELU, out_dtype=F32).cpu().double()
     assert torch.equal(got, (want.clamp(min=0.0) * want).float().double())
+
+
+# few tokens by every kernel; tiles; tiles in shares of the contraction; contractions that end inside a step, behind very long ones too
+SIZES = [(1, 50, 1), (13, 50, 33), (20, 50, 129), (33, 40, 41), (40, 2050, 65), (64, 9000, 39), (64, 300, 1031), (128, 50, 393), (65, 300, 30000), (129, 1100, 2600),
+         (200, 1024, 4095), (1000, 520, 1100), (8200, 1030, 70), (90, 1, 5000000), (40, 1030, 8200), (33, 2050, 8195), (300, 1024, 4096)]
+
+
+def marked(K, gen):
+    """Columns of a contraction that hold tokens: all of a short one; of a long one its ends, both sides of every place where a share of it may begin, and
+    others as they fall."""
+    if K <= 40000:
+        return torch.arange(K)
+    at = [torch.arange(200), torch.arange(K - 200, K), torch.randint(0, K, (20000,), generator=gen)]
+    whole = K // 64
+    for parts in range(2, 17):
+        for i in range(1, parts):
+            at.append(torch.arange(-70, 70) + whole * i // parts * 64)
+    return torch.unique(torch.cat(at))
+
+
+@pytest.mark.parametrize("M,N,K", SIZES, ids=str)
+@pytest.mark.parametrize("dtype,scale_dtype,group,zeros,gated", [(BF16, BF16, 128, False, False), (BF16, F32, 32, True, False), (F16, F16, 64, True, False),
+                                                                (F16, F32, 32, False, True), (BF16, F16, 64, True, True), (F16, BF16, 128, True, False)], ids=str)
+def test_equal(xb, M, N, K, dtype, scale_dtype, group, zeros, gated):
+    """With the workspace and without.  What is compared would differ were one step of the contraction left out, the last one or a share's first among them."""
+    gated = gated and K < 100000
+    gen = torch.Generator().manual_seed(M + K)
+    at = marked(K, gen)
+    x = torch.zeros(M, K, dtype=dtype, device="cuda")
+    # (-1, 0 and 1 in contractions whose sums would pass 2^24 otherwise)
+    most = 2 if K <= 2600 else 1
+    x[:, at.cuda()] = torch.randint(-most, most + 1, (M, len(at)), generator=gen).to(dtype).cuda()
+    ws = [matrix(xb, gen, N, K, group, zeros, scale_dtype) for _ in range(2 if gated else 1)]
+    xd = x[:, at.cuda()].cpu().double()
+    values = [xref.levels_of(w.q, K)[:, at].double() - (8.0 if w.zero is None else w.zero.cpu().double()[at // group].t()) for w in ws]
+    assert 15.0 * most * len(at) < 2.0 ** 24
+    # (all outputs of the definition, or those of some tokens where that takes long)
+    rows = torch.arange(M) if M * N * len(at) < 1 << 31 else torch.randint(0, M, (200,), generator=gen)
+    sums = [xd[rows] @ v.t() for v in values]
+    want = (sums[0].clamp(min=0.0) * sums[1]).float() if gated else sums[0].float()
+    # each step that holds tokens changes some output
+    steps = at // 64
+    for step in {int(steps[0]), int(steps[-1]), int(steps[len(at) // 2]), int(steps[len(at) // 3])}:
+        mine = steps == step
+        assert (xd[rows][:, mine] @ values[0][:, mine].t()).any()
+    call = (lambda space: xb.xnor_int4_gated(x, *ws, ref.RELU, out_dtype=F32, workspace=space)) if gated else (
+        lambda space: xb.xnor_int4_linear(x, ws[0], out_dtype=F32, workspace=space))
+    for space in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):
+        got = call(space)
+        assert torch.equal(got[rows.cuda()].cpu(), want)
