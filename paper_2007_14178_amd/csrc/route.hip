@@ -419,11 +419,16 @@ __global__ __launch_bounds__(kListThreads) void list_count_kernel(const ListArgs
     for (int e = threadIdx.x; e < p.E; e += kListThreads) p.counts[(long long)blockIdx.x * p.E + e] = count[e];
 }
 
+struct ListSums {
+    int pairs[kListWaves], tiles[kListWaves];
+};
+
 __global__ __launch_bounds__(kListThreads) void list_kernel(const ListArgs p, long long run)
 {
     extern __shared__ unsigned long long bits[];        // [kListWaves][E], then base [E] and room for as many
     int *const base = (int *)(bits + kListWaves * p.E);
-    __shared__ int wave_sums[kListWaves], wave_tiles[kListWaves];
+    __shared__ ListSums sums;
+    int *const wave_sums = sums.pairs, *const wave_tiles = sums.tiles;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const long long from = blockIdx.x * run, to = min(p.pairs, from + run);
     // of expert t: all its pairs, and those of the runs before
@@ -562,7 +567,7 @@ hipError_t launch_route_lists(const ListArgs &p, hipStream_t st)
     const long long run = list_run(p.pairs);
     const int runs = (int)std::max<long long>(1, (p.pairs + run - 1) / run);
     const size_t lds = (size_t)kListWaves * p.E * 8 + p.E * 8;
-    if (lds > 64 * 1024) {
+    if (lds + sizeof(ListSums) > 64 * 1024) {       // (the limit is for both)
         static std::atomic<bool> raised[64];
         int dev = 0;
         hipError_t e = hipGetDevice(&dev);
