@@ -8,6 +8,7 @@
 // (GPU time, bf16: 1 x 4096 x 4096 5.8 us, a launch and two loads' latencies; gated 1 x 4096 x 8192 in groups of 64 with zero points 12.9 us, 2.9 TB/s: 58 vector
 // instructions for a step's 16 rows, beside the loads; 16, 32 and 64 x 8192 x 8192 17.4, 24.3 and 39.2 us, whose tokens each workgroup reads again.)
 #include <algorithm>
+#include <cstddef>
 
 #include "int4_common.hpp"
 
@@ -34,11 +35,12 @@ __device__ inline void turn_about(uint32_t (&d)[4])
 #endif
 }
 
-// A wave's scales and zero points of some groups' 16 rows.
-struct Held {
+// A wave's scales and zero points of some groups' 16 rows.  (Scales are read four at a time.)
+struct alignas(16) Held {
     float scale[kMostGroups * 16];
     uint32_t zero[kMostGroups * 16];
 };
+static_assert(sizeof(Held) % 16 == 0 && offsetof(Held, scale) % 16 == 0, "");
 
 // What a wave multiplies.
 template <class T, int MATS, int TT>

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(2 * TM, 2) void int4_tile_kernel(const Int4Args p, 
     constexpr int kThreads = 2 * TM, A = 4, B = 512 / kThreads;         // chunks of the tokens and word pairs of the weights that a thread stages
     typedef Mat<T> Mul;
     __shared__ __align__(16) char lds[2][(TM + kRows) * kStep];
-    __shared__ float by[2][2][kRows];           // a step's scales, of its first and its second 32 values
+    __shared__ __align__(16) float by[2][2][kRows];         // a step's scales, of its first and its second 32 values
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     // Workgroups go round the eight XCDs by their index: each takes a run of consecutive tiles, groups of eight tiles of tokens for a tile of the
     // weights' rows, so that what its units work on at a time shares both in its L2.  (Experts: of the tiles that there are.)

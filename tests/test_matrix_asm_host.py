@@ -32,3 +32,12 @@ def test_the_check_sees_what_it_looks_for():
     assert list(instructions('asm("v_add_u32 %0, %1, %2" : "=v"(a) : "v"(b), "v"(c)); asm volatile("s_nop 0\\n\\ts_barrier" : : : "memory"); asm("" : "+v"(a));')) == [
         "v_add_u32 %0, %1, %2", "s_nop 0", "s_barrier"]
     assert len(SOURCES) > 8
+
+
+@pytest.mark.parametrize("path", SOURCES, ids=os.path.basename)
+def test_shared_memory_read_wide_is_declared_so(path):
+    """Shared arrays of bytes, words or floats that are read or written through wider pointers say their alignment; the compiler may place others anywhere."""
+    source = open(path).read()
+    for name in re.findall(r"__shared__ (?:char|int|float|uint32_t|uint16_t) (\w+)\[", source):
+        wide = re.search(r"\((?:const )?(?:f32x4|i32x4|i32x2|uint4|float4) \*\)\s*&?\(?%s\b" % name, source)
+        assert not wide, f"{os.path.basename(path)}: {name} is read through a wider pointer"
