@@ -626,8 +626,8 @@ int xnor_int4_gated(const void *x, int type, long long x_stride, const xnor_int4
  *   experts  out  int32 [T][k]
  *   weights  out  fp32 [T][k]: the chosen experts' p, divided by their sum if `renorm`, times `factor`
  * An expert whose logit is -inf or whose c is -inf or NaN is never chosen.  Where there are fewer than k to choose, the rest of a token's
- * experts is -1, of weight 0.  A token with a NaN among its logits (softmax: or +inf) has the experts -1 and weights NaN.  Weights whose sum is 0
- * (scores too small for 64 bits) are 0.
+ * experts is -1, of weight 0.  A token with a NaN among its logits (softmax: or +inf) has the experts -1 and weights NaN.  A softmax's weights under `renorm`
+ * are the softmax of the chosen logits, however far below the largest these are; sigmoids that are all 0 in 64 bits (logits below -709) have weights of 0.
  * XNOR_E_UNSUPPORTED for another score; XNOR_E_SHAPE where groups does not divide E, 1 <= groups_kept <= groups or the other ranges do not
  * hold, or k exceeds the experts of the groups kept, or T * k >= 2^31.
  *
@@ -640,7 +640,7 @@ int xnor_int4_gated(const void *x, int type, long long x_stride, const xnor_int4
  * _bwd: the logits' gradient from the weights' (none flows through the choice, so none to the bias).  With dw' = factor * dweights and, if renorm,
  * dw'' = (dw' - sum_s dw' p / S) / S with S the sum of the token's chosen p, in place of dw':  sigmoid: dlogit_e = dw' p (1 - p) for the chosen;
  * softmax: dlogit_e = p_e (dw'_e - sum_s dw' p), dw'_e = 0 for others.  Slots without an expert count nothing; one expert in several slots gets the
- * sum of theirs.  Tokens without any expert have gradients of 0, those of logits of -inf are 0.
+ * sum of theirs.  Tokens without any expert, or (sigmoid, renorm) whose scores are all 0 in 64 bits, have gradients of 0, those of logits of -inf are 0.
  *   dweights in   fp32 [T][k]           dlogits  out  [T][E], the logits' type
  */
 typedef enum { XNOR_SCORE_SOFTMAX = 0, XNOR_SCORE_SIGMOID = 1 } xnor_score;

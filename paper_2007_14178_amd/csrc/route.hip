@@ -238,11 +238,17 @@ __global__ __launch_bounds__(kThreads) void route_kernel(const RouteArgs p, long
         for (int i = 0; i < SLOTS; ++i)
             if (n == l + i * LANES) mine[i] = at;
     }
-    double w[SLOTS], sum = 0.;
+    double w[SLOTS], sum = 0., most = kNone;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
-        w[i] = 0.;
-        if (mine[i] >= 0) w[i] = score_of(p, (double)(float)logits[mine[i]], top, total);
+        w[i] = mine[i] >= 0 ? (double)(float)logits[mine[i]] : kNone;
+        most = w[i] > most ? w[i] : most;
+    }
+    // (a softmax's shares are those of exponentials relative to the chosen's largest, whatever its own score is)
+    if (p.renorm && p.score == XNOR_SCORE_SOFTMAX) top = max_lanes<LANES>(most), total = 1.;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+        w[i] = mine[i] >= 0 ? score_of(p, w[i], top, total) : 0.;
         sum += w[i];
     }
     if (p.renorm) sum = sum_lanes<LANES>(sum);
@@ -313,8 +319,13 @@ __global__ __launch_bounds__(kThreads) void route_back_kernel(const RouteArgs p,
         dw[i] = is ? p.factor * p.dweights[token * p.k + n] : 0.f;
         most = fmaxf(most, logit[i]);
     }
-    const bool empty = !any_lane<LANES>(any);
-    if (!dense) top = softmax ? max_of(most) : fminf(0.f, max_of(most));
+    bool empty = !any_lane<LANES>(any);
+    if (!dense) {
+        top = max_of(most);
+        // sigmoids that are all 0 in 64 bits have weights of 0, whatever the logits
+        if (!softmax && p.renorm && top < -700.f) empty |= !(1. / (1. + exp(-(double)top)) > 0.);
+        if (!softmax) top = fminf(0.f, top);
+    }
     float sum = 0.f, dot = 0.f;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i) {
