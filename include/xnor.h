@@ -661,7 +661,8 @@ int xnor_route_bwd(const float *dweights, const void *logits, int type, long lon
  *   experts, weights   in   int32, fp32 [T][k], k <= 32, T k < 2^31
  *   wg, wu   in   stacks of E matrices [F][K], as for xnor_int4_gated       wd  in  a stack of E matrices [N][F]; E <= 1024
  *   out      out  [T][N], out_type any
- *   workspace  16-byte aligned, xnor_int4_experts_workspace_bytes bytes (host only); its contents mean nothing afterwards
+ *   workspace  16-byte aligned, xnor_int4_experts_workspace_bytes bytes (host only; of more than 2^18 pairs one run after the other is taken, so that
+ *              they do not grow further); its contents mean nothing afterwards
  */
 int xnor_int4_experts_workspace_bytes(long long T, int k, int E, int K, int F, int N, size_t *bytes);
 int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, const int32_t *experts, const float *weights, int k, int E,

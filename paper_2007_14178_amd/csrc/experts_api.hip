@@ -61,6 +61,10 @@ int check_experts(long long T, int k, int E)
     if (T < 0 || T > kMaxRows || k <= 0 || k > kMaxChosen || E <= 0 || E > kMaxExperts || T * k > kMaxRows) return XNOR_E_SHAPE;
     return XNOR_OK;
 }
+// Tokens whose pairs the workspace is for: longer calls take one run after the other, so that it does not grow with them.  (A run of 2^18 pairs reads each of 256
+// experts' weights for 1024 of them.)
+long long most_tokens(int k) { return std::max(1LL, (1LL << 18) / k); }
+
 struct ExpertParts {
     size_t offsets, order, lists, tiles, hidden, pairs, bytes;
     int tile;
@@ -236,7 +240,7 @@ int xnor_int4_experts_workspace_bytes(long long T, int k, int E, int K, int F, i
     if (!bytes) return XNOR_E_NULL;
     if (const int rc = check_experts(T, k, E)) return rc;
     if (K <= 0 || K > kMaxCols || F <= 0 || F > kMaxCols || N <= 0 || N > kMaxCols) return XNOR_E_SHAPE;
-    *bytes = T > 0 ? expert_parts(T, k, E, F, N).bytes : 0;
+    *bytes = T > 0 ? expert_parts(std::min(T, most_tokens(k)), k, E, F, N).bytes : 0;
     return XNOR_OK;
 }
 
@@ -255,7 +259,7 @@ int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, 
                           vec(workspace, T > 0 ? 1 : 0, 16)};
     if ((rc = check(all))) return rc;
     if (T == 0) return XNOR_OK;
-    ExpertParts at = expert_parts(T, k, E, F, N);
+    ExpertParts at = expert_parts(std::min(T, most_tokens(k)), k, E, F, N);
     if (workspace_bytes < at.bytes) return XNOR_E_WORKSPACE;
     char *const held = (char *)workspace;
     const hipStream_t st = (hipStream_t)stream;
@@ -273,24 +277,34 @@ int xnor_int4_experts(const void *x, int type, long long x_stride, long long T, 
         b.pairs = experts, b.E = E, b.chosen = k, b.terms = terms;
         return hip_status(launch_int4_down(b, weights, st));
     }
-    ListArgs l{};
-    l.experts = experts, l.pairs = T * k, l.E = E, l.offsets = (int32_t *)(held + at.offsets), l.order = (int32_t *)(held + at.order);
-    l.counts = (int32_t *)(held + at.lists), l.tiles = (ExpertTile *)(held + at.tiles);
-    // hidden: rows by sorted position; pairs: rows by token and slot
-    Int4Args a = args_of(x, 2 * x_stride, wg, wu, T * k, held + at.hidden, out_type, ldh);
-    a.act = act, a.tiles = l.tiles, a.order_x = l.order, a.E = E, a.chosen = k, a.out_terms = terms;
-    Int4Args b = args_of(held + at.hidden, 2 * ldh, wd, nullptr, T * k, held + at.pairs, XNOR_TYPE_FP32, N);
-    b.tiles = l.tiles, b.order_out = l.order, b.E = E, b.chosen = k, b.terms = terms;
-    if (!int4_tiles_support(a) || !int4_tiles_support(b)) at.tile = std::min(at.tile, kInt4Few);
-    l.tile = a.tile = b.tile = at.tile;
-    hipError_t e = launch_route_lists(l, st);
-    if (e == hipSuccess) e = launch_int4(a, type, true, st);
-    if (e == hipSuccess) e = launch_int4(b, XNOR_TYPE_BF16, false, st);
-    if (e != hipSuccess) return hip_status(e);
-    CombineArgs c{};
-    c.pairs = (const float *)(held + at.pairs), c.experts = experts, c.weights = weights, c.T = T, c.ldo = out_stride, c.k = k, c.E = E, c.N = N;
-    c.out = out, c.out_type = out_type;
-    return hip_status(launch_combine(c, st));
+    // Tokens in runs: of what the workspace is for, and of what tiles reach with 31 bits from a run's first token.  (Tokens so far apart that a run would be short are
+    // left to the kernel for few, which reaches all of them.)
+    const long long ldx = 2 * x_stride, reach = ldx > 0 ? std::max(0LL, kTileReach - 2LL * K) / ldx : T;
+    long long run = std::min(T, most_tokens(k));
+    if (reach >= std::min<long long>(T, 1024)) run = std::min(run, reach);
+    for (long long from = 0; from < T; from += run) {
+        const long long n = std::min(run, T - from);
+        ListArgs l{};
+        l.experts = experts + from * k, l.pairs = n * k, l.E = E, l.offsets = (int32_t *)(held + at.offsets), l.order = (int32_t *)(held + at.order);
+        l.counts = (int32_t *)(held + at.lists), l.tiles = (ExpertTile *)(held + at.tiles);
+        // hidden: rows by sorted position; pairs: rows by token and slot
+        Int4Args a = args_of((const char *)x + from * ldx, ldx, wg, wu, n * k, held + at.hidden, out_type, ldh);
+        a.act = act, a.tiles = l.tiles, a.order_x = l.order, a.E = E, a.chosen = k, a.out_terms = terms;
+        Int4Args b = args_of(held + at.hidden, 2 * ldh, wd, nullptr, n * k, held + at.pairs, XNOR_TYPE_FP32, N);
+        b.tiles = l.tiles, b.order_out = l.order, b.E = E, b.chosen = k, b.terms = terms;
+        if (!int4_tiles_support(a) || !int4_tiles_support(b)) at.tile = std::min(at.tile, kInt4Few);
+        l.tile = a.tile = b.tile = at.tile;
+        hipError_t e = launch_route_lists(l, st);
+        if (e == hipSuccess) e = launch_int4(a, type, true, st);
+        if (e == hipSuccess) e = launch_int4(b, XNOR_TYPE_BF16, false, st);
+        if (e != hipSuccess) return hip_status(e);
+        CombineArgs c{};
+        c.pairs = (const float *)(held + at.pairs), c.experts = l.experts, c.weights = weights + from * k, c.T = n, c.ldo = out_stride, c.k = k, c.E = E, c.N = N;
+        c.out = (char *)out + from * out_stride * os, c.out_type = out_type;
+        e = launch_combine(c, st);
+        if (e != hipSuccess) return hip_status(e);
+    }
+    return XNOR_OK;
 }
 
 }  // extern "C"

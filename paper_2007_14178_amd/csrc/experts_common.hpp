@@ -97,6 +97,7 @@ inline bool int4_pairs_pay(long long pairs, int E) { return pairs <= 4 || 4 * pa
 hipError_t launch_int4_down(const Int4Args &p, const float *weights, hipStream_t st);
 // GATED: w and w2 with the activation.
 hipError_t launch_int4_few(const Int4Args &p, int type, bool gated, hipStream_t st);
+constexpr long long kTileReach = 0x7fffffff;     // bytes from where a tile's buffers begin
 bool int4_tiles_support(const Int4Args &p);
 hipError_t launch_int4_tiles(const Int4Args &p, int type, bool gated, hipStream_t st);
 // By the number of tokens (experts: by the tiles that they were cut into).

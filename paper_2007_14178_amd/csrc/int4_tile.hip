@@ -330,7 +330,7 @@ hipError_t by_tiles(const Int4Args &p, hipStream_t st)
 // Whether a tile's operands are within 31 bits of where its buffers begin.
 bool int4_tiles_support(const Int4Args &p)
 {
-    constexpr long long kMost = 0x7fffffff;
+    constexpr long long kMost = kTileReach;
     if (p.M == 0) return true;
     const long long groups = (p.K + p.group - 1) / p.group, last = p.order_x ? p.M / p.chosen : 256;
     return last * p.ldx + 2LL * p.K <= kMost && kRows * p.ldq <= kMost && (groups + 1) * p.N * 4 <= kMost;
