@@ -81,18 +81,14 @@ __host__ __device__ inline int hidden_stride(int F) { return (F + 7) / 8 * 8; }
 
 // Tiles of more of an expert's tokens than this go to the kernel for many.
 constexpr int kInt4Few = 64;
-// Whether a product goes there: of more than 64 tokens unless that is little work (us on the kernel for few and for many, with its shares of the contraction:
-// 256 x 1024 x 1024 9.1 and 13.9, 128 x 4096 x 4096 22.2 and 27.1, 192 x 4096 x 4096 40.9 and 32.9, 128 x 8192 x 8192 74 and 48), and of more than 32 where the
-// contraction is long (40 x 2048 x 8192 25.8 and 20.3, 64 x 2048 x 8192 33.7 and 21.8, gated 64 x 8192 x 8192 72 and 55; 64 x 4096 x 4096 18.8 and 20.4).
-inline bool int4_many(long long M, long long N, long long K)
-{
-    return (M > kInt4Few && (M + 63) / 64 * N * K > 1LL << 23) || (M > kInt4Few / 2 && K >= 8192 && N * K >= 1LL << 23);
-}
-// Whether so few pairs are better taken each by itself, without lists: experts of several are read for each of theirs, from the caches mostly.  us, by
+// Whether a product of all of x's rows goes there, in so many shares of the contraction.
+bool int4_many(long long M, int N, int K, bool gated, int parts);
+// Whether so few pairs are better taken each by itself, without lists: experts of several are read for each of theirs, from the caches mostly.  us of GPU time, by
 // lists and by pairs, for tokens to k of E experts, width x hidden (bf16, groups of 128):
-//     8 of 64, 2048 x 1024    1: 21.9 16.2    4: 40.1 35.7    8: 51.3 61.9        2 of 8, 4096 x 2048     1: 18.7 13.4    2: 27.7 22.2    4: 31.9 37.3
-//     8 of 128, 2048 x 512    1: 17.8 10.6    8: 43.7 37.9   16: 60.4 67.4        4 of 32, 1024 x 768     4: 18.4 11.9    8: 23.7 19.3   16: 26.7 32.9
-inline bool int4_pairs_pay(long long pairs, int E) { return pairs <= 4 || 4 * pairs <= 3LL * E; }
+//     8 of 64, 2048 x 1024    1: 23.6 18.8    4: 45.9 40.3    6: 51.7 55.9        2 of 8, 4096 x 2048     1: 22.0 17.6    2: 31.2 28.0    3: 30.9 36.8
+//     8 of 128, 2048 x 512    1: 20.0 13.9    8: 48.2 48.0   12: 58.4 67.2        4 of 32, 1024 x 768     4: 20.4 14.9    6: 22.7 23.0    8: 22.5 24.4
+//     8 of 256, 2048 x 512    4: 35.4 28.1    8: 52.3 47.9   12: 64.9 67.4        4 of 16, 2048 x 2048    2: 31.0 24.5    3: 36.1 36.2    6: 43.4 55.6
+inline bool int4_pairs_pay(long long pairs, int E) { return pairs <= 4 || (2 * pairs <= E && pairs <= 64); }
 // A token's chosen experts' second products and their sum in one launch: x holds the rows of the pairs, weights their shares, M the tokens.
 hipError_t launch_int4_down(const Int4Args &p, const float *weights, hipStream_t st);
 // GATED: w and w2 with the activation.

@@ -429,7 +429,7 @@ hipError_t launch_int4_down(const Int4Args &p, const float *weights, hipStream_t
 
 hipError_t launch_int4(const Int4Args &p, int type, bool gated, hipStream_t st)
 {
-    const bool many = p.tiles ? p.tile > kInt4Few : !p.pairs && int4_many(p.M, p.N, p.K) && int4_tiles_support(p);
+    const bool many = p.tiles ? p.tile > kInt4Few : !p.pairs && int4_many(p.M, p.N, p.K, gated, p.parts) && int4_tiles_support(p);
     return many ? launch_int4_tiles(p, type, gated, st) : launch_int4_few(p, type, gated, st);
 }
 

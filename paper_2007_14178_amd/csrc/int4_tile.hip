@@ -7,6 +7,7 @@
 // 4096 x 8192 x 8192 bf16 650-760 us, 0.73-0.85 PFLOP/s.  With weights rounded to the tokens' type on their way, (level - zero) * scale, there are no scales to
 // multiply by and it takes 560-640, but outputs are up to 1.6 times as far from the exact ones as those of products in fp32.
 #include <algorithm>
+#include <cmath>
 
 #include "int4_common.hpp"
 
@@ -342,16 +343,40 @@ int int4_expert_tile(long long pairs, int E)
     return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : 128;
 }
 
-// Shares of the contraction for few tiles: a step takes a workgroup 0.75 us, whether it is alone on its unit or not quite.  As many as make a workgroup a unit,
-// of at least four steps, or two a unit where that leaves 20 steps each; at most 16.  us without and with 2, 4, 8, 16 shares (bf16, all
-// 10 to 20 % more since the scales went to the sums):
-//     128 x 2048 x 8192  102  -  35.6  -  25.8     128 x 4096 x 4096  54.8  -  25.8  -  30.7     128 x 8192 x 2048  32.4  -  18.9  24.1
-//     192 x 8192 x 8192  113  -  54.9              384 x 8192 x 2048  33.5  35.7                 gated 192 x 8192 x 2048  34.6  39.4
-int int4_tile_parts(long long M, int N, int K, bool gated)
+// Shares of the contraction for few tiles: a step takes a workgroup 1.1 us, whether it is alone on its unit or not quite.  As many as make a workgroup a unit,
+// of at least four steps, or two a unit where that leaves 20 steps each; at most 16.  us of GPU time with 1, 2, 4, 8, 16 shares (bf16, groups of 128):
+//     128 x 2048 x 8192  134  73  43  30  25      128 x 4096 x 4096  71  43  30  27  30      128 x 8192 x 2048    40  26  20  26  36
+//     192 x 8192 x 8192  136  78  62  69  86      384 x 8192 x 2048  40  40  43  58  90      gated 192 x 8192 x 2048  42  43  55  81
+//     512 x 4096 x 4096   72  47  42  52  73      640 x 4096 x 4096  73  61  57  63  89      gated 128 x 8192 x 8192 136  82  69  82
+static int shares(long long M, int N, int K, bool gated)
 {
-    if (!int4_many(M, N, K)) return 1;
     const long long tiles = (M + 127) / 128 * ceil_div(N, gated ? 64 : 128), units = compute_units(), steps = K / kDeep;
     return (int)std::min<long long>(16, std::max<long long>({1, std::min(units / tiles, steps / 4), std::min(2 * units / tiles, steps / 20)}));
+}
+
+// By what both kernels take in us of GPU time, which these two forms meet within a tenth (880 products of 33 to 2048 tokens, 512 to 16384 rows, contractions of 512 to
+// 16384, linear and gated, bf16): the kernel for few a step of 1024 values at a time, in rounds of workgroups of 64 tokens; the tiles a step of 64, in rounds of
+// theirs, with their shares' sums.  The kernel for few has to be a seventh faster: of two that are near the tiles are taken (its loss to the faster of both is then
+// 1.0 % on the mean and 30 % at most; without that margin 0.5 %; a limit on M N K and one on K, as before, 4.2 % and 86 %).  Few and tiles:
+//     64 x 1024 x 4096   18.7 15.2    64 x 2048 x 8184  23.8 22.1     64 x 4096 x 4096  19.1 20.4     64 x 8192 x 8192  39.5 39.3     33 x 8192 x 8192  28.9 37.1
+//     128 x 2048 x 4096  19.3 22.9   128 x 4096 x 6144  29.8 27.9    256 x 4096 x 4096  38.5 31.4    256 x 2048 x 2048  13.3 22.4     64 x 512 x 8192   34.1 18.3
+bool int4_many(long long M, int N, int K, bool gated, int parts)
+{
+    if (M <= kInt4Few / 2) return false;
+    const double units = compute_units();
+    const long long rows = (M + 63) / 64, wide = rows * ceil_div(N, 32);
+    const double groups = (double)(gated || wide < units ? rows * ceil_div(N, 16) : wide);
+    const double few = 5.2 + K / 1024. * (1. + 0.044 * std::min<long long>(M, 64) + (gated ? 0.17 : 0.)) * (1. + 1.14 * (std::ceil(groups / units) - 1.));
+    const double tiles = (double)((M + 127) / 128) * ceil_div(N, gated ? 64 : 128) * parts;
+    const double sums = parts > 1 ? 2.35e-6 * parts * M * N * (gated ? 2 : 1) - 3. : 0.;
+    const double many = 11.6 + 0.99 * std::ceil(K / 64.) / parts * (1. + 0.69 * std::max(0., tiles / units - 1.)) + sums;
+    return few > 0.87 * many;
+}
+
+int int4_tile_parts(long long M, int N, int K, bool gated)
+{
+    const int parts = M > 0 ? shares(M, N, K, gated) : 1;
+    return int4_many(M, N, K, gated, parts) ? parts : 1;
 }
 
 hipError_t launch_int4_tiles(const Int4Args &p, int type, bool gated, hipStream_t st)
