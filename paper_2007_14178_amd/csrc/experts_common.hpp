@@ -73,7 +73,7 @@ struct Int4Args {
 };
 // Between the experts' two products a value is held as the sum of bf16 ones: two hold 16 bits of it (outputs in 16 bits are then as far from the definition as
 // those of products in fp32; rounded to the tokens' type they are 1.35 to 1.5 times as far), three the 24 of fp32, for outputs in fp32.  bf16 for f16 tokens
-// too: a block's outputs may pass f16's largest value.  (4096 tokens to 8 of 64 experts, 2048 x 1024, bf16: 1076 us, with hidden values in bf16 837; 24 tokens to 3 of 30
+// too: a block's outputs may pass f16's largest value.  (4096 tokens to 8 of 64 experts, 2048 x 1024, bf16: 1030-1075 us, with hidden values in bf16 837; 24 tokens to 3 of 30
 // 37.9 and 32.8, one token to 8 of 64 18.9 and 17.2.)
 constexpr int kMostTerms = 3;
 inline int hidden_terms(int out_type) { return out_type == XNOR_TYPE_FP32 ? 3 : 2; }

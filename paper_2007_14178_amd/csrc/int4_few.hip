@@ -5,8 +5,9 @@
 // turn the four words of the four lanes of a row about, so that instruction i takes the values 32 i .. 32 i + 31, which have one scale.
 // A group's sum is multiplied by its scale in fp32: the weights are never rounded.  Some steps' loads are on their way together, behind no branch; their
 // scales and zero points come with one load each, and reach the lanes that need them through LDS.
-// (GPU time, bf16: 1 x 4096 x 4096 5.8 us, a launch and two loads' latencies; gated 1 x 4096 x 8192 in groups of 64 with zero points 12.9 us, 2.9 TB/s: 58 vector
-// instructions for a step's 16 rows, beside the loads; 16, 32 and 64 x 8192 x 8192 17.4, 24.3 and 39.2 us, whose tokens each workgroup reads again.)
+// (GPU time, bf16, weights in the last-level cache and from memory: 1 x 4096 x 4096 5.7 and 7.3 us, a launch and two loads' latencies; gated 1 x 4096 x 8192 in groups of 64
+// with zero points 14.0-14.9 and 15.6 us, 2.4 TB/s: 70 vector instructions a step and matrix are about 7 us of it, and a wave has one step of loads on its way.  16, 32 and
+// 64 x 8192 x 8192 17.6, 24.7 and 39.0 us, whose tokens each workgroup reads again.)
 #include <algorithm>
 #include <cstddef>
 
@@ -326,8 +327,8 @@ hipError_t few_of(const Int4Args &p, hipStream_t st)
 template <class T, bool GATED, int TT>
 hipError_t few(const Int4Args &p, hipStream_t st)
 {
-    // Four waves where there is a workgroup for each unit (24 tokens to 3 of 30 experts, 1100 x 777, in groups of 32: 16.9 and 13.4 us, with eight 19.9 and 16.0;
-    // 1 x 4096 x 4096 6.1 and 6.0), eight where there are fewer
+    // Four waves where there is a workgroup for each unit (24 tokens to 3 of 30 experts, 1100 x 777, in groups of 32, hidden values in f16: 16.9 and 13.4 us, with eight 19.9
+    // and 16.0; 1 x 4096 x 4096 6.1 and 6.0), eight where there are fewer
     const long long tiles = p.pairs || p.tiles ? p.M : (p.M + 16 * TT - 1) / (16 * TT);
     // (and of one matrix twice 16 rows where that leaves a workgroup a unit: 64 x 8192 x 8192 41 us, by 16 rows 67, x 4096 x 4096 21.8 and 20.4)
     const long long units = compute_units();
