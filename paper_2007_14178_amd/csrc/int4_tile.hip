@@ -355,23 +355,24 @@ static int shares(long long M, int N, int K, bool gated)
     return (int)std::min<long long>(16, std::max<long long>({1, std::min(units / tiles, steps / 4), std::min(2 * units / tiles, steps / 20)}));
 }
 
-// By what both kernels take in us of GPU time, which these two forms meet within a tenth (880 products of 33 to 2048 tokens, 512 to 16384 rows, contractions of 512 to
-// 16384, linear and gated, bf16): the kernel for few a step of 1024 values at a time, in rounds of workgroups of 64 tokens; the tiles a step of 64, in rounds of
-// theirs, with their shares' sums.  The kernel for few has to be a seventh faster: of two that are near the tiles are taken (its loss to the faster of both is then
-// 1.0 % on the mean and 30 % at most; without that margin 0.5 %; a limit on M N K and one on K, as before, 4.2 % and 86 %).  Few and tiles:
+// By what both kernels take in us of GPU time, which these two forms meet within a tenth (926 products of 33 to 100000 tokens, 64 to 65536 rows, contractions of 60 to
+// 16384, linear and gated, bf16): of each a round of workgroups, a contraction and what a workgroup begins and ends with, then the rounds that follow, and the
+// shares' sums.  The kernel for few has to be a tenth faster: of two that are near the tiles are taken (the loss to the faster of both is then 1.0 % on the mean
+// and 30 % at most, without that margin 0.4 %; of a limit on M N K and one on K it is 4.4 % and a factor of 3.5).  Few and tiles:
 //     64 x 1024 x 4096   18.7 15.2    64 x 2048 x 8184  23.8 22.1     64 x 4096 x 4096  19.1 20.4     64 x 8192 x 8192  39.5 39.3     33 x 8192 x 8192  28.9 37.1
 //     128 x 2048 x 4096  19.3 22.9   128 x 4096 x 6144  29.8 27.9    256 x 4096 x 4096  38.5 31.4    256 x 2048 x 2048  13.3 22.4     64 x 512 x 8192   34.1 18.3
+//     8200 x 1030 x 70   59.0 25.9  4096 x 512 x 512    17.7 24.8    4096 x 8192 x 64     191 40.2    8192 x 512 x 1024  45.9 27.8   32768 x 64 x 1024 29.0 27.7
 bool int4_many(long long M, int N, int K, bool gated, int parts)
 {
     if (M <= kInt4Few / 2) return false;
     const double units = compute_units();
     const long long rows = (M + 63) / 64, wide = rows * ceil_div(N, 32);
     const double groups = (double)(gated || wide < units ? rows * ceil_div(N, 16) : wide);
-    const double few = 5.2 + K / 1024. * (1. + 0.044 * std::min<long long>(M, 64) + (gated ? 0.17 : 0.)) * (1. + 1.14 * (std::ceil(groups / units) - 1.));
+    const double few = 2.2 + (2.5 + K / 1024. * (0.86 + 0.053 * std::min<long long>(M, 64) + (gated ? 0.17 : 0.))) * (1. + 0.74 * (std::ceil(groups / units) - 1.));
     const double tiles = (double)((M + 127) / 128) * ceil_div(N, gated ? 64 : 128) * parts;
-    const double sums = parts > 1 ? 2.35e-6 * parts * M * N * (gated ? 2 : 1) - 3. : 0.;
-    const double many = 11.6 + 0.99 * std::ceil(K / 64.) / parts * (1. + 0.69 * std::max(0., tiles / units - 1.)) + sums;
-    return few > 0.87 * many;
+    const double sums = parts > 1 ? 2.31e-6 * parts * M * N * (gated ? 2 : 1) - 2.1 : 0.;
+    const double many = (11.4 + 1.06 * std::ceil(K / 64.) / parts) * (1. + 0.39 * std::max(0., tiles / units - 1.)) - 1. + sums;
+    return few > 0.9 * many;
 }
 
 int int4_tile_parts(long long M, int N, int K, bool gated)

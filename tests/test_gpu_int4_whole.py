@@ -67,7 +67,7 @@ def test_a_token_that_meets_zero_points_costs_nothing(xb, M, group, zeros, dtype
 
 # few tokens by every kernel; tiles; tiles in shares of the contraction; contractions that end inside a step, behind very long ones too
 SIZES = [(1, 50, 1), (13, 50, 33), (20, 50, 129), (33, 40, 41), (40, 2050, 65), (64, 9000, 39), (64, 300, 1031), (128, 50, 393), (65, 300, 30000), (129, 1100, 2600),
-         (200, 1024, 4095), (1000, 520, 1100), (8200, 1030, 70), (90, 1, 5000000), (40, 1030, 8200), (33, 2050, 8195), (300, 1024, 4096)]
+         (200, 1024, 4095), (1000, 520, 1100), (8200, 1030, 70), (90, 1, 5000000), (40, 1030, 8200), (33, 2050, 8195), (300, 1024, 4096), (40000, 300, 60), (3000, 70, 520)]
 
 
 def marked(K, gen):
