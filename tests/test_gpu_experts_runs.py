@@ -62,3 +62,30 @@ def test_tokens_far_apart(xb, T, apart):
     want, _, _ = definition(x, chosen, share, *w)
     got = xb.xnor_int4_experts(far, chosen.cuda(), share.cuda(), *w, act=ref.RELU, out_dtype=F32)
     assert torch.equal(got.cpu().double(), want)
+
+
+def test_runs_replayed(xb):
+    """A call of two runs and one of a single run captured with one workspace, replayed in turn with other tokens beside eager calls."""
+    T, k, E = 131073, 2, 5
+    x, chosen, share, w = case(xb, T, k, E, 24, 20, 36)
+    x, chosen, share = x.cuda(), chosen.cuda(), share.cuda()
+    space = torch.empty(xb.xnor_int4_experts_workspace_bytes(T, k, E, 24, 20, 36), dtype=torch.uint8, device="cuda")
+    outs = [torch.empty(n, 36, device="cuda") for n in (T, 700)]
+
+    def call(n, out=None, workspace=None):
+        return xb.xnor_int4_experts(x[:n], chosen[:n], share[:n], *w, act=ref.RELU, out=out, out_dtype=F32 if out is None else None, workspace=workspace)
+    for out in outs:
+        call(len(out), out, space)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for graph, out in zip(graphs, outs):
+        with torch.cuda.graph(graph):
+            call(len(out), out, space)
+    for seed in range(3):
+        x.copy_(torch.randint(-1, 2, x.shape, generator=torch.Generator().manual_seed(seed)))
+        eager = [call(len(out)) for out in outs]
+        torch.cuda.synchronize()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, outs))
